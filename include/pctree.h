@@ -64,6 +64,8 @@ extern "C" {
 #define PCTREE_MAX_RANK_BF16 512 /* and rank % 32 == 0 */
 #define PCTREE_MAX_RANK_F32 128  /* and rank % 16 == 0 */
 #define PCTREE_MAX_MASK_BUDGET 1024
+#define PCTREE_MAX_PAGE_SIZE 1024
+#define PCTREE_MAX_PAGED_SLOTS (1 << 30) /* max_pages * page_size */
 
 typedef enum pctree_status {
   PCTREE_OK = 0,
@@ -74,8 +76,9 @@ typedef enum pctree_status {
 } pctree_status;
 
 typedef enum pctree_dtype {
-  PCTREE_F32 = 0, /* float32 base logits and head weights */
-  PCTREE_BF16 = 1 /* bfloat16 base logits and head weights, fp32 accumulation */
+  PCTREE_F32 = 0,  /* float32 base logits and head weights */
+  PCTREE_BF16 = 1, /* bfloat16 base logits and head weights, fp32 accumulation */
+  PCTREE_F16 = 2   /* float16: paged caches and sampled logits only */
 } pctree_dtype;
 
 /* Scoring of a parent's children (Sec. 5.3 compares the three).  Other
@@ -297,6 +300,130 @@ pctree_status pctree_tree_attention(const pctree_attn_shape* shape, const void* 
                                     const uint32_t* mask, const int32_t* count,
                                     const int32_t* prefix_len, void* out, void* workspace,
                                     size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------
+ * The target's verification step over a paged cache (Sec. 4.2: "one target
+ * forward"; App. A): a target that serves many requests keeps its keys and
+ * values in pages of a pool.  pctree_append_paged norms and rotates the new
+ * rows' queries and keys and puts keys and values into their pages,
+ * pctree_paged_attention lets a chunk of new rows (part of a prompt, one
+ * token, or a tree) attend to the request's pages, pctree_sample draws the
+ * target's token at every row, and pctree_compact_paged is pctree_compact_kv
+ * for pages.
+ *
+ * Slot s of request r is slot s % page_size of page page_table[r][s / page_size].
+ * A page index outside [0, pages) is no page: its slots are neither read nor
+ * written and are admitted by no row (so unused entries may hold anything).
+ * --------------------------------------------------------------------- */
+
+/* One layer's keys and values. */
+typedef struct pctree_paged_cache {
+  void* k;             /* [pages][Hkv][page_size][D] dtype                              */
+  void* v;             /* the same layout                                               */
+  int64_t page_stride; /* elements between two pages of k (and of v): a multiple of 8,
+                          at least Hkv * page_size * D; more than that where pages lie
+                          in a larger pool                                              */
+  int32_t pages;       /* pages of the pool                                             */
+  int32_t page_size;   /* slots of a page: a power of two, at most PCTREE_MAX_PAGE_SIZE */
+  int32_t kv_heads;    /* Hkv                                                           */
+  int32_t head_dim;    /* D: 64 or 128                                                  */
+  int32_t dtype;       /* PCTREE_BF16 or PCTREE_F16                                     */
+} pctree_paged_cache;
+
+/* Which rows of a call belong to which request.  Row row_start[r] + i, i <
+ * row_count[r], is request r's i-th new row and sits at slot prefix_len[r] + i.
+ * Rows of different requests must not overlap; rows of no request are neither
+ * read nor written.  Device arrays, so one captured graph serves changing
+ * batches; what they hold is clamped: a start outside [0, rows] gives no rows,
+ * counts to [0, min(max_rows, rows - start)], prefixes to [0, capacity], with
+ * capacity = max_pages * page_size.  Slots at or past capacity do not exist. */
+typedef struct pctree_paged_batch {
+  const int32_t* row_start;  /* [R]                                          */
+  const int32_t* row_count;  /* [R]                                          */
+  const int32_t* prefix_len; /* [R] slots in the cache before the new rows   */
+  const int32_t* page_table; /* [R][max_pages]                               */
+  int32_t requests;          /* R                                            */
+  int32_t max_pages;         /* width of the page table                      */
+  int32_t rows;              /* T: rows of q, k, v and out                   */
+  int32_t max_rows;          /* the most rows that a request has, <= rows    */
+} pctree_paged_batch;
+
+/* New rows of one layer.  Head h of row t starts at element t * row_stride +
+ * h * D (so a fused projection's output needs no split); strides and pointers
+ * are multiples of 8 elements and 16 bytes. */
+typedef struct pctree_append {
+  const void* q;           /* [T][Hq][D], or NULL: keys and values only               */
+  const void* k;           /* [T][Hkv][D]                                             */
+  const void* v;           /* [T][Hkv][D]                                             */
+  void* q_out;             /* [T][Hq][D] (may be q itself); NULL iff q is             */
+  int64_t q_stride;        /* row strides in elements, >= heads * D                   */
+  int64_t k_stride;
+  int64_t v_stride;
+  int64_t q_out_stride;
+  const void* q_norm;      /* [D] dtype weight of the queries' norm, or NULL: none    */
+  const void* k_norm;      /* [D] dtype weight of the keys' norm, or NULL: none       */
+  const float* rope;       /* [positions][rot_dim]: cos of the position's rot_dim / 2
+                              angles, then their sines; or NULL: no rotation          */
+  const int32_t* position; /* [T], or NULL: a row's position is its slot              */
+  float eps;               /* of the norms, >= 0                                      */
+  int32_t q_heads;         /* Hq (0 where q is NULL)                                  */
+  int32_t rot_dim;         /* rotated leading elements of a head: a multiple of 16, <= D */
+  int32_t positions;       /* rows of rope                                            */
+  int32_t interleaved;     /* 0: element i turns with i + rot_dim / 2; 1: 2 i with 2 i + 1 */
+} pctree_append;
+
+/* For every row t of a request: y = x * rsqrt(mean(x^2) + eps) * weight per
+ * head of q and k (where there is a weight), then (a, b) -> (a cos - b sin,
+ * b cos + a sin) for the pairs of the first rot_dim elements; q goes to q_out,
+ * k and the unchanged v to the row's slot.  float32 throughout, one rounding
+ * at the end.  A position outside [0, positions) is clamped to that range.
+ * Rows whose slot does not exist only have their q written. */
+pctree_status pctree_append_paged(const pctree_paged_cache* cache, const pctree_paged_batch* batch,
+                                  const pctree_append* rows, void* stream);
+
+/* Workspace bytes pctree_paged_attention needs (0: none, or invalid arguments).
+ * Depends on sizes only (head counts, D, requests, max_pages, page_size, rows,
+ * max_rows), not on pointers.  Pure host arithmetic. */
+size_t pctree_paged_attention_workspace_bytes(const pctree_paged_cache* cache,
+                                              const pctree_paged_batch* batch, int32_t q_heads);
+
+/* out[t][h] = sum_s softmax_s(scale * q[t][h] . k[s][h/g]) v[s][h/g], g = Hq /
+ * Hkv, for every row t of a request, over the admitted slots s:
+ * - mask NULL: causal; the request's i-th row admits [0, prefix + i];
+ * - else its row i admits the prefix and prefix + j for every bit j < count of
+ *   mask row [r][i] ([R][budget][(budget+31)/32], as from pctree_build_mask);
+ *   counts are also clamped to budget.
+ * q and out [T][Hq][D] dtype, contiguous; float32 scores, softmax and sums, the
+ * weights rounded to dtype before the weighted sum.  Rows that admit no slot
+ * are zero.  The pages must already hold the new rows' keys and values
+ * (pctree_append_paged).  Slots past the request's last row are never read; a
+ * slot before it that a row does not admit adds nothing to that row, whatever
+ * it holds (infinities and NaN included).
+ * Errors: as for pctree_tree_attention; UNSUPPORTED also for a page_size that
+ * is no power of two or beyond its limit, R > 65535, and
+ * max_pages * page_size > PCTREE_MAX_PAGED_SLOTS. */
+pctree_status pctree_paged_attention(const pctree_paged_cache* cache,
+                                     const pctree_paged_batch* batch, const void* q,
+                                     int32_t q_heads, float scale, const uint32_t* mask,
+                                     int32_t budget, void* out, void* workspace,
+                                     size_t workspace_bytes, void* stream);
+
+/* Compaction in pages: pool holds, per group (e.g. one layer's K or V), `pages`
+ * pages of [heads][page_size][slot_bytes]; group g's page p starts at byte
+ * g * group_stride + p * page_stride.  Tree node i of request r sits at slot
+ * prefix_len[r] + i; the accepted nodes n_0..n_a (accept_node [R][W],
+ * accept_len [R] from pctree_accept_greedy) move, in place, to slots
+ * prefix_len[r] + 0..a.  Other slots keep their contents.  A request is left
+ * untouched if its accepted nodes are not strictly increasing, not below
+ * budget, or lie on (or move to) slots that do not exist.  slot_bytes and the
+ * strides are multiples of 16. */
+pctree_status pctree_compact_paged(void* pool, int64_t group_stride, int64_t page_stride,
+                                   int32_t groups, int32_t pages, int32_t heads,
+                                   int32_t page_size, int32_t slot_bytes,
+                                   const int32_t* page_table, int32_t max_pages,
+                                   const int32_t* prefix_len, const int32_t* accept_node,
+                                   const int32_t* accept_len, int32_t requests, int32_t budget,
+                                   int32_t max_depth, void* stream);
 
 /* Static, human-readable name of a status code. */
 const char* pctree_status_string(pctree_status status);

@@ -45,14 +45,10 @@
 
 #include "pctree_attention.h"
 #include "pctree_lds.h"
+#include "pctree_tile.h"
 
 namespace pctree {
 namespace {
-
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kGroupThreads = 256;  // a slot group: 4 waves
 constexpr int kColTiles = 2;       // 16-row MFMA column tiles per wave
@@ -60,70 +56,8 @@ constexpr int kRowsPerWave = 16 * kColTiles;
 constexpr int kRowsPerBlock = 4 * kRowsPerWave;  // query rows of one workgroup
 constexpr int kChunk = 64;         // key slots per LDS stage (two 32-slot halves)
 constexpr int kMaxSplits = 32;     // slot runs of a layer at most
-constexpr int kXcds = 8;           // L2 domains the dispatcher deals workgroups over
 constexpr int kMergeThreads = 256;
 constexpr int kMergeBatch = 8;     // slot runs whose loads one merge thread issues together
-constexpr float kNegInf = -__builtin_inff();
-
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-
-__device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
-
-// Two floats to packed bf16 (round to nearest even), the low half first.
-__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
-  bf16x2 v;
-  v[0] = (__bf16)lo;
-  v[1] = (__bf16)hi;
-  return __builtin_bit_cast(uint32_t, v);
-}
-
-__device__ __forceinline__ f32x4 mfma_bf16(u32x4 a, u32x4 b, f32x4 c) {
-  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a),
-                                                  __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
-}
-
-// Permutation of the 16-byte units of a K or V row in LDS (an XOR of the unit
-// index).  A K fragment read takes one unit of the 16 rows {0..3, 8..11,
-// 16..19, 24..27} (+ 4, + 32); with 256-byte rows all of them start in one
-// bank, so the four row bits that vary choose among the 16 units (rows of 128
-// bytes alternate between two halves of the banks: three bits choose among
-// 8).  A V fragment read takes 32 bytes (two units) of four consecutive keys
-// per lane group: pairs of units are permuted by the key's low two bits and
-// its bit 3, all that fits the 8 pairs (or two of the three, D = 64).
-template <int D>
-__device__ __forceinline__ int k_unit(int row) {
-  return D == 128 ? (row & 3) | ((row >> 1) & 12) : ((row >> 1) & 1) | ((row >> 2) & 6);
-}
-template <int D>
-__device__ __forceinline__ int v_unit(int row) {
-  return D == 128 ? ((row & 3) << 1) | (row & 8) : (row & 2) | ((row >> 1) & 4);
-}
-
-// Every vector-memory load of the wave has landed, those into LDS among them.
-__device__ __forceinline__ void wait_loads() {
-  __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0)
-  __atomic_signal_fence(__ATOMIC_SEQ_CST);
-}
-// A workgroup barrier for LDS traffic.
-__device__ __forceinline__ void lds_barrier() {
-  __atomic_signal_fence(__ATOMIC_SEQ_CST);
-  __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
-  __builtin_amdgcn_s_barrier();
-  __atomic_signal_fence(__ATOMIC_SEQ_CST);
-}
-
-// Transposing LDS read: in each 16 lanes, lanes 4 i .. 4 i + 3 address row i (16
-// consecutive 16-bit values), and lane l receives column l of rows 0 .. 3.
-typedef short s16x4 __attribute__((ext_vector_type(4)));
-__device__ __forceinline__ u32x2 read_tr(const uint16_t* src) {
-  return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-      (__attribute__((address_space(3))) s16x4*)src));
-}
-
-// Low `n` bits set, n in [0, 64].
-__device__ __forceinline__ uint64_t low_bits(int n) {
-  return n >= 64 ? ~0ull : ((1ull << n) - 1ull);
-}
 
 // Admitted key range of request r: [0, prefix + count) clamped to the cache.
 struct ReqRange {
@@ -173,19 +107,6 @@ __device__ __forceinline__ Work work_of(const AttnArgs& a, int qblocks, int nspl
     w.r = __builtin_ctzll(__ballot(rank == w.r));
   }
   return w;
-}
-
-// Maximum over the four lanes that hold one query row (lanes l, l ^ 16,
-// l ^ 32, l ^ 48), exchanged on the VALU (v_permlane{16,32}_swap return the
-// lane's own value and its partner's, in a lane-dependent order that a
-// maximum does not care about).
-__device__ __forceinline__ float row_max4(float v) {
-  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false,
-                                                   false);
-  v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
-  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false,
-                                                   false);
-  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 
 // Online softmax of one 16-row column tile over a 64-slot chunk.  s[h][t]

@@ -1,0 +1,514 @@
+// Attention of a chunk of new rows over a paged cache (part of a prompt, one
+// token, or a tree to verify): out_i = sum_s w_is v_s, w_is = softmax over the
+// slots s that row i admits of scale q_i . k_s.
+//
+// Layout (bf16 or float16): q and out [T][Hq][D], pages [Hkv][page_size][D];
+// query head h reads key/value head h / g, g = Hq / Hkv.  The g heads of a
+// key/value head are rows of one matrix, row rho = i * g + (h mod g) of request
+// row i, so that K and V are read once for all of them.
+//
+// One workgroup takes 128 such rows and a run of slots.  K and V of a 64-slot
+// chunk go from their pages straight into LDS, one chunk ahead; every lane holds
+// the page of one slot of the chunk, read another chunk ahead, and the lanes
+// that load a slot's row fetch its page from that lane.  A wave computes
+// S^T = K Q^T and O^T += V^T P^T on MFMA 16x16x32 for its 32 rows, with an online
+// softmax in base 2 (32-bit maximum, sum and output); the two K tiles of a pair
+// are arranged so that a lane ends with 8 consecutive slots of its row, the B
+// operand of the second product.  The weights are rounded to 16 bits there, an
+// operand of the matrix units; their sum is not.
+//
+// Masked slots: scores are replaced, not added to, so K may hold anything.  A
+// weight of zero times an infinite or NaN value would still be NaN, so in chunks
+// that some row sees only in part such values are replaced first, and the rows
+// that do admit them are mended afterwards.
+#include "pctree.h"
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "pctree_lds.h"
+#include "pctree_paged.h"
+#include "pctree_tile.h"
+
+namespace pctree {
+namespace {
+
+constexpr int kChunk = 64;
+constexpr int kThreads = 256;
+constexpr int kWaves = kThreads / 64;
+constexpr int kColTiles = 2;
+constexpr int kRowsPerWave = 16 * kColTiles;
+constexpr int kRowsPerBlock = kWaves * kRowsPerWave;
+constexpr int kMaxSplits = 32;
+constexpr int kMergeThreads = 256;
+constexpr int kMergeBatch = 8;
+// float16 weights are 2^12 times the softmax's (as is their sum): weights down
+// to 2^-36 of the row's largest then stay above float16's smallest, 2^-24, and
+// the largest is 4096.
+constexpr float kHalfLift = 12.0f;
+
+// Slots per run of a request whose rows end at slot `end`.
+__device__ __forceinline__ int run_slots(int end, int nsplit) {
+  const int chunks = (end + kChunk - 1) / kChunk;
+  const int ns = min(nsplit, max(1, chunks / 2));
+  return (chunks + ns - 1) / ns * kChunk;
+}
+
+// End of the slots that row i may admit.
+__device__ __forceinline__ int row_end(const PagedAttnArgs& a, const PagedReq& q, int i) {
+  return min(q.prefix + (a.mask ? q.cnt : i + 1), a.b.C);
+}
+
+struct Work {
+  int r, kvh, split, qb;
+  bool ok;
+};
+// Row blocks of one (request, kv head, run) read the same K and V: they are
+// given block ids that land on one XCD (ids are dealt round-robin).  Blocks of
+// later rows, which see more slots, come first.
+__device__ __forceinline__ Work work_of(const PagedAttnArgs& a) {
+  const int b = blockIdx.x, j = b / kXcds;
+  const int grp = (j / a.qblocks) * kXcds + b % kXcds;
+  Work w;
+  w.ok = grp < a.b.R * a.Hkv * a.nsplit;
+  w.qb = a.qblocks - 1 - j % a.qblocks;
+  w.split = grp % a.nsplit;
+  w.kvh = grp / a.nsplit % a.Hkv;
+  w.r = grp / a.nsplit / a.Hkv;
+  return w;
+}
+
+// Online softmax of one 16-row column tile over a chunk: s[h][t] holds the raw
+// scores of half h, tile t (slots 32 h + 8 grp + 4 t + e); bit 8 h + i of `adm` is
+// set when slot 32 h + 8 grp + i is admitted (ignored when `all`).  Writes the
+// weights as B operands and returns the factor for the output so far.
+template <bool H>
+__device__ __forceinline__ float softmax_chunk(const f32x4 (&s)[2][2], uint32_t adm, bool all,
+                                               float c, float& m, float& l, u32x4 (&bp)[2]) {
+  float v[16];
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      v[8 * h + e] = s[h][0][e];
+      v[8 * h + 4 + e] = s[h][1][e];
+    }
+  if (!all) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = ((adm >> i) & 1u) ? v[i] : kNegInf;
+  }
+  float cmax = v[0];
+#pragma unroll
+  for (int i = 1; i < 16; ++i) cmax = fmaxf(cmax, v[i]);
+  const float mx = row_max4(cmax);
+  float alpha = 1.0f;
+  if (__any(mx > m)) {
+    const float mn = fmaxf(m, mx);
+    alpha = mn == m ? 1.0f : exp2_hw((m - mn) * c);  // m = -inf: 0
+    m = mn;
+    l *= alpha;
+  }
+  const float off = (m == kNegInf ? 0.0f : m * c) - (H ? kHalfLift : 0.0f);
+  float ps = 0.0f;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    v[i] = exp2_hw(__builtin_fmaf(v[i], c, -off));
+    ps += v[i];
+  }
+  l += ps;
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) bp[h][i] = pack16<H>(v[8 * h + 2 * i], v[8 * h + 2 * i + 1]);
+  return alpha;
+}
+
+// Admitted slots of the chunk at c0 for row i, the 16 bits of lane group grp
+// (bits 8 h + j for slot 32 h + 8 grp + j).  mw: the row's mask words in LDS.
+__device__ __forceinline__ uint32_t admitted(const PagedAttnArgs& a, const PagedReq& q,
+                                             const uint32_t* mw, int i, int c0, int kend,
+                                             uint64_t bad, int grp) {
+  uint64_t win;
+  if (a.mask) {
+    const int j0 = c0 - q.prefix;
+    const int wb = j0 >> 5, sh = j0 & 31;  // (floor)
+    const uint32_t w0 = wb >= 0 && wb < a.NW ? mw[wb] : 0u;
+    const uint32_t w1 = wb + 1 >= 0 && wb + 1 < a.NW ? mw[wb + 1] : 0u;
+    const uint32_t w2 = wb + 2 >= 0 && wb + 2 < a.NW ? mw[wb + 2] : 0u;
+    const uint64_t lo64 = ((uint64_t)w1 << 32) | w0;
+    const uint64_t tree = sh ? (lo64 >> sh) | ((uint64_t)w2 << (64 - sh)) : lo64;
+    const int np = min(max(-j0, 0), kChunk);
+    win = low_bits(np) | (tree & ~low_bits(np));
+  } else {
+    win = low_bits(min(max(q.prefix + i + 1 - c0, 0), kChunk));
+  }
+  win &= low_bits(min(max(kend - c0, 0), kChunk)) & ~bad;
+  return ((uint32_t)(win >> (8 * grp)) & 0xffu) | ((uint32_t)(win >> (32 + 8 * grp)) & 0xffu) << 8;
+}
+
+// Whether a 16-bit value is an infinity or NaN; a packed pair without such values.
+template <bool H>
+__device__ __forceinline__ bool odd16(uint32_t w) {
+  constexpr uint32_t E = H ? 0x7c00u : 0x7f80u;
+  return (w & E) == E;
+}
+template <bool H>
+__device__ __forceinline__ uint32_t fine_pair(uint32_t w) {
+  return (odd16<H>(w) ? 0u : w & 0xffffu) | (odd16<H>(w >> 16) ? 0u : w & 0xffff0000u);
+}
+
+template <int D, bool H>
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) void paged_attn_kernel(
+    PagedAttnArgs a) {
+  constexpr int KS = D / 32, DT = D / 16, UPR = D / 8, CT = kColTiles;
+  constexpr int TILE = kChunk * D;
+  constexpr int IPW = kChunk * UPR / kThreads;  // load instructions per wave, chunk and tensor
+  __shared__ __attribute__((aligned(16))) uint16_t sKV[2][2][TILE];
+  __shared__ int sOdd;  // values were set to zero because some row may not admit them
+  extern __shared__ uint32_t sMask[];
+
+  const Work wk = work_of(a);
+  if (!wk.ok) return;
+  const PagedReq rq = paged_req(a.b, wk.r);
+  const int cnt = a.mask ? min(rq.cnt, a.N) : rq.cnt;
+  PagedReq q = rq;
+  q.cnt = cnt;
+  const int rows = cnt * a.g, rho0 = wk.qb * kRowsPerBlock;
+  if (rho0 >= rows) return;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x & 63;
+  const int col = lane & 15, grp = lane >> 4;
+  const int i_first = rho0 / a.g;  // request rows of the block
+  const int i_last = min((rho0 + kRowsPerBlock - 1) / a.g, cnt - 1);
+  const int end = min(q.prefix + cnt, a.b.C);
+  const int run = run_slots(end, a.nsplit);
+  const bool direct = run >= end;  // one run: no merge
+  const int kbeg = wk.split * run, kend = min(kbeg + run, row_end(a, q, i_last));
+  if (kbeg >= kend) return;
+
+  // this lane's rows and their Q^T fragments
+  bool row_in[CT];
+  int ri[CT], hq[CT];
+  u32x4 bq[CT][KS];
+#pragma unroll
+  for (int c = 0; c < CT; ++c) {
+    const int rho = rho0 + wave * kRowsPerWave + 16 * c + col;
+    row_in[c] = rho < rows;
+    const int rr = min(rho, rows - 1);
+    ri[c] = rr / a.g;
+    hq[c] = wk.kvh * a.g + rr % a.g;
+    const uint16_t* qrow = a.q + ((size_t)(q.start + ri[c]) * a.Hq + hq[c]) * D + grp * 8;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) bq[c][s] = *(const u32x4*)(qrow + s * 32);
+  }
+  // the rows of the whole wave (uniform)
+  const int w_first = min(rho0 + wave * kRowsPerWave, rows - 1) / a.g;
+  const int w_last = min(rho0 + wave * kRowsPerWave + kRowsPerWave, rows) - 1;
+  const int w_end = row_end(a, q, max(w_last, 0) / a.g);
+  const bool w_live = rho0 + wave * kRowsPerWave < rows;
+
+  // slots below it are admitted by every row of the block (where they have a page)
+  const int all_see = min(kend, q.prefix + (a.mask ? 0 : i_first + 1));
+
+  const int* table = a.b.page_table + (size_t)wk.r * a.b.max_pages;
+  const int pmask = (1 << a.b.page_shift) - 1;
+  // (slots past the run repeat its last one)
+  auto page_of = [&](int c0) __attribute__((always_inline)) {
+    return table[min(c0 + lane, kend - 1) >> a.b.page_shift];
+  };
+  // The chunk's K and V into a buffer; the slots without a page.
+  auto fetch = [&](int c0, int pg, int buf) __attribute__((always_inline)) -> uint64_t {
+    const bool none = (unsigned)pg >= (unsigned)a.b.pages;
+    const uint64_t bad = __ballot(none);
+    const uint32_t pgc = none ? 0u : (uint32_t)pg;
+    const int last = kend - 1 - c0;
+#pragma unroll
+    for (int i = 0; i < IPW; ++i) {
+      const int u = (wave * IPW + i) * 64 + lane;
+      const int row = u / UPR, pos = u % UPR;
+      const uint32_t p = __builtin_amdgcn_ds_bpermute(row * 4, pgc);
+      const int slot = (c0 + min(row, last)) & pmask;
+      const size_t base = (size_t)p * a.b.page_units + (size_t)wk.kvh * a.b.head_units +
+                          (uint32_t)slot * UPR;
+      load_lds16((const uint4*)a.k + base + (pos ^ k_unit<D>(row)),
+                 &sKV[buf][0][(wave * IPW + i) * 512]);
+      load_lds16((const uint4*)a.v + base + (pos ^ v_unit<D>(row)),
+                 &sKV[buf][1][(wave * IPW + i) * 512]);
+    }
+    return bad;
+  };
+  int pg = page_of(kbeg);
+  uint64_t bad_next = fetch(kbeg, pg, 0);
+  pg = page_of(min(kbeg + kChunk, kend - 1));
+
+  if (threadIdx.x == 0) sOdd = 0;
+  if (a.mask) {
+    const uint32_t* mg = a.mask + ((size_t)wk.r * a.N + i_first) * a.NW;
+    for (int i = threadIdx.x; i < (i_last - i_first + 1) * a.NW; i += kThreads) sMask[i] = mg[i];
+  }
+
+  f32x4 o[CT][DT];
+  float m[CT], l[CT];
+#pragma unroll
+  for (int c = 0; c < CT; ++c) {
+    m[c] = kNegInf;
+    l[c] = 0.0f;
+#pragma unroll
+    for (int t = 0; t < DT; ++t) o[c][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  // A rows of a tile pair: tile 0 holds keys 8c + e, tile 1 keys 8c + 4 + e
+  const int krow0 = 8 * (col >> 2) + (col & 3);
+  const int vkey = 8 * grp + (col >> 2);  // the key this lane addresses (of the first four)
+
+  int buf = 0;
+  bool some_bad = false;
+  for (int c0 = kbeg; c0 < kend; c0 += kChunk, buf ^= 1) {
+    wait_loads();
+    lds_barrier();  // the chunk is complete; the other buffer is no longer read
+    const uint64_t bad = bad_next;
+    some_bad |= bad != 0;
+    if (c0 + kChunk < kend) {
+      bad_next = fetch(c0 + kChunk, pg, buf ^ 1);
+      pg = page_of(min(c0 + 2 * kChunk, kend - 1));
+    }
+    uint16_t* sK = sKV[buf][0];
+    uint16_t* sV = sKV[buf][1];
+    // Chunks that some row of the block sees only in part (the same in every
+    // wave): infinite and NaN values, and those of no page, become zeros.
+    if (bad || c0 + kChunk > all_see) {
+      bool odd = false;
+#pragma unroll
+      for (int i = 0; i < IPW; ++i) {
+        const int u = i * kThreads + threadIdx.x;
+        u32x4 w = *(const u32x4*)(sV + u * 8);
+        const bool none = (bad >> (u / UPR)) & 1;
+        bool any = none;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t f = none ? 0u : fine_pair<H>(w[e]);
+          odd |= !none && f != w[e];
+          any |= f != w[e];
+          w[e] = f;
+        }
+        if (any) *(u32x4*)(sV + u * 8) = w;
+      }
+      if (odd) sOdd = 1;
+      lds_barrier();
+    }
+    if (!w_live || c0 >= w_end) continue;  // (causal) no row of this wave sees the chunk
+    // every row of the wave admits every slot
+    const bool full = !bad && c0 + kChunk <= min(kend, q.prefix + (a.mask ? 0 : w_first + 1));
+
+    f32x4 sacc[CT][2][2];
+#pragma unroll
+    for (int c = 0; c < CT; ++c)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) sacc[c][h][0] = sacc[c][h][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < KS; ++k) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const uint16_t* kr = sK + (32 * h + krow0) * D + ((4 * k + grp) ^ k_unit<D>(krow0)) * 8;
+        const u32x4 a0 = *(const u32x4*)kr;
+        const u32x4 a1 = *(const u32x4*)(kr + 4 * D);
+#pragma unroll
+        for (int c = 0; c < CT; ++c) {
+          sacc[c][h][0] = mfma16<H>(a0, bq[c][k], sacc[c][h][0]);
+          sacc[c][h][1] = mfma16<H>(a1, bq[c][k], sacc[c][h][1]);
+        }
+      }
+    }
+    u32x4 bp[CT][2];
+#pragma unroll
+    for (int c = 0; c < CT; ++c) {
+      const uint32_t adm =
+          full ? 0u : admitted(a, q, sMask + (ri[c] - i_first) * a.NW, ri[c], c0, kend, bad, grp);
+      const float alpha = softmax_chunk<H>(sacc[c], adm, full, a.scale_log2, m[c], l[c], bp[c]);
+      if (__any(alpha != 1.0f)) {
+#pragma unroll
+        for (int t = 0; t < DT; ++t) o[c][t] *= alpha;
+      }
+    }
+    auto value = [&](int t, int h) __attribute__((always_inline)) {
+      const uint16_t* vr = sV + (32 * h + vkey) * D +
+                           ((2 * t + ((col >> 1) & 1)) ^ v_unit<D>(vkey)) * 8 + (col & 1) * 4;
+      const u32x2 lo = read_tr(vr), hi = read_tr(vr + 4 * D);
+      return u32x4{lo[0], lo[1], hi[0], hi[1]};
+    };
+#pragma unroll
+    for (int t = 0; t < DT; ++t)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const uint16_t* vr = sV + (32 * h + vkey) * D +
+                             ((2 * t + ((col >> 1) & 1)) ^ v_unit<D>(vkey)) * 8 + (col & 1) * 4;
+        const u32x2 lo = read_tr(vr), hi = read_tr(vr + 4 * D);
+        const u32x4 av = {lo[0], lo[1], hi[0], hi[1]};
+#pragma unroll
+        for (int c = 0; c < CT; ++c) o[c][t] = mfma16<H>(av, bp[c][h], o[c][t]);
+      }
+  }
+  // (every wave is past the loop's last barrier)
+  if (sOdd) {
+    // Infinite and NaN values that were set to zero: they make the outputs of the
+    // rows that do admit them NaN.  (Rare, so slot by slot from memory.)
+    const int first = some_bad ? kbeg : kbeg + max(all_see - kbeg, 0) / kChunk * kChunk;
+#pragma unroll 1
+    for (int s = first; s < kend; ++s) {
+      const int p = table[s >> a.b.page_shift];
+      if ((unsigned)p >= (unsigned)a.b.pages) continue;
+      const uint16_t* vrow = a.v + ((size_t)p * a.b.page_units + (size_t)wk.kvh * a.b.head_units) * 8 +
+                             (size_t)(s & pmask) * D + 4 * grp;
+      bool sees[CT];
+#pragma unroll
+      for (int c = 0; c < CT; ++c) {
+        const int j = s - q.prefix;
+        sees[c] = j < 0 || (a.mask ? (sMask[(ri[c] - i_first) * a.NW + (j >> 5)] >> (j & 31)) & 1
+                                   : j <= ri[c]);
+      }
+#pragma unroll
+      for (int t = 0; t < DT; ++t) {
+        const u32x2 w = *(const u32x2*)(vrow + 16 * t);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const bool odd = odd16<H>(w[e / 2] >> (16 * (e & 1)));
+#pragma unroll
+          for (int c = 0; c < CT; ++c)
+            if (odd && sees[c]) o[c][t][e] = __builtin_nanf("");
+        }
+      }
+    }
+  }
+
+#pragma unroll
+  for (int c = 0; c < CT; ++c) {
+    l[c] += __shfl_xor(l[c], 16, 64);
+    l[c] += __shfl_xor(l[c], 32, 64);
+    if (!row_in[c]) continue;
+    const size_t qidx = (size_t)(q.start + ri[c]) * a.Hq + hq[c];
+    if (direct) {
+      const float inv = l[c] == 0.0f ? 0.0f : 1.0f / l[c];  // (no admitted slot)
+      uint16_t* orow = a.out + qidx * D;
+#pragma unroll
+      for (int t = 0; t < DT; ++t) {
+        const f32x4 v = o[c][t] * inv;
+        u32x2 w;
+        w[0] = pack16<H>(v[0], v[1]);
+        w[1] = pack16<H>(v[2], v[3]);
+        *(u32x2*)(orow + t * 16 + 4 * grp) = w;
+      }
+    } else {
+      const size_t prow = (size_t)wk.split * a.b.T * a.Hq + qidx;
+      float* po = a.part_o + prow * D;
+#pragma unroll
+      for (int t = 0; t < DT; ++t) *(f32x4*)(po + t * 16 + 4 * grp) = o[c][t];
+      if (grp == 0) {
+        a.part_ml[2 * prow] = m[c];
+        a.part_ml[2 * prow + 1] = l[c];
+      }
+    }
+  }
+}
+
+// Merge of the runs: a wave takes 256 / D heads of one row, D / 4 threads each,
+// 4 consecutive elements apiece.  Requests of one run are already written.
+template <int D, bool H>
+__global__ __launch_bounds__(kMergeThreads) void paged_merge_kernel(PagedAttnArgs a) {
+  constexpr int TPR = D / 4, HPW = 64 / TPR;
+  const int per_row = (a.Hq + HPW - 1) / HPW;
+  const int wave =
+      __builtin_amdgcn_readfirstlane(blockIdx.x * (kMergeThreads / 64) + threadIdx.x / 64);
+  const int lane = threadIdx.x & 63;
+  const int t = wave / per_row;
+  if (t >= a.b.T) return;
+  const int r = request_of_row(a.b, t);
+  if (r < 0) return;
+  PagedReq q = paged_req(a.b, r);
+  if (a.mask) q.cnt = min(q.cnt, a.N);
+  const int i = t - q.start, h = wave % per_row * HPW + lane / TPR, d = lane % TPR * 4;
+  if (i >= q.cnt) return;
+  const int end = min(q.prefix + q.cnt, a.b.C), run = run_slots(end, a.nsplit);
+  if (run >= end || h >= a.Hq) return;
+  const int ns = (row_end(a, q, i) + run - 1) / run;
+  const size_t rows = (size_t)a.b.T * a.Hq, qidx = (size_t)t * a.Hq + h;
+  float M = kNegInf, L = 0.0f;
+  f32x4 O = {0.f, 0.f, 0.f, 0.f};
+  for (int s0 = 0; s0 < ns; s0 += kMergeBatch) {
+    float ms[kMergeBatch], ls[kMergeBatch];
+    f32x4 os[kMergeBatch];
+#pragma unroll
+    for (int j = 0; j < kMergeBatch; ++j) {
+      const size_t prow = (size_t)min(s0 + j, ns - 1) * rows + qidx;
+      ms[j] = a.part_ml[2 * prow];
+      ls[j] = a.part_ml[2 * prow + 1];
+      os[j] = *(const f32x4*)(a.part_o + prow * D + d);
+    }
+    float Mn = M;
+#pragma unroll
+    for (int j = 0; j < kMergeBatch; ++j)
+      if (s0 + j < ns) Mn = fmaxf(Mn, ms[j]);
+    // (equal maxima, -inf among them: factor 1; a run that admits nothing holds zeros)
+    const float sc = M == Mn ? 1.0f : exp2_hw((M - Mn) * a.scale_log2);
+    L *= sc;
+    O *= sc;
+#pragma unroll
+    for (int j = 0; j < kMergeBatch; ++j) {
+      if (s0 + j < ns) {
+        const float w = ms[j] == Mn ? 1.0f : exp2_hw((ms[j] - Mn) * a.scale_log2);
+        L += w * ls[j];
+        O += os[j] * w;
+      }
+    }
+    M = Mn;
+  }
+  const float inv = L == 0.0f ? 0.0f : 1.0f / L;
+  u32x2 w;
+  w[0] = pack16<H>(O[0] * inv, O[1] * inv);
+  w[1] = pack16<H>(O[2] * inv, O[3] * inv);
+  *(u32x2*)(a.out + qidx * D + d) = w;
+}
+
+template <int D, bool H>
+hipError_t launch(const PagedAttnArgs& a, const PagedPlan& p, hipStream_t stream) {
+  unsigned mask_bytes = 0;
+  if (a.mask) {  // 128 rows touch at most 127 / g + 2 request rows
+    const int nodes = (kRowsPerBlock - 1) / a.g + 2;
+    mask_bytes = (unsigned)((nodes < a.N ? nodes : a.N) * a.NW * sizeof(uint32_t));
+  }
+  paged_attn_kernel<D, H><<<(unsigned)p.blocks, kThreads, mask_bytes, stream>>>(a);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || a.nsplit == 1) return e;
+  constexpr int HPW = 256 / D;
+  const long long waves = (long long)a.b.T * ((a.Hq + HPW - 1) / HPW);
+  paged_merge_kernel<D, H>
+      <<<(unsigned)((waves + 3) / 4), kMergeThreads, 0, stream>>>(a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+PagedPlan plan_paged_attention(int R, int T, int max_rows, int Hq, int Hkv, int D, int C,
+                               int cus) {
+  PagedPlan p;
+  const int g = Hq / Hkv;
+  const long long qb = ((long long)max_rows * g + kRowsPerBlock - 1) / kRowsPerBlock;
+  p.qblocks = (int)qb;
+  // row blocks that can hold rows: all of a request's, or by the rows there are
+  const long long some = (long long)T * g / kRowsPerBlock + R;
+  const long long base = Hkv * (some < qb * R ? some : qb * R);
+  const int chunks = (C + kChunk - 1) / kChunk;
+  long long ns = base < 2 * cus ? (2 * cus + base - 1) / base : 1;
+  ns = ns < (chunks + 1) / 2 ? ns : (chunks + 1) / 2;
+  ns = ns < kMaxSplits ? ns : kMaxSplits;
+  p.nsplit = (int)(ns < 1 ? 1 : ns);
+  const long long groups = (long long)R * Hkv * p.nsplit;
+  p.blocks = (groups + kXcds - 1) / kXcds * kXcds * qb;
+  p.ws_bytes = p.nsplit > 1 ? (size_t)p.nsplit * T * Hq * (D + 2) * sizeof(float) + 256 : 0;
+  return p;
+}
+
+hipError_t launch_paged_attention(const PagedAttnArgs& a, const PagedPlan& p, int D, bool f16,
+                                  hipStream_t stream) {
+  if (D == 128) return f16 ? launch<128, true>(a, p, stream) : launch<128, false>(a, p, stream);
+  return f16 ? launch<64, true>(a, p, stream) : launch<64, false>(a, p, stream);
+}
+
+}  // namespace pctree

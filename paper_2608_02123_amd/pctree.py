@@ -28,6 +28,12 @@ __all__ = [
     "attention_workspace_bytes",
     "tree_attention",
     "TreeAttention",
+    "PagedBatch",
+    "rope_table",
+    "append_paged",
+    "PagedAttention",
+    "paged_attention",
+    "compact_paged",
     "TreeBuilder",
     "timeline_available",
     "timeline_read",
@@ -36,6 +42,7 @@ __all__ = [
     "debug_set",
     "F32",
     "BF16",
+    "F16",
     "MODE_PARENT",
     "MODE_SHARED",
     "MODE_INDEPENDENT",
@@ -49,7 +56,7 @@ TIMELINE_LIB_PATH = os.path.join(_HERE, "libpctree_timeline.so")
 TIMELINE_WHO, TIMELINE_STAGES, TIMELINE_EVENTS = 5, 65, 8
 
 OK, ERR_INVALID_ARGUMENT, ERR_UNSUPPORTED, ERR_WORKSPACE, ERR_HIP = range(5)
-F32, BF16 = 0, 1
+F32, BF16, F16 = 0, 1, 2
 NOALLOC_SCRATCH_BYTES = 32 << 20  # PCTREE_NOALLOC_SCRATCH_BYTES
 MODE_PARENT, MODE_SHARED, MODE_INDEPENDENT = 0, 1, 2  # pctree_mode
 
@@ -78,6 +85,27 @@ class AttnShape(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in
                 ("requests", "budget", "q_heads", "kv_heads", "head_dim", "capacity")] + \
                [("scale", ctypes.c_float)]
+
+
+class _PagedCache(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("page_stride", ctypes.c_int64)] + \
+               [(n, ctypes.c_int32) for n in
+                ("pages", "page_size", "kv_heads", "head_dim", "dtype")]
+
+
+class _PagedBatch(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in
+                ("row_start", "row_count", "prefix_len", "page_table")] + \
+               [(n, ctypes.c_int32) for n in ("requests", "max_pages", "rows", "max_rows")]
+
+
+class _Append(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("q", "k", "v", "q_out")] + \
+               [(n, ctypes.c_int64) for n in
+                ("q_stride", "k_stride", "v_stride", "q_out_stride")] + \
+               [(n, ctypes.c_void_p) for n in ("q_norm", "k_norm", "rope", "position")] + \
+               [("eps", ctypes.c_float)] + \
+               [(n, ctypes.c_int32) for n in ("q_heads", "rot_dim", "positions", "interleaved")]
 
 
 class _Inputs(ctypes.Structure):
@@ -139,6 +167,17 @@ def lib() -> ctypes.CDLL:
         L.pctree_tree_attention.argtypes = [ctypes.POINTER(AttnShape), vp, vp, vp, vp, vp, vp, vp,
                                             vp, sz, vp]
         L.pctree_tree_attention.restype = ctypes.c_int
+        cache, batch = ctypes.POINTER(_PagedCache), ctypes.POINTER(_PagedBatch)
+        L.pctree_append_paged.argtypes = [cache, batch, ctypes.POINTER(_Append), vp]
+        L.pctree_append_paged.restype = ctypes.c_int
+        L.pctree_paged_attention_workspace_bytes.argtypes = [cache, batch, i32]
+        L.pctree_paged_attention_workspace_bytes.restype = sz
+        L.pctree_paged_attention.argtypes = [cache, batch, vp, i32, ctypes.c_float, vp, i32, vp,
+                                             vp, sz, vp]
+        L.pctree_paged_attention.restype = ctypes.c_int
+        L.pctree_compact_paged.argtypes = [vp, i64, i64, i32, i32, i32, i32, i32, vp, i32, vp, vp,
+                                           vp, i32, i32, i32, vp]
+        L.pctree_compact_paged.restype = ctypes.c_int
         L.pctree_status_string.argtypes = [ctypes.c_int]
         L.pctree_status_string.restype = ctypes.c_char_p
         L.pctree_abi_version.argtypes = []
@@ -517,6 +556,246 @@ def tree_attention(q, k, v, mask, count, prefix_len, scale=None, stream=None):
     Hkv, C = k.shape[1], k.shape[2]
     return TreeAttention(R, N, Hq, Hkv, D, C, scale, device=q.device)(
         q, k, v, mask, count, prefix_len, stream=stream)
+
+
+# ---------------------------------------------------------------------------
+# the verification step over a paged cache
+# ---------------------------------------------------------------------------
+
+_HALVES = {torch.bfloat16: BF16, torch.float16: F16}
+
+
+class _Here:
+    """The calls' device and stream: the tensors' device, and its current stream or
+    the one that is passed (what a call allocates is then that stream's)."""
+
+    def __init__(self, t, stream):
+        self.ctx = None
+        if stream is not None:
+            if stream.device != t.device:
+                raise ValueError(f"the stream is one of {stream.device}, the tensors of {t.device}")
+            self.ctx = torch.cuda.stream(stream)
+        elif t.is_cuda and t.device.index != torch.cuda.current_device():
+            self.ctx = torch.cuda.device(t.device)
+
+    def __enter__(self):
+        if self.ctx is not None:
+            self.ctx.__enter__()
+        return _stream()
+
+    def __exit__(self, *exc):
+        if self.ctx is not None:
+            self.ctx.__exit__(*exc)
+
+
+def _device_tensor(name, t, dtype, shape, device=None):
+    if not isinstance(t, torch.Tensor) or t.dtype != dtype:
+        raise TypeError(f"{name} must be a {dtype} tensor")
+    if not t.is_cuda or (device is not None and t.device != device):
+        raise ValueError(f"{name} must be on the device of the other tensors")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+
+
+class PagedBatch:
+    """Which rows of a call belong to which request, and the requests' pages.
+
+    Row ``row_start[r] + i`` (``i < row_count[r]``) is request ``r``'s i-th new
+    row and sits at slot ``prefix_len[r] + i``, that is slot ``% page_size`` of
+    page ``page_table[r][slot // page_size]`` (an entry that is no page's index
+    stands for no page).  All are int32 device tensors whose contents may change
+    from call to call; ``rows`` is the row count of q, k, v and out, ``max_rows``
+    the most rows any request has (``rows`` if not given).
+    """
+
+    def __init__(self, row_start, row_count, prefix_len, page_table, rows, max_rows=None):
+        if not isinstance(page_table, torch.Tensor) or page_table.dim() != 2:
+            raise ValueError("page_table must be an [R][max_pages] tensor")
+        R, W = page_table.shape
+        for name, t, shp in (("page_table", page_table, (R, W)), ("row_start", row_start, (R,)),
+                             ("row_count", row_count, (R,)), ("prefix_len", prefix_len, (R,))):
+            _device_tensor(name, t, torch.int32, shp, page_table.device)
+        self.requests, self.max_pages, self.rows = R, W, int(rows)
+        self.max_rows = self.rows if max_rows is None else int(max_rows)
+        self.device = page_table.device
+        self._keep = (row_start, row_count, prefix_len, page_table)
+        self._c = _PagedBatch(*(t.data_ptr() for t in self._keep), R, W, self.rows, self.max_rows)
+
+    @property
+    def sizes(self):
+        return self.requests, self.max_pages, self.rows, self.max_rows
+
+
+def _paged_cache(k, v, device):
+    """The C view of one layer's pages [pages][Hkv][page_size][D]; the pages may lie
+    apart (stride 0 is free, the same for both)."""
+    for name, t in (("k_cache", k), ("v_cache", v)):
+        if not isinstance(t, torch.Tensor) or t.dtype not in _HALVES:
+            raise TypeError(f"{name} must be a bfloat16 or float16 tensor")
+        if t.dim() != 4 or not t.is_cuda or t.device != device:
+            raise ValueError(f"{name} must be a [pages][Hkv][page_size][D] tensor on {device}")
+    if k.shape != v.shape or k.dtype != v.dtype or (k.shape[0] > 1 and k.stride(0) != v.stride(0)):
+        raise ValueError("k_cache and v_cache must have one shape, type and page stride")
+    pages, Hkv, P, D = k.shape
+    for t in (k, v):
+        if not t[0].is_contiguous():
+            raise ValueError("a page's [Hkv][page_size][D] must be contiguous")
+    stride = k.stride(0) if pages > 1 else Hkv * P * D
+    return _PagedCache(k.data_ptr(), v.data_ptr(), stride, pages, P, Hkv, D, _HALVES[k.dtype])
+
+
+def _row_tensor(name, t, T, D, dtype, device):
+    """Row stride of a [T][heads][D] tensor whose rows may lie apart."""
+    if not isinstance(t, torch.Tensor) or t.dtype != dtype:
+        raise TypeError(f"{name} must be a {dtype} tensor")
+    if t.dim() != 3 or t.shape[0] != T or t.shape[2] != D or not t.is_cuda or t.device != device:
+        raise ValueError(f"{name} must be a [{T}][heads][{D}] tensor on {device}")
+    if not t[0].is_contiguous():
+        raise ValueError(f"a row of {name} must be contiguous")
+    return t.stride(0) if T > 1 else t.shape[1] * D
+
+
+def rope_table(positions, rot_dim, theta=10000.0, device="cuda"):
+    """The table that :func:`append_paged` rotates by: ``[positions][rot_dim]`` float32,
+    the cosines of a position's ``rot_dim / 2`` angles ``p * theta^(-2 i / rot_dim)``,
+    then their sines.  The angles are float64: far positions have many turns."""
+    if rot_dim < 16 or rot_dim % 16:
+        raise ValueError("rot_dim must be a multiple of 16")
+    inv = float(theta) ** (-torch.arange(0, rot_dim, 2, dtype=torch.float64, device=device)
+                           / rot_dim)
+    a = torch.arange(positions, dtype=torch.float64, device=device)[:, None] * inv
+    return torch.cat([a.cos(), a.sin()], 1).float()
+
+
+def append_paged(batch, k_cache, v_cache, k, v, q=None, *, q_norm=None, k_norm=None, eps=1e-6,
+                 rope=None, interleaved=False, position=None, q_out=None, stream=None):
+    """New rows into their pages: ``k``, ``v [T][Hkv][D]`` and, if given, ``q [T][Hq][D]``
+    (views of a fused projection will do) are normed per head (``q_norm``, ``k_norm
+    [D]``: root mean square), rotated by ``rope`` (:func:`rope_table`) at ``position
+    [T]`` (a row's slot if not given); keys and values go to the rows' slots.
+    Returns the normed and rotated q in ``q_out`` (a new tensor if not given; rows
+    of no request are not written)."""
+    dev, T = batch.device, batch.rows
+    c = _paged_cache(k_cache, v_cache, dev)
+    dt, D = k_cache.dtype, c.head_dim
+    ks, vs = _row_tensor("k", k, T, D, dt, dev), _row_tensor("v", v, T, D, dt, dev)
+    if k.shape[1] != c.kv_heads or v.shape[1] != c.kv_heads:
+        raise ValueError(f"k and v must have the cache's {c.kv_heads} heads")
+    for name, w in (("q_norm", q_norm), ("k_norm", k_norm)):
+        if w is not None:
+            _device_tensor(name, w, dt, (D,), dev)
+    if position is not None:
+        _device_tensor("position", position, torch.int32, (T,), dev)
+    rot = npos = 0
+    if rope is not None:
+        if not isinstance(rope, torch.Tensor) or rope.dim() != 2:
+            raise ValueError("rope must be a [positions][rot_dim] tensor")
+        npos, rot = rope.shape
+        _device_tensor("rope", rope, torch.float32, (npos, rot), dev)
+    if q is None and (q_out is not None or q_norm is not None):
+        raise ValueError("q_out and q_norm go with q")
+    with _Here(k_cache, stream) as st:
+        qs = os_ = Hq = 0
+        if q is not None:
+            qs, Hq = _row_tensor("q", q, T, D, dt, dev), q.shape[1]
+            if q_out is None:
+                q_out = torch.empty((T, Hq, D), dtype=dt, device=dev)
+            os_ = _row_tensor("q_out", q_out, T, D, dt, dev)
+            if q_out.shape != q.shape:
+                raise ValueError("q_out must have q's shape")
+        a = _Append(_ptr(q), _ptr(k), _ptr(v), _ptr(q_out), qs, ks, vs, os_, _ptr(q_norm),
+                    _ptr(k_norm), _ptr(rope), _ptr(position), eps, Hq, rot, npos,
+                    1 if interleaved else 0)
+        _check(lib().pctree_append_paged(ctypes.byref(c), ctypes.byref(batch._c), ctypes.byref(a),
+                                         st), "pctree_append_paged")
+    return q_out
+
+
+class PagedAttention:
+    """Attention of a batch's new rows over paged caches, with its workspace, for
+    repeated calls of one size (calls that may overlap need an object each)."""
+
+    def __init__(self, batch, q_heads, kv_heads, head_dim, page_size, scale=None):
+        self.sizes = batch.sizes
+        self.q_heads, self.kv_heads, self.head_dim = q_heads, kv_heads, head_dim
+        self.page_size = page_size
+        self.scale = float(scale) if scale is not None else head_dim ** -0.5
+        c = _PagedCache(None, None, kv_heads * page_size * head_dim, 1, page_size, kv_heads,
+                        head_dim, BF16)
+        self.ws_bytes = int(lib().pctree_paged_attention_workspace_bytes(
+            ctypes.byref(c), ctypes.byref(batch._c), q_heads))
+        self.workspace = torch.empty(max(self.ws_bytes, 1), dtype=torch.uint8,
+                                     device=batch.device)
+
+    def __call__(self, q, k_cache, v_cache, batch, mask=None, out=None, stream=None):
+        """``q [T][Hq][D]`` over ``k_cache, v_cache [pages][Hkv][page_size][D]``; causal, or
+        with ``mask`` (:func:`build_mask`) the tree's.  Returns ``out [T][Hq][D]``
+        (rows of no request are not written)."""
+        dev = self.workspace.device
+        if batch.sizes != self.sizes or batch.device != dev:
+            raise ValueError("the batch is not of this object's sizes")
+        c = _paged_cache(k_cache, v_cache, dev)
+        if (c.kv_heads, c.head_dim, c.page_size) != (self.kv_heads, self.head_dim,
+                                                     self.page_size):
+            raise ValueError("the pages are not of this object's sizes")
+        shp = (batch.rows, self.q_heads, self.head_dim)
+        _device_tensor("q", q, k_cache.dtype, shp, dev)
+        budget = 0
+        if mask is not None:
+            if mask.dtype != torch.int32 and mask.dtype != torch.uint32:
+                raise TypeError("mask must be the [R][N][(N+31)/32] words of build_mask")
+            budget = mask.shape[1] if mask.dim() == 3 else 0
+            _device_tensor("mask", mask, mask.dtype,
+                           (batch.requests, budget, (budget + 31) // 32), dev)
+        if out is not None:
+            _device_tensor("out", out, k_cache.dtype, shp, dev)
+        with _Here(q, stream) as st:
+            if out is None:
+                out = torch.empty(shp, dtype=q.dtype, device=dev)
+            _check(lib().pctree_paged_attention(
+                ctypes.byref(c), ctypes.byref(batch._c), _ptr(q), self.q_heads, self.scale,
+                _ptr(mask), budget, _ptr(out), _ptr(self.workspace), self.ws_bytes, st),
+                "pctree_paged_attention")
+        return out
+
+
+def paged_attention(q, k_cache, v_cache, batch, mask=None, scale=None, out=None, stream=None):
+    """One call of :class:`PagedAttention`."""
+    with _Here(k_cache, stream):
+        layer = PagedAttention(batch, q.shape[1], k_cache.shape[1], k_cache.shape[3],
+                               k_cache.shape[2], scale)
+        return layer(q, k_cache, v_cache, batch, mask=mask, out=out)
+
+
+def compact_paged(pool, page_table, prefix_len, accept_node, accept_len, budget, stream=None):
+    """Move each request's accepted slots right after its prefix, in place.
+
+    ``pool [groups][pages][heads][page_size][...]`` (e.g. every layer's K and V):
+    the dimensions past ``page_size`` form a slot of a head, a multiple of 16 bytes;
+    groups and pages may lie apart."""
+    if not isinstance(pool, torch.Tensor) or not pool.is_cuda or pool.dim() < 5 or \
+            not pool[0, 0].is_contiguous():
+        raise ValueError("pool must be a [groups][pages][heads][page_size][...] device tensor "
+                         "with contiguous pages")
+    G, pages, heads, P = pool.shape[:4]
+    R, W = accept_node.shape
+    dev = pool.device
+    _device_tensor("page_table", page_table, torch.int32, (R, page_table.shape[-1]), dev)
+    _device_tensor("accept_node", accept_node, torch.int32, (R, W), dev)
+    _device_tensor("prefix_len", prefix_len, torch.int32, (R,), dev)
+    _device_tensor("accept_len", accept_len, torch.int32, (R,), dev)
+    es = pool.element_size()
+    slot = math.prod(pool.shape[4:]) * es
+    page_stride = pool.stride(1) * es if pages > 1 else heads * P * slot
+    group_stride = pool.stride(0) * es if G > 1 else 0
+    with _Here(pool, stream) as st:
+        _check(lib().pctree_compact_paged(
+            _ptr(pool), group_stride, page_stride, G, pages, heads, P, slot, _ptr(page_table),
+            page_table.shape[1], _ptr(prefix_len), _ptr(accept_node), _ptr(accept_len), R, budget,
+            W - 1, st), "pctree_compact_paged")
+    return pool
 
 
 def device_inputs(inp: dict, device="cuda") -> dict:
