@@ -408,6 +408,43 @@ pctree_status pctree_paged_attention(const pctree_paged_cache* cache,
                                      int32_t budget, void* out, void* workspace,
                                      size_t workspace_bytes, void* stream);
 
+/* Sampling: a token for every row of logits, from given random numbers.  Row t
+ * of logits starts at element t * row_stride (>= vocab).  temperature, top_k,
+ * top_p and min_p are [rows] device arrays or NULL (1, off, off, off).
+ *
+ * With weights w_i = e^((l_i - max l) / temperature), of the row's tokens are kept,
+ * in turn: those with w_i >= min_p (off at min_p <= 0; the largest always stay);
+ * the top_k with the largest logits (off at top_k <= 0); the fewest with the
+ * largest logits whose weights sum to at least top_p times the sum of those left
+ * (off at top_p >= 1; at least one stays).  Equal logits rank by token id.  The
+ * token is the first kept one, by id, at which the running sum of kept weights
+ * exceeds uniform * (their total): uniform in [0, 1), values outside are clamped
+ * (1 and more: the last kept token of positive weight).  logprob (may be NULL) is
+ * the log of the token's share of the kept weights.
+ *
+ * A temperature of 0 (or below, or NaN) takes the first largest logit, logprob 0.
+ * A logit of -inf (a masked token) or NaN is never taken; a row of nothing else
+ * gives token -1, logprob -inf; +inf logits share the row among themselves.
+ * Weights below e^-700 count as 0; a NaN uniform as 0, a NaN top_p or min_p as
+ * off.  Weights and their sums are float64: the same row gives the same token
+ * wherever it lies and whatever else is in the call.
+ *
+ * The sampled tokens of a tree's nodes are the target_next of
+ * pctree_accept_greedy: following the children that match them is then sampling
+ * from the target (Sec. 4.2's lossless verification without greedy decoding).
+ *
+ * dtype: PCTREE_F32, PCTREE_BF16 or PCTREE_F16; logits aligned to one element.
+ * Errors: INVALID_ARGUMENT (null or misaligned pointer, size < 1, row_stride <
+ * vocab, bad dtype), UNSUPPORTED (vocab > PCTREE_MAX_VOCAB, more than 2^31 - 1
+ * blocks of 512 logits in all), WORKSPACE. */
+size_t pctree_sample_workspace_bytes(int32_t rows, int32_t vocab);
+
+pctree_status pctree_sample(const void* logits, int32_t dtype, int32_t rows, int32_t vocab,
+                            int64_t row_stride, const float* uniform, const float* temperature,
+                            const int32_t* top_k, const float* top_p, const float* min_p,
+                            int32_t* token, float* logprob, void* workspace,
+                            size_t workspace_bytes, void* stream);
+
 /* Compaction in pages: pool holds, per group (e.g. one layer's K or V), `pages`
  * pages of [heads][page_size][slot_bytes]; group g's page p starts at byte
  * g * group_stride + p * page_stride.  Tree node i of request r sits at slot

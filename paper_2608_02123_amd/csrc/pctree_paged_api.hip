@@ -3,6 +3,7 @@
 #include "pctree.h"
 
 #include "pctree_paged.h"
+#include "pctree_sample.h"
 
 namespace pctree {
 namespace {
@@ -77,6 +78,14 @@ pctree_status check_attention(const pctree_paged_cache* c, const pctree_paged_ba
                                c->head_dim, b->max_pages * c->page_size, kPlanCUs);
   if (plan->blocks > INT32_MAX) return PCTREE_ERR_UNSUPPORTED;
   return PCTREE_OK;
+}
+
+pctree_status check_sample(int32_t rows, int32_t vocab) {
+  if (rows < 1 || vocab < 1) return PCTREE_ERR_INVALID_ARGUMENT;
+  if (vocab > PCTREE_MAX_VOCAB) return PCTREE_ERR_UNSUPPORTED;
+  SampleArgs a;
+  plan_sample(vocab, &a.ng, &a.nb, &a.gshift);
+  return (int64_t)rows * a.nb > INT32_MAX ? PCTREE_ERR_UNSUPPORTED : PCTREE_OK;
 }
 
 }  // namespace
@@ -192,6 +201,48 @@ pctree_status pctree_paged_attention(const pctree_paged_cache* cache,
     (void)hipGetLastError();
     const hipError_t e = launch_paged_attention(a, plan, cache->head_dim,
                                                 cache->dtype == PCTREE_F16, (hipStream_t)stream);
+    return e == hipSuccess ? PCTREE_OK : PCTREE_ERR_HIP;
+  } catch (...) {
+    return PCTREE_ERR_HIP;
+  }
+}
+
+size_t pctree_sample_workspace_bytes(int32_t rows, int32_t vocab) {
+  return check_sample(rows, vocab) == PCTREE_OK ? sample_bytes(rows, vocab) : 0;
+}
+
+pctree_status pctree_sample(const void* logits, int32_t dtype, int32_t rows, int32_t vocab,
+                            int64_t row_stride, const float* uniform, const float* temperature,
+                            const int32_t* top_k, const float* top_p, const float* min_p,
+                            int32_t* token, float* logprob, void* workspace,
+                            size_t workspace_bytes, void* stream) {
+  try {
+    const pctree_status st = check_sample(rows, vocab);
+    if (st != PCTREE_OK) return st;
+    if (dtype != PCTREE_F32 && dtype != PCTREE_BF16 && dtype != PCTREE_F16)
+      return PCTREE_ERR_INVALID_ARGUMENT;
+    if (!logits || !uniform || !token || row_stride < vocab ||
+        row_stride > INT64_MAX / 4 / rows || !aligned(logits, dtype == PCTREE_F32 ? 4 : 2) ||
+        !aligned(uniform, 4) || !aligned(temperature, 4) || !aligned(top_k, 4) ||
+        !aligned(top_p, 4) || !aligned(min_p, 4) || !aligned(token, 4) || !aligned(logprob, 4))
+      return PCTREE_ERR_INVALID_ARGUMENT;
+    if (!workspace || !aligned(workspace, 256) || workspace_bytes < sample_bytes(rows, vocab))
+      return PCTREE_ERR_WORKSPACE;
+    SampleArgs a;
+    a.logits = logits;
+    a.uniform = uniform;
+    a.temperature = temperature;
+    a.top_k = top_k;
+    a.top_p = top_p;
+    a.min_p = min_p;
+    a.token = token;
+    a.logprob = logprob;
+    a.row_stride = row_stride;
+    a.T = rows;
+    a.V = vocab;
+    place_sample(&a, workspace);
+    (void)hipGetLastError();
+    const hipError_t e = launch_sample(a, dtype, (hipStream_t)stream);
     return e == hipSuccess ? PCTREE_OK : PCTREE_ERR_HIP;
   } catch (...) {
     return PCTREE_ERR_HIP;

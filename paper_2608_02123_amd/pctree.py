@@ -34,6 +34,8 @@ __all__ = [
     "PagedAttention",
     "paged_attention",
     "compact_paged",
+    "Sampler",
+    "sample",
     "TreeBuilder",
     "timeline_available",
     "timeline_read",
@@ -175,6 +177,10 @@ def lib() -> ctypes.CDLL:
         L.pctree_paged_attention.argtypes = [cache, batch, vp, i32, ctypes.c_float, vp, i32, vp,
                                              vp, sz, vp]
         L.pctree_paged_attention.restype = ctypes.c_int
+        L.pctree_sample_workspace_bytes.argtypes = [i32, i32]
+        L.pctree_sample_workspace_bytes.restype = sz
+        L.pctree_sample.argtypes = [vp, i32, i32, i32, i64] + [vp] * 8 + [sz, vp]
+        L.pctree_sample.restype = ctypes.c_int
         L.pctree_compact_paged.argtypes = [vp, i64, i64, i32, i32, i32, i32, i32, vp, i32, vp, vp,
                                            vp, i32, i32, i32, vp]
         L.pctree_compact_paged.restype = ctypes.c_int
@@ -796,6 +802,66 @@ def compact_paged(pool, page_table, prefix_len, accept_node, accept_len, budget,
             page_table.shape[1], _ptr(prefix_len), _ptr(accept_node), _ptr(accept_len), R, budget,
             W - 1, st), "pctree_compact_paged")
     return pool
+
+
+_LOGITS = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
+
+
+class Sampler:
+    """Sampling of up to ``rows`` rows over ``vocab`` tokens, with its workspace, for
+    repeated calls (calls that may overlap need an object each)."""
+
+    def __init__(self, rows, vocab, device="cuda"):
+        self.rows, self.vocab = rows, vocab
+        nb = int(lib().pctree_sample_workspace_bytes(rows, vocab))
+        if nb == 0:
+            _check(lib().pctree_sample(None, F32, rows, vocab, vocab, *([None] * 8), 0, None),
+                   "sizes")
+        self.workspace = torch.empty(nb, dtype=torch.uint8, device=device)
+
+    def __call__(self, logits, uniform, *, temperature=None, top_k=None, top_p=None, min_p=None,
+                 token=None, logprob=None, stream=None):
+        """A token per row of ``logits [T][V]`` (float32, bfloat16 or float16; rows may lie
+        apart) from ``uniform [T]`` in [0, 1).  ``temperature``, ``top_p``, ``min_p``
+        (float32) and ``top_k`` (int32) are ``[T]`` or None; see include/pctree.h.
+        Returns ``(token [T] int32, logprob [T] float32)``."""
+        dev = self.workspace.device
+        if not isinstance(logits, torch.Tensor) or logits.dtype not in _LOGITS:
+            raise TypeError("logits must be a float32, bfloat16 or float16 tensor")
+        if logits.dim() != 2 or logits.device != dev or logits.shape[1] != self.vocab or \
+                not 1 <= logits.shape[0] <= self.rows:
+            raise ValueError(f"logits must be a [T][{self.vocab}] tensor on {dev}, T at most "
+                             f"{self.rows}")
+        T, V = logits.shape
+        if (V > 1 and logits.stride(1) != 1) or (T > 1 and logits.stride(0) < V):
+            raise ValueError("a row of logits must be contiguous, rows must not overlap")
+        for name, t, dt in (("uniform", uniform, torch.float32),
+                            ("temperature", temperature, torch.float32),
+                            ("top_k", top_k, torch.int32), ("top_p", top_p, torch.float32),
+                            ("min_p", min_p, torch.float32), ("token", token, torch.int32),
+                            ("logprob", logprob, torch.float32)):
+            if t is not None or name == "uniform":
+                _device_tensor(name, t, dt, (T,), dev)
+        with _Here(logits, stream) as st:
+            if token is None:
+                token = torch.empty(T, dtype=torch.int32, device=dev)
+            if logprob is None:
+                logprob = torch.empty(T, dtype=torch.float32, device=dev)
+            _check(lib().pctree_sample(
+                _ptr(logits), _LOGITS[logits.dtype], T, V, logits.stride(0) if T > 1 else V,
+                _ptr(uniform), _ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p),
+                _ptr(token), _ptr(logprob), _ptr(self.workspace), self.workspace.numel(), st),
+                "pctree_sample")
+        return token, logprob
+
+
+def sample(logits, uniform, *, temperature=None, top_k=None, top_p=None, min_p=None, stream=None):
+    """One call of :class:`Sampler`."""
+    if not isinstance(logits, torch.Tensor) or logits.dim() != 2 or not logits.is_cuda:
+        raise ValueError("logits must be a [T][V] device tensor")
+    with _Here(logits, stream):
+        return Sampler(*logits.shape, device=logits.device)(
+            logits, uniform, temperature=temperature, top_k=top_k, top_p=top_p, min_p=min_p)
 
 
 def device_inputs(inp: dict, device="cuda") -> dict:
