@@ -231,10 +231,12 @@ pctree_status pctree_sample(const void* logits, int32_t dtype, int32_t rows, int
     SampleArgs a;
     a.logits = logits;
     a.uniform = uniform;
-    a.temperature = temperature;
-    a.top_k = top_k;
-    a.top_p = top_p;
-    a.min_p = min_p;
+    a.has = (temperature ? kHasTemperature : 0) | (top_k ? kHasTopK : 0) |
+            (top_p ? kHasTopP : 0) | (min_p ? kHasMinP : 0);
+    a.temperature = temperature ? temperature : uniform;
+    a.top_k = top_k ? top_k : (const int32_t*)uniform;
+    a.top_p = top_p ? top_p : uniform;
+    a.min_p = min_p ? min_p : uniform;
     a.token = token;
     a.logprob = logprob;
     a.row_stride = row_stride;

@@ -13,15 +13,22 @@
 // rate of float32; the histograms' sums are whole numbers, so that the order of
 // their atomics does not matter.
 //
-// Two launches.  scan_kernel reads the logits once: maxima of groups of 64
-// logits, and for the rows that need all of it (no top_k, no min_p) the sum of
-// weights of each block of 512.  pick_kernel, one workgroup a row, starts from
-// those.  With a top_k of at most the number of groups, the k-th largest group
-// maximum is a lower bound of the k-th largest logit, so only groups that reach
-// it are read again, and what reaches it, hardly more than k logits, is sorted in
-// LDS; min_p gives such a bound too, and a top_p alone first tries the logits
-// from the 256-th largest group maximum up.  Rows that this does not settle are
-// cut by histograms over the whole row.
+// scan_kernel reads the logits once: maxima of groups of 8 to 512 logits (at most
+// 2560 of a row), and for the rows that need all of it (no top_k, no min_p) the sum
+// of weights of each block of 512.  pick_kernel, one workgroup a row, starts from
+// those.  The k-th largest of maxima over disjoint parts of the row is a lower bound
+// of the k-th largest logit, so only groups that reach it are read again, and what
+// reaches it, hardly more than k logits, is sorted in LDS; min_p gives such a bound
+// too, and a top_p alone first tries the logits from the 256-th largest maximum up.
+// A row without filters needs only the blocks' sums and the one block that the draw
+// falls into.
+//
+// Open rows, where top_p or min_p keeps more than that, are left to three more launches
+// over all compute units: hist_kernel sums the weights in bins of 1/64 in log
+// weight, mark_kernel finds the bin in which top_p is reached, sums each block's
+// weights above it and lists the bin's own logits, and finish_kernel cuts that list
+// and draws.  One workgroup could do it alone (whole_row; it does for calls of few
+// rows, and where the list does not do), which takes several times as long.
 #include "pctree.h"
 
 #include <hip/hip_runtime.h>
@@ -41,7 +48,11 @@ constexpr int kScanThreads = 256;
 constexpr int kPickThreads = 512;
 constexpr int kPickWaves = kPickThreads / 64;
 constexpr int kList = 2048;           // logits sorted in LDS
-constexpr int kBins = 2048;
+constexpr int kParts = 512;           // parts of a row whose maxima bound its k-th largest logit,
+constexpr int kManyParts = 2048;      // ... and where k is more than a quarter of that
+constexpr int kMaxBound = 1024;       // the largest k that is bounded so
+constexpr int kTry = 256;             // (top_p alone) the rank of the bound that is tried first
+constexpr int kBins = 2048;           // of 1/64 in log weight
 constexpr double kLowest = -700.0;    // weights below e^-700 are 0
 constexpr double kLog2e = 1.4426950408889634074;
 
@@ -81,6 +92,13 @@ __device__ __forceinline__ float of_ord(uint32_t o) {
   return __uint_as_float(o & 0x80000000u ? o & 0x7fffffffu : ~o);
 }
 
+// A logit and its index as one number: larger logits first, then lower indices.
+__device__ __forceinline__ uint64_t key_of(float v, int i) {
+  return (uint64_t)ord_of(v) << 32 | (uint32_t)~i;
+}
+__device__ __forceinline__ float logit_of(uint64_t key) { return of_ord((uint32_t)(key >> 32)); }
+__device__ __forceinline__ int index_of(uint64_t key) { return (int)~(uint32_t)key; }
+
 // A row at any alignment: `base` is its start rounded down to 16 bytes, and logit
 // i is element lo + i from there, i < V.  Units of 8 elements from base on are a
 // lane's share; NaN counts as -inf, and so does what lies outside the row.
@@ -98,40 +116,68 @@ __device__ __forceinline__ Row row_of(const SampleArgs& a, int t) {
   r.hi = r.lo + a.V;
   return r;
 }
+// (a unit's bytes, as loaded)
 template <int DT>
-__device__ __forceinline__ void load_unit(const Row& r, int u, float (&v)[kUnit]) {
-  const int j0 = u * kUnit;
-  if (j0 >= r.lo && j0 + kUnit <= r.hi) {
+struct Raw {
+  u32x4 x[DT == PCTREE_F32 ? 2 : 1];
+};
+template <int DT>
+__device__ __forceinline__ Raw<DT> load_raw(const Row& r, int u) {
+  Raw<DT> w;
+  constexpr int N = DT == PCTREE_F32 ? 2 : 1;
+#pragma unroll
+  for (int i = 0; i < N; ++i) w.x[i] = ((const u32x4*)r.base)[(size_t)u * N + i];
+  return w;
+}
+template <int DT>
+__device__ __forceinline__ void unpack(const Raw<DT>& w, float (&v)[kUnit]) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
     if constexpr (DT == PCTREE_F32) {
-      const f32x4* p = (const f32x4*)(r.base + (size_t)j0 * 4);
-      const f32x4 x = p[0], y = p[1];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        v[e] = x[e];
-        v[4 + e] = y[e];
-      }
+      v[e] = __uint_as_float(w.x[0][e]);
+      v[4 + e] = __uint_as_float(w.x[1][e]);
     } else {
-      const u32x4 x = *(const u32x4*)(r.base + (size_t)j0 * 2);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        v[2 * e] = lo16<DT == PCTREE_F16>(x[e]);
-        v[2 * e + 1] = hi16<DT == PCTREE_F16>(x[e]);
-      }
-    }
-  } else {
-#pragma unroll
-    for (int e = 0; e < kUnit; ++e) {
-      v[e] = kNegInf;
-      if (j0 + e >= r.lo && j0 + e < r.hi) {
-        if constexpr (DT == PCTREE_F32)
-          v[e] = ((const float*)r.base)[j0 + e];
-        else
-          v[e] = lo16<DT == PCTREE_F16>(((const uint16_t*)r.base)[j0 + e]);
-      }
+      v[2 * e] = lo16<DT == PCTREE_F16>(w.x[0][e]);
+      v[2 * e + 1] = hi16<DT == PCTREE_F16>(w.x[0][e]);
     }
   }
 #pragma unroll
   for (int e = 0; e < kUnit; ++e) v[e] = v[e] == v[e] ? v[e] : kNegInf;
+}
+template <int DT>
+__device__ __forceinline__ void load_unit(const Row& r, int u, float (&v)[kUnit]) {
+  const int j0 = u * kUnit;
+  if (j0 >= r.lo && j0 + kUnit <= r.hi) {
+    unpack<DT>(load_raw<DT>(r, u), v);
+    return;
+  }
+#pragma unroll
+  for (int e = 0; e < kUnit; ++e) {
+    v[e] = kNegInf;
+    if (j0 + e >= r.lo && j0 + e < r.hi) {
+      if constexpr (DT == PCTREE_F32)
+        v[e] = ((const float*)r.base)[j0 + e];
+      else
+        v[e] = lo16<DT == PCTREE_F16>(((const uint16_t*)r.base)[j0 + e]);
+    }
+    v[e] = v[e] == v[e] ? v[e] : kNegInf;
+  }
+}
+// The units u0 + 64 i + lane, i < N, of a wave: all loads before the first use where
+// the wave is inside the row.
+template <int DT, int N>
+__device__ __forceinline__ void load_units(const Row& r, int u0, float (&v)[N][kUnit]) {
+  const int lane = threadIdx.x & 63;
+  if (u0 * kUnit >= r.lo && (u0 + 64 * N) * kUnit <= r.hi) {
+    Raw<DT> w[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) w[i] = load_raw<DT>(r, u0 + 64 * i + lane);
+#pragma unroll
+    for (int i = 0; i < N; ++i) unpack<DT>(w[i], v[i]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i) load_unit<DT>(r, u0 + 64 * i + lane, v[i]);
+  }
 }
 
 // A row's parameters.
@@ -140,34 +186,58 @@ struct Params {
   int k;        // 0: off
   bool greedy;  // a temperature of 0 (or below, or NaN): the largest logit
 };
+// (Absent arrays point at `uniform`, so that all loads are issued together.)
 __device__ __forceinline__ Params params_of(const SampleArgs& a, int t) {
+  const float T = a.temperature[t], p = a.top_p[t], m = a.min_p[t], u = a.uniform[t];
+  const int k = a.top_k[t];
   Params q;
-  const float T = a.temperature ? a.temperature[t] : 1.0f;
-  q.greedy = !(T > 0.0f);
-  q.inv_t = q.greedy ? 1.0 : 1.0 / (double)T;
-  const int k = a.top_k ? a.top_k[t] : 0;
-  q.k = k > 0 && k < a.V ? k : 0;
-  const float p = a.top_p ? a.top_p[t] : 1.0f;
-  q.p = p < 1.0f ? (double)p : 1.0;  // (NaN: off)
-  const float m = a.min_p ? a.min_p[t] : 0.0f;
-  q.min_p = m > 0.0f ? (double)fminf(m, 1.0f) : 0.0;
-  const float u = a.uniform[t];
+  q.greedy = (a.has & kHasTemperature) && !(T > 0.0f);
+  q.inv_t = q.greedy || !(a.has & kHasTemperature) ? 1.0 : 1.0 / (double)T;
+  q.k = (a.has & kHasTopK) && k > 0 && k < a.V ? k : 0;
+  q.p = (a.has & kHasTopP) && p < 1.0f ? (double)p : 1.0;  // (NaN: off)
+  q.min_p = (a.has & kHasMinP) && m > 0.0f ? (double)fminf(m, 1.0f) : 0.0;
   q.u = u > 0.0f ? (double)u : 0.0;
   return q;
 }
 // Whether the row is settled from its largest logits, without the sum of all.
 __device__ __forceinline__ bool bounded(const SampleArgs& a, const Params& q) {
-  return q.greedy || q.min_p > 0.0 || (q.k > 0 && q.k <= a.ng);
+  return q.greedy || q.min_p > 0.0 || (q.k > 0 && q.k <= min(a.ng, kMaxBound));
+}
+
+// Sums over the lanes up to each one, and over the wave.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int dpp_add(int x) {
+  return x + __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xf, false);
+}
+__device__ __forceinline__ int wave_upto(int x) {  // (the lane's own among it)
+  x = dpp_add<0x111, 0xf>(x);  // row_shr:1, 2, 4, 8
+  x = dpp_add<0x112, 0xf>(x);
+  x = dpp_add<0x114, 0xf>(x);
+  x = dpp_add<0x118, 0xf>(x);
+  x = dpp_add<0x142, 0xa>(x);  // row_bcast:15 into rows 1 and 3
+  x = dpp_add<0x143, 0xc>(x);  // row_bcast:31 into rows 2 and 3
+  return x;
+}
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t dpp_most(uint32_t x) {
+  return max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, ROWS, 0xf, false));
+}
+__device__ __forceinline__ uint32_t wave_most(uint32_t x) {
+  x = dpp_most<0x111, 0xf>(x);
+  x = dpp_most<0x112, 0xf>(x);
+  x = dpp_most<0x114, 0xf>(x);
+  x = dpp_most<0x118, 0xf>(x);
+  x = dpp_most<0x142, 0xa>(x);
+  x = dpp_most<0x143, 0xc>(x);
+  return (uint32_t)__builtin_amdgcn_readlane((int)x, 63);
+}
+__device__ __forceinline__ int wave_count(int x) {
+  return __builtin_amdgcn_readlane(wave_upto(x), 63);
 }
 
 __device__ __forceinline__ double wave_sum(double v) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
-  return v;
-}
-__device__ __forceinline__ float wave_max(float v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
   return v;
 }
 
@@ -179,9 +249,8 @@ __global__ __launch_bounds__(kScanThreads) void scan_kernel(SampleArgs a, int se
   if (b0 >= a.nb) return;
   const Row row = row_of<DT>(a, t);
   float v[BPW][kUnit], mx[BPW];
-#pragma unroll
-  for (int i = 0; i < BPW; ++i) load_unit<DT>(row, (b0 + i) * 64 + lane, v[i]);
-  const int lanes = 8 << a.gshift;  // of a group
+  load_units<DT, BPW>(row, b0 * 64, v);
+  const int lanes = 1 << a.gshift;  // of a group
   float all = kNegInf;
 #pragma unroll
   for (int i = 0; i < BPW; ++i) {
@@ -195,7 +264,7 @@ __global__ __launch_bounds__(kScanThreads) void scan_kernel(SampleArgs a, int se
   }
   const Params q = params_of(a, t);
   if (bounded(a, q)) return;
-  const float ref = wave_max(all);
+  const float ref = of_ord(wave_most(ord_of(all)));
 #pragma unroll
   for (int i = 0; i < BPW; ++i) {
     double s = 0.0;
@@ -215,24 +284,24 @@ __global__ __launch_bounds__(kScanThreads) void scan_kernel(SampleArgs a, int se
 // ---------------------------------------------------------------------------
 
 struct PickShared {
-  float gmax[kMaxGroups + 3];
+  float gmax[6 * kPickThreads];  // (of which kMaxGroups are used)
   union {
     struct {
-      uint64_t list[kList];
-      double w[kList];
+      union {
+        uint64_t list[kList];
+        int ties[kMaxBlocks + 1];  // per block
+      };
+      double w[kMaxBlocks + 1];  // of the list; blocks' sums
     } l;
     struct {
       unsigned long long mass[kBins];
       uint32_t count[kBins];
     } h;
-    struct {
-      double mass[kMaxBlocks + 1];
-      int ties[kMaxBlocks + 1];
-    } b;
   };
+  uint16_t group[kMaxGroups + 3];
   double part[kPickWaves];
   int parti[kPickWaves];
-  int n, found, extra;
+  int n, groups, found, extra;
   uint32_t lo, hi;
 };
 
@@ -291,48 +360,99 @@ __device__ __forceinline__ int block_before(int v, PickShared& sh) {
   return base;
 }
 
-// The j-th largest group maximum (j >= 1; all of them: -inf), as a float whose
-// low 12 bits may be rounded down.
-__device__ float group_bound(const SampleArgs& a, int j, PickShared& sh) {
-  uint32_t lo = 0;  // at least j maxima are >= lo
-  for (int bit = 31; bit >= 12; --bit) {
+// A lower bound of the row's j-th largest logit, j <= min(groups, kMaxBound): the j-th
+// largest of the maxima of parts of the row, its order's low 12 bits rounded down.
+// With P parts and logits in any order about P log(P / (P - j)) logits reach it: 52 of
+// 512 parts for j = 50, 450 of 2048 for j = 400 (777 with 512).  Each wave searches by
+// itself, P / 64 maxima to a lane.
+template <int P>
+__device__ __forceinline__ float rank_bound(const SampleArgs& a, int j, const PickShared& sh) {
+  const int lane = threadIdx.x & 63;
+  uint32_t o[P / 64];
+#pragma unroll
+  for (int i = 0; i < P / 64; ++i) {
+    float m = kNegInf;
+    for (int g = i * 64 + lane; g < a.ng; g += P) m = fmaxf(m, sh.gmax[g]);
+    o[i] = ord_of(m);
+  }
+  // (from the first bit in which the largest and the smallest differ)
+  uint32_t least = o[0], most = o[0];
+#pragma unroll
+  for (int i = 1; i < P / 64; ++i) {
+    least = min(least, o[i]);
+    most = max(most, o[i]);
+  }
+  least = ~wave_most(~least);
+  most = wave_most(most);
+  const int top = least == most ? 11 : 31 - __builtin_clz(least ^ most);
+  uint32_t lo = most & ~((2u << top) - 1);  // at least j maxima are >= lo
+  for (int bit = top; bit >= 12; --bit) {
     const uint32_t mid = lo | (1u << bit);
     int c = 0;
-    for (int g = threadIdx.x; g < a.ng; g += kPickThreads) c += ord_of(sh.gmax[g]) >= mid;
-    if (block_sum(c, sh) >= j) lo = mid;
+#pragma unroll
+    for (int i = 0; i < P / 64; ++i) c += o[i] >= mid;
+    c = wave_count(c);
+    if (c >= j) lo = mid;
+    if (c >= j && c <= j + j / 8 + 2) break;  // (close enough)
   }
   return lo < 0x00800000u ? kNegInf : of_ord(lo);
+}
+__device__ __forceinline__ float bound_of(const SampleArgs& a, int j, const PickShared& sh) {
+  return j <= kParts / 4 ? rank_bound<kParts>(a, j, sh) : rank_bound<kManyParts>(a, j, sh);
 }
 
 // Logits >= bound into the list (unordered), as (order, lowest index first);
 // returns how many there are (more than kList: not all are in the list).
 template <int DT>
 __device__ int gather(const SampleArgs& a, const Row& row, float bound, PickShared& sh) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  constexpr int B = 4;  // groups whose loads are in flight together
+  if (threadIdx.x == 0) sh.n = sh.groups = 0;
   __syncthreads();
-  if (threadIdx.x == 0) sh.n = 0;
-  __syncthreads();
-  const int per = 8 << a.gshift;  // units of a group
-  // a wave takes 64 / 8 groups of 64 logits at a time
-  const int step = 64 / per;
-  for (int g0 = wave * step; g0 < a.ng; g0 += kPickWaves * step) {
-    const int g = g0 + lane / per;
-    const bool in = g < a.ng && sh.gmax[min(g, a.ng - 1)] >= bound;
-    if (!__any(in)) continue;
-    float v[kUnit];
-    const int u = g * per + lane % per;
-    int hits = 0;
-    if (in) {
-      load_unit<DT>(row, u, v);
+  {
+    constexpr int N = (kMaxGroups + kPickThreads - 1) / kPickThreads;
+    uint32_t in = 0;
 #pragma unroll
-      for (int e = 0; e < kUnit; ++e) hits += v[e] >= bound && v[e] != kNegInf;
+    for (int i = 0; i < N; ++i) {
+      const int g = i * kPickThreads + threadIdx.x;
+      in |= g < a.ng && sh.gmax[g] >= bound ? 1u << i : 0u;
     }
-    if (hits) {
-      int at = atomicAdd(&sh.n, hits);
+    const int c = __builtin_popcount(in), upto = wave_upto(c);
+    int at = 0;
+    if ((threadIdx.x & 63) == 63 && upto) at = atomicAdd(&sh.groups, upto);
+    at = __builtin_amdgcn_readlane(at, 63) + upto - c;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (in >> i & 1) sh.group[at++] = (uint16_t)(i * kPickThreads + threadIdx.x);
+  }
+  __syncthreads();
+  const int per = 1 << a.gshift, units = sh.groups << a.gshift;
+  for (int i1 = 0; i1 < units; i1 += B * kPickThreads) {
+    const int i0 = i1 + threadIdx.x;
+    float v[B][kUnit];
+    int u[B];
+#pragma unroll
+    for (int k = 0; k < B; ++k) {
+      const int i = i0 + k * kPickThreads;
+      // (past the end: a unit outside the row)
+      u[k] = i < units ? sh.group[i >> a.gshift] * per + (i & (per - 1)) : row.hi / kUnit + 1;
+      load_unit<DT>(row, u[k], v[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < B; ++k) {
+      uint32_t hits = 0;
 #pragma unroll
       for (int e = 0; e < kUnit; ++e)
-        if (v[e] >= bound && v[e] != kNegInf) {
-          if (at < kList) sh.l.list[at] = (uint64_t)ord_of(v[e]) << 32 | (uint32_t)~(u * kUnit + e - row.lo);
+        hits |= v[k][e] >= bound && v[k][e] != kNegInf ? 1u << e : 0u;
+      if (!__any(hits)) continue;
+      // the lane's place: one atomic for the wave
+      const int c = __builtin_popcount(hits), upto = wave_upto(c);
+      int at = 0;
+      if ((threadIdx.x & 63) == 63) at = atomicAdd(&sh.n, upto);
+      at = __builtin_amdgcn_readlane(at, 63) + upto - c;
+#pragma unroll
+      for (int e = 0; e < kUnit; ++e)
+        if (hits >> e & 1) {
+          if (at < kList) sh.l.list[at] = key_of(v[k][e], u[k] * kUnit + e - row.lo);
           ++at;
         }
     }
@@ -341,24 +461,73 @@ __device__ int gather(const SampleArgs& a, const Row& row, float bound, PickShar
   return sh.n;
 }
 
-// Sorts list[0, n) downwards (the keys differ).
-__device__ void sort_down(uint64_t* list, int n) {
+// Sorts list[0, n) downwards (the keys differ), n <= E * kPickThreads: a bitonic
+// network whose element e * kPickThreads + tid is register e of thread tid.  Distances
+// below 64 go between lanes, up to kPickThreads through LDS, above between registers.
+template <int E>
+__device__ void sort_network(uint64_t* list, int n) {
+  uint64_t r[E];
+  const int tid = threadIdx.x;
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    const int i = e * kPickThreads + tid;
+    r[e] = i < n ? list[i] : 0;
+  }
   int m = 64;
   while (m < n) m <<= 1;
-  for (int i = n + threadIdx.x; i < m; i += kPickThreads) list[i] = 0;
-  __syncthreads();
-  for (int size = 2; size <= m; size <<= 1)
-    for (int d = size >> 1; d > 0; d >>= 1) {
-      for (int i = threadIdx.x; i < m / 2; i += kPickThreads) {
-        const int x = 2 * i - (i & (d - 1)), y = x + d;
-        const uint64_t p = list[x], q = list[y];
-        if ((p < q) == ((x & size) == 0)) {
-          list[x] = q;
-          list[y] = p;
+  auto keep = [&](int e, uint64_t other, int d, int size) {
+    const int i = e * kPickThreads + tid;
+    const bool larger = ((i & d) == 0) == ((i & size) == 0);
+    r[e] = (other > r[e]) == larger ? other : r[e];
+  };
+#pragma unroll 1
+  for (int size = 2; size <= m; size <<= 1) {
+    if constexpr (E >= 2) {
+#pragma unroll
+      for (int dr = E / 2; dr > 0; dr >>= 1) {
+        const int d = dr * kPickThreads;
+        if (d < size) {
+#pragma unroll
+          for (int e = 0; e < E; ++e)
+            if ((e & dr) == 0) {
+              const uint64_t x = r[e], y = r[e + dr];
+              keep(e, y, d, size);
+              keep(e + dr, x, d, size);
+            }
         }
       }
-      __syncthreads();
     }
+#pragma unroll 1
+    for (int d = min(size, kPickThreads) >> 1; d >= 64; d >>= 1) {
+      __syncthreads();
+#pragma unroll
+      for (int e = 0; e < E; ++e) list[e * kPickThreads + tid] = r[e];
+      __syncthreads();
+#pragma unroll
+      for (int e = 0; e < E; ++e) keep(e, list[e * kPickThreads + (tid ^ d)], d, size);
+    }
+#pragma unroll 1
+    for (int d = min(size, 64) >> 1; d > 0; d >>= 1) {
+#pragma unroll
+      for (int e = 0; e < E; ++e)
+        keep(e, (uint64_t)__shfl_xor((unsigned long long)r[e], d, 64), d, size);
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    const int i = e * kPickThreads + tid;
+    if (i < n) list[i] = r[e];
+  }
+  __syncthreads();
+}
+__device__ __forceinline__ void sort_down(uint64_t* list, int n) {
+  static_assert(kList == 4 * kPickThreads, "the largest network");
+  __syncthreads();
+  if (n <= kPickThreads)
+    sort_network<1>(list, n);
+  else
+    sort_network<4>(list, n);
 }
 
 __device__ __forceinline__ double z_of(float v, float mx, double inv_t) {
@@ -397,6 +566,21 @@ __device__ __forceinline__ void emit(const SampleArgs& a, int t, int token, doub
   if (a.logprob) a.logprob[t] = (float)lp;
 }
 
+// Sorts the first n of the list and returns the key of the last kept one: the first
+// whose running sum of weights, from `base` on, reaches the limit.
+__device__ uint64_t last_of_list(int n, double base, double limit, float mx, const Params& q,
+                                 PickShared& sh) {
+  sort_down(sh.l.list, n);
+  for (int i = threadIdx.x; i < n; i += kPickThreads)
+    sh.l.w[i] = weight(logit_of(sh.l.list[i]), mx, q.inv_t);
+  __syncthreads();
+  running_sums(sh.l.w, n, sh);
+  int before = 0;
+  for (int i = threadIdx.x; i < n; i += kPickThreads) before += base + sh.l.w[i] < limit;
+  before = min(block_sum(before, sh), n - 1);
+  return sh.l.list[before];
+}
+
 // The draw among the first n of the sorted list.
 __device__ void draw_from_list(const SampleArgs& a, int t, const Params& q, float mx, int n,
                                PickShared& sh) {
@@ -425,7 +609,78 @@ __device__ void draw_from_list(const SampleArgs& a, int t, const Params& q, floa
   }
 }
 
-// Applies a function to every logit of the row above -inf: f(logit, unit's element).
+// The draw by blocks: sh.l.w[b] holds the kept weights of block b.  keep(logit,
+// index, weight) says what is kept.
+template <int DT, typename F>
+__device__ void draw_from_blocks(const SampleArgs& a, int t, const Row& row, const Params& q,
+                                 float mx, PickShared& sh, F keep) {
+  constexpr int PER = (kMaxBlocks + kPickThreads - 1) / kPickThreads;
+  const int lane = threadIdx.x & 63;
+  __syncthreads();
+  {
+    double x[PER], s = 0.0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int b = threadIdx.x * PER + i;
+      x[i] = b < a.nb ? sh.l.w[b] : 0.0;
+      s += x[i];
+    }
+    double before = block_before(s, sh);
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int b = threadIdx.x * PER + i;
+      before += x[i];
+      if (b < a.nb) sh.l.w[b] = before;
+    }
+  }
+  __syncthreads();
+  const double total = sh.l.w[a.nb - 1], target = q.u * total;
+  int first = 0;  // the first block whose running sum passes the target
+  for (int b = threadIdx.x; b < a.nb; b += kPickThreads) first += sh.l.w[b] <= target;
+  first = block_sum(first, sh);
+  if (threadIdx.x >= 64) return;
+  // Block by block from there (the sum within a block may round otherwise, then the
+  // next one has it); where nothing passes (a uniform of 1), the last one of positive
+  // weight.
+  for (int step = 0; step < 2 * a.nb; ++step) {
+    const bool back = first + step >= a.nb;
+    const int b = back ? 2 * a.nb - 1 - (first + step) : first + step;
+    if (b < 0) break;
+    float v[kUnit];
+    double w[kUnit], s = 0.0;
+    load_unit<DT>(row, b * 64 + lane, v);
+#pragma unroll
+    for (int e = 0; e < kUnit; ++e) {
+      const double f = v[e] == kNegInf ? 0.0 : weight(v[e], mx, q.inv_t);
+      w[e] = v[e] != kNegInf && keep(v[e], (b * 64 + lane) * kUnit + e - row.lo, f) ? f : 0.0;
+      s += w[e];
+    }
+    double x = s;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const double y = __shfl_up(x, o, 64);
+      if (lane >= o) x += y;
+    }
+    double run = (b ? sh.l.w[b - 1] : 0.0) + (x - s);
+    int hit = -1;
+    float hv = 0.0f;
+#pragma unroll
+    for (int e = 0; e < kUnit; ++e) {
+      run += w[e];
+      if (w[e] > 0.0 && (back || (hit < 0 && run > target))) {
+        hit = e;
+        hv = v[e];
+      }
+    }
+    const uint64_t any = __ballot(hit >= 0);
+    if (!any) continue;
+    if (lane == (back ? 63 - (int)__builtin_clzll(any) : (int)__builtin_ctzll(any)))
+      emit(a, t, (b * 64 + lane) * kUnit + hit - row.lo, log_prob(hv, mx, q.inv_t, total));
+    return;
+  }
+}
+
+// Applies f(logit, index) to every logit of the row above -inf.
 template <int DT, typename F>
 __device__ __forceinline__ void each_logit(const Row& row, F f) {
   const int units = (row.hi + kUnit - 1) / kUnit;
@@ -434,7 +689,7 @@ __device__ __forceinline__ void each_logit(const Row& row, F f) {
     load_unit<DT>(row, u, v);
 #pragma unroll
     for (int e = 0; e < kUnit; ++e)
-      if (v[e] != kNegInf) f(v[e], u * kUnit + e);
+      if (v[e] != kNegInf) f(v[e], u * kUnit + e - row.lo);
   }
 }
 
@@ -471,6 +726,7 @@ template <int DT>
 __device__ void kth_largest(const Row& row, int k, PickShared& sh, uint32_t& key, int& equals) {
   uint32_t prefix = 0;
   int need = k;
+#pragma unroll 1
   for (int pass = 0; pass < 3; ++pass) {
     const int shift = pass == 0 ? 21 : (pass == 1 ? 10 : 0);
     const uint32_t bins = pass < 2 ? 0x7ffu : 0x3ffu;
@@ -497,25 +753,94 @@ __device__ void kth_largest(const Row& row, int k, PickShared& sh, uint32_t& key
   equals = need;
 }
 
-// The whole row: cuts it by histograms and draws.  What is kept at the end is
-// every logit above `cut`, and the first `equals` of those that equal it.
+// The key of the n-th logit, by index, of those whose order is `cut` (n >= 1, and
+// there are that many).
 template <int DT>
-__device__ void whole_row(const SampleArgs& a, int t, const Row& row, const Params& q, float mx,
-                          PickShared& sh) {
-  uint32_t cut = 0;  // (-inf's order and below: nothing equals it)
+__device__ uint64_t nth_equal(const SampleArgs& a, const Row& row, uint32_t cut, int n,
+                              PickShared& sh) {
+  const int lane = threadIdx.x & 63;
+  auto equal_in = [&](int b, int (&eq)[kUnit]) {
+    float v[kUnit];
+    load_unit<DT>(row, b * 64 + lane, v);
+    int c = 0;
+#pragma unroll
+    for (int e = 0; e < kUnit; ++e) {
+      eq[e] = v[e] != kNegInf && ord_of(v[e]) == cut;
+      c += eq[e];
+    }
+    return c;
+  };
+  __syncthreads();
+  for (int b = threadIdx.x >> 6; b < a.nb; b += kPickWaves) {
+    int eq[kUnit];
+    int c = equal_in(b, eq);
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) c += __shfl_xor(c, o, 64);
+    if (lane == 0) sh.l.ties[b] = c;
+  }
+  __syncthreads();
+  constexpr int PER = (kMaxBlocks + kPickThreads - 1) / kPickThreads;
+  int c[PER], s = 0;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int b = threadIdx.x * PER + i;
+    c[i] = b < a.nb ? sh.l.ties[b] : 0;
+    s += c[i];
+  }
+  int before = block_before(s, sh);
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    if (before < n && before + c[i] >= n) {
+      sh.found = threadIdx.x * PER + i;
+      sh.extra = before;
+    }
+    before += c[i];
+  }
+  __syncthreads();
+  const int b = sh.found;
+  int need = n - sh.extra;
+  int eq[kUnit];
+  int x = equal_in(b, eq);
+  need += x;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int y = __shfl_up(x, o, 64);
+    if (lane >= o) x += y;
+  }
+  need -= x;  // (of the lane's own)
+  if (threadIdx.x < 64) {
+#pragma unroll
+    for (int e = 0; e < kUnit; ++e) {
+      need -= eq[e];
+      if (eq[e] && need == 0) sh.extra = (b * 64 + lane) * kUnit + e - row.lo;
+    }
+  }
+  __syncthreads();
+  const int at = sh.extra;
+  __syncthreads();
+  return (uint64_t)cut << 32 | (uint32_t)~at;
+}
+
+// The whole row by one workgroup: cuts it by histograms and draws.  What is kept at
+// the end is every logit whose key is at least `last`.
+template <int DT>
+__device__ __noinline__ void whole_row(const SampleArgs& a, int t, const Row& row, const Params& q,
+                                       float mx, PickShared& sh) {
+  uint64_t last = 0;
+  uint32_t cut = 0;  // logits above it, and the first `equals` of those that equal it
   int equals = 0;
   if (q.k > 0) {
     kth_largest<DT>(row, q.k, sh, cut, equals);
     // below min_p already: the cut is min_p's
     if (equals && weight(of_ord(cut), mx, q.inv_t) < q.min_p) cut = 0, equals = 0;
   }
-  const bool cuts = q.k > 0 || q.p < 1.0 || q.min_p > 0.0;
   auto kept = [&](float v, double w) { return ord_of(v) > cut && w >= q.min_p; };
   if (q.p < 1.0) {
     const double w_cut = equals ? weight(of_ord(cut), mx, q.inv_t) : 0.0;
     double top = 0.0, width = 1.0 / 64.0;  // the bins: [top - (b + 1) width, top - b width)
     double base = 0.0, limit = 0.0;        // weight above the bins; top_p of all
     int count = 0;                         // logits above the bins
+#pragma unroll 1
     for (int level = 0;; ++level) {
       // (the top is the top of a bin one level up; the last bin of the first level
       // takes everything below, which no top_p reaches)
@@ -535,7 +860,7 @@ __device__ void whole_row(const SampleArgs& a, int t, const Row& row, const Para
       each_logit<DT>(row, [&](float v, int) {
         const int b = bin_of(v);
         if (b < 0) return;
-        const double w = v == mx ? 1.0 : weight_of(z_of(v, mx, q.inv_t));
+        const double w = weight(v, mx, q.inv_t);
         if (!kept(v, w) || w == 0.0) return;
         // relative to the weight at the bin's top, so that nothing is lost
         const double rel =
@@ -574,7 +899,9 @@ __device__ void whole_row(const SampleArgs& a, int t, const Row& row, const Para
       }
       if (b == kBins) {  // reached among the equals of the cut, or by rounding at the end
         const double c = w_cut > 0.0 ? ceil((limit - all) / w_cut) : 0.0;
-        equals = c < (double)equals ? max((int)c, 0) : equals;
+        // (fewer than one: the logits above the cut reach it)
+        if (equals && c < (double)equals) equals = max((int)c, 0);
+        if (equals == 0 && cut) cut += 1;
         break;
       }
       if (b > 0) base = __longlong_as_double((long long)sh.h.mass[b - 1]);
@@ -588,31 +915,17 @@ __device__ void whole_row(const SampleArgs& a, int t, const Row& row, const Para
       if (here <= kList) {
         if (threadIdx.x == 0) sh.n = 0;
         __syncthreads();
-        each_logit<DT>(row, [&](float v, int j) {
-          if (bin_of(v) != b) return;
-          if (!kept(v, v == mx ? 1.0 : weight_of(z_of(v, mx, q.inv_t)))) return;
+        each_logit<DT>(row, [&](float v, int i) {
+          if (bin_of(v) != b || !kept(v, weight(v, mx, q.inv_t))) return;
           const int at = atomicAdd(&sh.n, 1);
-          if (at < kList) sh.l.list[at] = (uint64_t)ord_of(v) << 32 | (uint32_t)~(j - row.lo);
+          if (at < kList) sh.l.list[at] = key_of(v, i);
         });
         __syncthreads();
-        const int n = min(sh.n, kList);
-        sort_down(sh.l.list, n);
-        for (int i = threadIdx.x; i < n; i += kPickThreads)
-          sh.l.w[i] = weight(of_ord((uint32_t)(sh.l.list[i] >> 32)), mx, q.inv_t);
-        __syncthreads();
-        running_sums(sh.l.w, n, sh);
-        // the last kept one is the first whose running sum reaches the limit
-        int before = 0;
-        for (int i = threadIdx.x; i < n; i += kPickThreads) before += base + sh.l.w[i] < limit;
-        before = min(block_sum(before, sh), n - 1);
-        cut = (uint32_t)(sh.l.list[before] >> 32);
-        int eq = 0;
-        for (int i = threadIdx.x; i <= before; i += kPickThreads)
-          eq += (uint32_t)(sh.l.list[i] >> 32) == cut;
-        equals = block_sum(eq, sh);
+        last = last_of_list(min(sh.n, kList), base, limit, mx, q, sh);
+        equals = -1;  // (known)
         break;
       }
-      // too many to sort: one value, or values whose weights are the same to 2^-50
+      // too many to sort: one value, or values whose weights are the same to 2^-45
       if (threadIdx.x == 0) {
         sh.lo = 0xffffffffu;
         sh.hi = 0;
@@ -621,8 +934,7 @@ __device__ void whole_row(const SampleArgs& a, int t, const Row& row, const Para
       {
         uint32_t lo = 0xffffffffu, hi = 0;
         each_logit<DT>(row, [&](float v, int) {
-          if (bin_of(v) != b) return;
-          if (!kept(v, v == mx ? 1.0 : weight_of(z_of(v, mx, q.inv_t)))) return;
+          if (bin_of(v) != b || !kept(v, weight(v, mx, q.inv_t))) return;
           lo = min(lo, ord_of(v));
           hi = max(hi, ord_of(v));
         });
@@ -647,263 +959,214 @@ __device__ void whole_row(const SampleArgs& a, int t, const Row& row, const Para
       width /= kBins;
     }
   }
+  if (equals > 0)
+    last = nth_equal<DT>(a, row, cut, equals, sh);
+  else if (equals == 0)
+    last = (uint64_t)cut << 32;  // (cut 0: everything)
 
-  // The draw: blocks' counts of equals of the cut, then their weights.
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int per_group = (64 << a.gshift);
-  auto block_max = [&](int b) {  // of a block of 512 (at most that many groups)
-    float m = kNegInf;
-    for (int g = b * kBlock / per_group; g <= (b * kBlock + kBlock - 1) / per_group; ++g)
-      if (g < a.ng) m = fmaxf(m, sh.gmax[g]);
-    return m;
-  };
+  // The draw: the blocks' kept weights first.
+  auto keep = [&](float v, int i, double w) { return key_of(v, i) >= last && w >= q.min_p; };
+  const int lane = threadIdx.x & 63;
   __syncthreads();
-  for (int b = wave; b < a.nb; b += kPickWaves) {
-    int c = 0;
-    if (equals && ord_of(block_max(b)) >= cut) {
-      float v[kUnit];
-      load_unit<DT>(row, b * 64 + lane, v);
-#pragma unroll
-      for (int e = 0; e < kUnit; ++e) c += v[e] != kNegInf && ord_of(v[e]) == cut;
-#pragma unroll
-      for (int o = 32; o > 0; o >>= 1) c += __shfl_xor(c, o, 64);
-    }
-    if (lane == 0) sh.b.ties[b] = c;
-  }
-  __syncthreads();
-  {
-    constexpr int PER = (kMaxBlocks + kPickThreads - 1) / kPickThreads;
-    int c[PER], s = 0;
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const int b = threadIdx.x * PER + i;
-      c[i] = b < a.nb ? sh.b.ties[b] : 0;
-      s += c[i];
-    }
-    int before = block_before(s, sh);
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const int b = threadIdx.x * PER + i;
-      if (b < a.nb) sh.b.ties[b] = before;
-      before += c[i];
-    }
-  }
-  __syncthreads();
-  // a lane's weights of block b
-  auto weights = [&](int b, float (&v)[kUnit], double (&w)[kUnit]) {
+  for (int b = threadIdx.x >> 6; b < a.nb; b += kPickWaves) {
+    float v[kUnit];
     load_unit<DT>(row, b * 64 + lane, v);
-    int c = 0;
-#pragma unroll
-    for (int e = 0; e < kUnit; ++e) c += v[e] != kNegInf && ord_of(v[e]) == cut;
-    int x = c;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int y = __shfl_up(x, o, 64);
-      if (lane >= o) x += y;
-    }
-    int tie = sh.b.ties[b] + x - c;
-#pragma unroll
-    for (int e = 0; e < kUnit; ++e) {
-      const double f = v[e] == kNegInf ? 0.0 : weight(v[e], mx, q.inv_t);
-      const bool eq = v[e] != kNegInf && ord_of(v[e]) == cut;
-      w[e] = (ord_of(v[e]) > cut || (eq && tie < equals)) && f >= q.min_p ? f : 0.0;
-      tie += eq;
-    }
-  };
-  for (int b = wave; b < a.nb; b += kPickWaves) {
     double s = 0.0;
-    if (!cuts) {  // every logit is kept: the sums of the first launch
-      const float ref = a.bref[(size_t)t * a.nb + b];
-      if (lane == 0)
-        sh.b.mass[b] =
-            ref == kNegInf ? 0.0 : a.bmass[(size_t)t * a.nb + b] * weight(ref, mx, q.inv_t);
-      continue;
-    }
-    const float m = block_max(b);
-    if (m != kNegInf && ord_of(m) >= cut) {
-      float v[kUnit];
-      double w[kUnit];
-      weights(b, v, w);
-#pragma unroll
-      for (int e = 0; e < kUnit; ++e) s += w[e];
-      s = wave_sum(s);
-    }
-    if (lane == 0) sh.b.mass[b] = s;
-  }
-  __syncthreads();
-  double total;
-  {
-    constexpr int PER = (kMaxBlocks + kPickThreads - 1) / kPickThreads;
-    double x[PER], s = 0.0;
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const int b = threadIdx.x * PER + i;
-      x[i] = b < a.nb ? sh.b.mass[b] : 0.0;
-      s += x[i];
-    }
-    double before = block_before(s, sh);
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const int b = threadIdx.x * PER + i;
-      before += x[i];
-      if (b < a.nb) sh.b.mass[b] = before;
-    }
-    __syncthreads();
-    total = sh.b.mass[a.nb - 1];
-  }
-  const double target = q.u * total;
-  int first = 0;  // the first block whose running sum passes the target
-  for (int b = threadIdx.x; b < a.nb; b += kPickThreads) first += sh.b.mass[b] <= target;
-  first = block_sum(first, sh);
-  if (wave != 0) return;
-  // (the sum within a block may round otherwise: then the next block has it)
-  for (int b = first; b < a.nb; ++b) {
-    float v[kUnit];
-    double w[kUnit], s = 0.0;
-    weights(b, v, w);
-#pragma unroll
-    for (int e = 0; e < kUnit; ++e) s += w[e];
-    double x = s;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const double y = __shfl_up(x, o, 64);
-      if (lane >= o) x += y;
-    }
-    double run = (b ? sh.b.mass[b - 1] : 0.0) + (x - s);
-    int hit = -1;
 #pragma unroll
     for (int e = 0; e < kUnit; ++e) {
-      run += w[e];
-      if (hit < 0 && w[e] > 0.0 && run > target) hit = e;
+      const double w = v[e] == kNegInf ? 0.0 : weight(v[e], mx, q.inv_t);
+      if (v[e] != kNegInf && keep(v[e], (b * 64 + lane) * kUnit + e - row.lo, w)) s += w;
     }
-    const uint64_t any = __ballot(hit >= 0);
-    if (any) {
-      if (lane == (int)__builtin_ctzll(any)) {
-#pragma unroll
-        for (int e = 0; e < kUnit; ++e)
-          if (e == hit)
-            emit(a, t, (b * 64 + lane) * kUnit + e - row.lo,
-                 log_prob(v[e], mx, q.inv_t, total));
-      }
-      return;
-    }
+    s = wave_sum(s);
+    if (lane == 0) sh.l.w[b] = s;
   }
-  // nothing passes (a uniform of 1 or more): the last one with a weight
-  for (int b = a.nb - 1; b >= 0; --b) {
-    float v[kUnit];
-    double w[kUnit];
-    weights(b, v, w);
-    int hit = -1;
+  draw_from_blocks<DT>(a, t, row, q, mx, sh, keep);
+}
+
+// The first largest logit.
+template <int DT>
+__device__ void pick_largest(const SampleArgs& a, int t, const Row& row, float mx,
+                             PickShared& sh) {
+  const int n = gather<DT>(a, row, mx, sh);  // the largest and its equals
+  uint64_t best = 0;
+  for (int i = threadIdx.x; i < min(n, kList); i += kPickThreads)
+    best = best > sh.l.list[i] ? best : sh.l.list[i];
+  if (n > kList) {  // (more equals than the list holds)
+    each_logit<DT>(row, [&](float v, int i) {
+      const uint64_t k = key_of(v, i);
+      best = best > k ? best : k;
+    });
+  }
 #pragma unroll
-    for (int e = 0; e < kUnit; ++e)
-      if (w[e] > 0.0) hit = e;
-    const uint64_t any = __ballot(hit >= 0);
-    if (any) {
-      if (lane == 63 - (int)__builtin_clzll(any)) {
-#pragma unroll
-        for (int e = 0; e < kUnit; ++e)
-          if (e == hit)
-            emit(a, t, (b * 64 + lane) * kUnit + e - row.lo,
-                 log_prob(v[e], mx, q.inv_t, total));
-      }
-      return;
+  for (int o = 32; o > 0; o >>= 1) {
+    const uint64_t x = __shfl_xor((unsigned long long)best, o, 64);
+    best = best > x ? best : x;
+  }
+  if ((threadIdx.x & 63) == 0) sh.l.w[threadIdx.x >> 6] = __longlong_as_double((long long)best);
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int w = 0; w < kPickWaves; ++w) {
+      const uint64_t x = (uint64_t)__double_as_longlong(sh.l.w[w]);
+      best = best > x ? best : x;
     }
+    emit(a, t, index_of(best), 0.0);
   }
 }
 
-template <int DT>
-__global__ __launch_bounds__(kPickThreads) void pick_kernel(SampleArgs a) {
+__device__ __forceinline__ uint64_t lane_of(uint64_t x, int lane) {
+  return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(x >> 32), lane) << 32 |
+         (uint32_t)__builtin_amdgcn_readlane((int)x, lane);
+}
+
+// The rest of a row whose list has at most 64 logits: filters (total: of all weights,
+// where the list is only part of them; 0: the list's) and draw.  Wave w compares with
+// the logits 8 w .. 8 w + 7, and wave 0 joins the parts.  Returns whether the list was
+// enough.
+__device__ bool pick_of_64(const SampleArgs& a, int t, const Params& q, float mx, int n,
+                           double total, PickShared& sh) {
+  static_assert(kPickWaves == 8, "eight logits to a wave");
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const bool in = lane < n;
+  uint64_t key = in ? sh.l.list[lane] : 0;
+  int rank = 0;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) rank += lane_of(key, wave * 8 + j) > key;
+  int* ranks = (int*)sh.l.w;
+  ranks[wave * 64 + lane] = rank;
+  __syncthreads();
+  rank = 0;
+#pragma unroll
+  for (int w = 0; w < 8; ++w) rank += ranks[w * 64 + lane];
+  if (wave == 0 && in) sh.l.list[64 + rank] = key;
+  __syncthreads();
+  key = in ? sh.l.list[64 + lane] : 0;  // the lane's logit, larger ones before it
+  const float v = logit_of(key);
+  const double w = in ? weight(v, mx, q.inv_t) : 0.0;
+  int m = q.min_p > 0.0 ? max(__builtin_popcountll(__ballot(in && w >= q.min_p)), 1) : n;
+  if (q.k > 0) m = min(m, q.k);
+  double run = lane < m ? w : 0.0;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const double y = __shfl_up(run, o, 64);
+    if (lane >= o) run += y;
+  }
+  if (q.p < 1.0) {
+    const double sum = __shfl(run, m - 1, 64), limit = q.p * (total > 0.0 ? total : sum);
+    if (total > 0.0 && sum < limit) return false;
+    double before = __shfl_up(run, 1, 64);
+    if (lane == 0) before = 0.0;
+    m = max(__builtin_popcountll(__ballot(lane < m && before < limit)), 1);
+  }
+  const double all = __shfl(run, m - 1, 64), target = q.u * all;
+  // the kept weights up to the lane's logit, by index (added in the list's order)
+  const int at = index_of(key);
+  double part = 0.0;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const int i = wave * 8 + j;
+    const double wj = __longlong_as_double((long long)lane_of((uint64_t)__double_as_longlong(w), i));
+    part += i < m && __builtin_amdgcn_readlane(at, i) <= at ? wj : 0.0;
+  }
+  sh.l.w[512 + wave * 64 + lane] = part;
+  __syncthreads();
+  if (wave != 0) return true;
+  double cum = 0.0;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) cum += sh.l.w[512 + j * 64 + lane];
+  // the first by index that passes the target (none: the last of positive weight)
+  const bool kept = lane < m && w > 0.0;
+  const uint64_t pass = __ballot(kept && cum > target);
+  // (indices are below 2^20; what is no candidate is 0)
+  const uint32_t rate = !kept ? 0 : (!pass ? 1u + at : (cum > target ? (1u << 30) - at : 0));
+  const uint32_t best = wave_most(rate);
+  if (kept && rate == best) emit(a, t, at, log_prob(v, mx, q.inv_t, all));
+  return true;
+}
+
+template <int DT, bool DEFER>
+__global__ __launch_bounds__(kPickThreads) __attribute__((amdgpu_waves_per_eu(4))) void pick_kernel(
+    SampleArgs a) {
   __shared__ PickShared sh;
   const int t = blockIdx.x;
   const Row row = row_of<DT>(a, t);
   const Params q = params_of(a, t);
+  if (DEFER && threadIdx.x == 0) a.open[t].state = 0;
   float mx = kNegInf;
-  for (int g = threadIdx.x; g < a.ng; g += kPickThreads) {
-    const float m = a.gmax[(size_t)t * a.ng + g];
-    sh.gmax[g] = m;
-    mx = fmaxf(mx, m);
-  }
-  mx = wave_max(mx);
-  if ((threadIdx.x & 63) == 0) sh.part[threadIdx.x >> 6] = (double)mx;
-  __syncthreads();
+  {
+    constexpr int N = (kMaxGroups + kPickThreads - 1) / kPickThreads;
+    float m[N];
 #pragma unroll
-  for (int w = 0; w < kPickWaves; ++w) mx = fmaxf(mx, (float)sh.part[w]);
-  __syncthreads();
+    for (int i = 0; i < N; ++i) {
+      const int g = i * kPickThreads + threadIdx.x;
+      m[i] = a.gmax[(size_t)t * a.ng + min(g, a.ng - 1)];
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int g = i * kPickThreads + threadIdx.x;
+      if (g < a.ng) sh.gmax[g] = m[i];
+      mx = fmaxf(mx, m[i]);
+    }
+  }
+  {
+    const uint32_t o = wave_most(ord_of(mx));
+    if ((threadIdx.x & 63) == 0) sh.parti[threadIdx.x >> 6] = (int)o;
+    __syncthreads();
+    uint32_t most = 0;
+#pragma unroll
+    for (int w = 0; w < kPickWaves; ++w) most = max(most, (uint32_t)sh.parti[w]);
+    mx = of_ord(most);
+  }
   if (mx == kNegInf) {  // no token
     if (threadIdx.x == 0) emit(a, t, -1, (double)kNegInf);
     return;
   }
   if (q.greedy) {
-    const int n = gather<DT>(a, row, mx, sh);  // the largest and its equals
-    uint64_t best = 0;
-    for (int i = threadIdx.x; i < min(n, kList); i += kPickThreads)
-      best = best > sh.l.list[i] ? best : sh.l.list[i];
-    if (n > kList) {  // (more equals than the list holds)
-      each_logit<DT>(row, [&](float v, int j) {
-        const uint64_t k = (uint64_t)ord_of(v) << 32 | (uint32_t)~(j - row.lo);
-        best = best > k ? best : k;
-      });
-    }
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) {
-      const uint64_t x = __shfl_xor((unsigned long long)best, o, 64);
-      best = best > x ? best : x;
-    }
-    if ((threadIdx.x & 63) == 0) sh.l.w[threadIdx.x >> 6] = __longlong_as_double((long long)best);
-    __syncthreads();
-    if (threadIdx.x == 0) {
-      for (int w = 0; w < kPickWaves; ++w) {
-        const uint64_t x = (uint64_t)__double_as_longlong(sh.l.w[w]);
-        best = best > x ? best : x;
-      }
-      emit(a, t, (int)~(uint32_t)best, 0.0);
-    }
+    pick_largest<DT>(a, t, row, mx, sh);
     return;
   }
-  const bool cuts = q.k > 0 || q.p < 1.0 || q.min_p > 0.0;
-  float bound = kNegInf;
-  double total = 0.0;  // of all weights, where the row has no other filter than top_p
-  bool try_list = a.V <= kList;
-  if (bounded(a, q)) {
-    if (q.k > 0 && q.k <= a.ng) bound = group_bound(a, q.k, sh);
-    if (q.min_p > 0.0) {
-      // a little below the logit of weight min_p
-      const double v = (double)mx + log(q.min_p) / q.inv_t;
-      bound = fmaxf(bound, (float)(v - fabs(v) * 1e-6 - 1e-30));
+  const bool all_in = a.V <= kList, bnd = bounded(a, q);
+  if (q.k > 0 || q.p < 1.0 || q.min_p > 0.0) {
+    float bound = kNegInf;
+    double total = 0.0;  // of all weights, where top_p is the only filter
+    if (bnd) {
+      if (q.k > 0 && q.k <= min(a.ng, kMaxBound)) bound = bound_of(a, q.k, sh);
+      if (q.min_p > 0.0) {
+        // a little below the logit of weight min_p
+        const double v = (double)mx + log(q.min_p) / q.inv_t;
+        bound = fmaxf(bound, (float)(v - fabs(v) * 1e-6 - 1e-30));
+      }
+    } else if (!all_in && q.k == 0) {
+      double s = 0.0;
+      for (int b = threadIdx.x; b < a.nb; b += kPickThreads) {
+        const float ref = a.bref[(size_t)t * a.nb + b];
+        s += ref == kNegInf ? 0.0 : a.bmass[(size_t)t * a.nb + b] * weight(ref, mx, q.inv_t);
+      }
+      total = block_sum(s, sh);
+      bound = bound_of(a, min(a.ng, kTry), sh);
     }
-    try_list = true;
-  } else {
-    double s = 0.0;
-    for (int b = threadIdx.x; b < a.nb; b += kPickThreads) {
-      const float ref = a.bref[(size_t)t * a.nb + b];
-      s += ref == kNegInf ? 0.0 : a.bmass[(size_t)t * a.nb + b] * weight(ref, mx, q.inv_t);
-    }
-    total = block_sum(s, sh);
-    if (cuts && q.k == 0 && a.V > kList) {
-      bound = group_bound(a, min(a.ng, 256), sh);
-      try_list = true;
-    }
-  }
-  if (try_list && cuts) {
-    const int n = gather<DT>(a, row, bound, sh);
-    if (n <= kList) {
+    const bool list = bnd || all_in || q.k == 0;  // (else a top_k beyond the bounds)
+    const int n = list ? gather<DT>(a, row, bound, sh) : kList + 1;
+    if (n <= 64) {
+      if (pick_of_64(a, t, q, mx, n, !bnd && !all_in ? total : 0.0, sh)) return;
+    } else if (n <= kList) {
       sort_down(sh.l.list, n);
       int fit = 0;  // of at least min_p
       for (int i = threadIdx.x; i < n; i += kPickThreads) {
-        const double w = weight(of_ord((uint32_t)(sh.l.list[i] >> 32)), mx, q.inv_t);
+        const double w = weight(logit_of(sh.l.list[i]), mx, q.inv_t);
         sh.l.w[i] = w;
         fit += w >= q.min_p;
       }
-      int m = max(block_sum(fit, sh), 1);
+      int m = q.min_p > 0.0 ? max(block_sum(fit, sh), 1) : n;
       if (q.k > 0) m = min(m, q.k);
+      __syncthreads();
       bool done = true;
       if (q.p < 1.0) {
         running_sums(sh.l.w, m, sh);
         const double sum = sh.l.w[m - 1];
-        // only top_p, and logits outside the list: its sum is that of the row
-        const bool open = !bounded(a, q) && a.V > kList;
-        const double limit = q.p * (open ? total : sum);
-        done = !open || sum >= limit;
+        // only top_p, and logits outside the list: the sum is that of the row
+        const bool part = !bnd && !all_in;
+        const double limit = q.p * (part ? total : sum);
+        done = !part || sum >= limit;
         int kept = 0;
         for (int i = threadIdx.x; i < m; i += kPickThreads)
           kept += (i ? sh.l.w[i - 1] : 0.0) < limit;
@@ -914,48 +1177,344 @@ __global__ __launch_bounds__(kPickThreads) void pick_kernel(SampleArgs a) {
         return;
       }
     }
+    if constexpr (DEFER) {
+      const bool by_bins = q.k == 0;
+      if (by_bins)
+        for (int i = threadIdx.x; i < kBins; i += kPickThreads) a.hist[(size_t)t * kBins + i] = 0;
+      if (threadIdx.x == 0) {
+        OpenRow o;
+        o.state = by_bins ? 1 : 2;
+        o.n = 0;
+        o.mx = mx;
+        o.bin = kBins;
+        o.base = o.limit = 0.0;
+        a.open[t] = o;
+      }
+    } else {
+      whole_row<DT>(a, t, row, q, mx, sh);
+    }
+    return;
   }
-  whole_row<DT>(a, t, row, q, mx, sh);
+  // no filter: the sums of the first launch
+  __syncthreads();
+  for (int b = threadIdx.x; b < a.nb; b += kPickThreads) {
+    const float ref = a.bref[(size_t)t * a.nb + b];
+    sh.l.w[b] = ref == kNegInf ? 0.0 : a.bmass[(size_t)t * a.nb + b] * weight(ref, mx, q.inv_t);
+  }
+  draw_from_blocks<DT>(a, t, row, q, mx, sh, [](float, int, double) { return true; });
+}
+
+// ---------------------------------------------------------------------------
+// open rows: the bins' weights, the blocks' weights above the border, the cut
+// ---------------------------------------------------------------------------
+
+// The bin of a logit: 1/64 in log weight each, the last takes the rest.  (A bin that
+// top_p is reached in is never the last: what lies below e^-32 of the largest weight
+// is less than 2^20 e^-32, under the 2^-24 that a float top_p stays below 1.)
+__device__ __forceinline__ int open_bin(double z) {
+  const double x = z * -64.0;
+  return x < (double)(kBins - 1) ? (int)x : kBins - 1;
+}
+
+template <int DT, int BPW>
+__global__ __launch_bounds__(kScanThreads) void hist_kernel(SampleArgs a, int segs) {
+  const int t = blockIdx.x / segs, seg = blockIdx.x % segs;
+  if (a.open[t].state != 1) return;
+  __shared__ unsigned long long mass[kBins];
+  for (int i = threadIdx.x; i < kBins; i += kScanThreads) mass[i] = 0;
+  __syncthreads();
+  const Row row = row_of<DT>(a, t);
+  const Params q = params_of(a, t);
+  if (q.p >= 1.0) return;
+  const float mx = a.open[t].mx;
+  // log weights of at least min_p: all from `floor` on that weigh enough, all from
+  // `floor_sure` on
+  const double lnp = q.min_p > 0.0 ? log(q.min_p) : kLowest;
+  const double floor = fmax(kLowest, lnp - 1e-9);
+  const double floor_sure = q.min_p > 0.0 ? lnp + 1e-9 : kLowest;
+  const int b0 = (seg * (kScanThreads / 64) + threadIdx.x / 64) * BPW;
+  float u[BPW][kUnit];
+  load_units<DT, BPW>(row, b0 * 64, u);
+#pragma unroll
+  for (int i = 0; i < BPW; ++i) {
+    int bin[kUnit];
+    double w[kUnit];
+    bool in[kUnit], rest = false;
+#pragma unroll
+    for (int e = 0; e < kUnit; ++e) {
+      const double z = u[i][e] == mx ? 0.0 : z_of(u[i][e], mx, q.inv_t);
+      in[e] = z >= floor;
+      bin[e] = open_bin(z);
+      rest |= in[e] && (bin[e] == kBins - 1 || z < floor_sure);
+      // e^d, -1/64 < d <= 0, relative to the bin's top: the seventh term of the series
+      // is below 2^-53
+      const double d = __builtin_fma((double)bin[e], 1.0 / 64.0, z);
+      w[e] = 1.0 / 720;
+      w[e] = __builtin_fma(w[e], d, 1.0 / 120);
+      w[e] = __builtin_fma(w[e], d, 1.0 / 24);
+      w[e] = __builtin_fma(w[e], d, 1.0 / 6);
+      w[e] = __builtin_fma(w[e], d, 0.5);
+      w[e] = __builtin_fma(w[e], d, 1.0);
+      w[e] = __builtin_fma(w[e], d, 1.0);
+    }
+    if (__any(rest)) {  // the last bin, and weights next to min_p
+#pragma unroll 1
+      for (int e = 0; e < kUnit; ++e) {
+        float v = u[i][0];
+#pragma unroll
+        for (int j = 1; j < kUnit; ++j) v = e == j ? u[i][j] : v;
+        const double z = v == mx ? 0.0 : z_of(v, mx, q.inv_t);
+        const bool ok = z >= floor && weight(v, mx, q.inv_t) >= q.min_p;
+        const double far = weight_of(fmin(z + (kBins - 1) / 64.0, 0.0));
+#pragma unroll
+        for (int j = 0; j < kUnit; ++j)
+          if (e == j) {
+            in[j] = ok;
+            if (bin[j] == kBins - 1) w[j] = far;
+          }
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < kUnit; ++e) {
+      // (w 2^42 as the low bits of a float64 of that step)
+      const long long fixed = __double_as_longlong(__builtin_fma(w[e], 0x1p42, 0x1p52)) & ((1ll << 52) - 1);
+      if (in[e]) atomicAdd(&mass[bin[e]], (unsigned long long)fixed);
+    }
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < kBins; i += kScanThreads)
+    if (mass[i]) atomicAdd(&a.hist[(size_t)t * kBins + i], mass[i]);
+}
+
+template <int DT, int BPW>
+__global__ __launch_bounds__(kScanThreads) void mark_kernel(SampleArgs a, int segs) {
+  const int t = blockIdx.x / segs, seg = blockIdx.x % segs;
+  if (a.open[t].state != 1) return;
+  constexpr int W = kScanThreads / 64, PER = kBins / kScanThreads;
+  __shared__ double part[W];
+  __shared__ double running[kBins];
+  __shared__ uint64_t mine[kList];  // the workgroup's logits of the border bin
+  __shared__ int found, count, place;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const Row row = row_of<DT>(a, t);
+  const Params q = params_of(a, t);
+  const float mx = a.open[t].mx;
+  const double floor = kLowest;
+  // the border bin: every workgroup finds the same (without a top_p there is none)
+  double m[PER], s = 0.0;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int b = threadIdx.x * PER + i;
+    const unsigned long long f = q.p < 1.0 ? a.hist[(size_t)t * kBins + b] : 0;
+    m[i] = f ? (double)f * 0x1p-42 * weight_of(b * (-1.0 / 64.0)) : 0.0;
+    s += m[i];
+  }
+  double x = s;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const double y = __shfl_up(x, o, 64);
+    if (lane >= o) x += y;
+  }
+  if (lane == 63) part[wave] = x;
+  if (threadIdx.x == 0) {
+    found = kBins;
+    count = 0;
+  }
+  __syncthreads();
+  double all = 0.0, run = x - s;
+#pragma unroll
+  for (int w = 0; w < W; ++w) {
+    if (w < wave) run += part[w];
+    all += part[w];
+  }
+  const double limit = q.p * all;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int b = threadIdx.x * PER + i;
+    run += m[i];
+    running[b] = run;
+    if (m[i] > 0.0 && run >= limit) atomicMin(&found, b);
+  }
+  __syncthreads();
+  const int border = found;
+  if (seg == 0 && threadIdx.x == 0) {
+    a.open[t].bin = border;
+    a.open[t].limit = limit;
+    a.open[t].base = border > 0 && border < kBins ? running[border - 1] : 0.0;
+  }
+  if (border == kBins && q.p < 1.0) return;  // (rounding at the end: the row is done alone)
+  const int b0 = (seg * W + wave) * BPW;
+  float u[BPW][kUnit];
+  load_units<DT, BPW>(row, b0 * 64, u);
+#pragma unroll
+  for (int i = 0; i < BPW; ++i) {
+    if (b0 + i >= a.nb) break;
+    double sum = 0.0;
+    uint32_t listed = 0;
+#pragma unroll
+    for (int e = 0; e < kUnit; ++e) {
+      const double z = u[i][e] == mx ? 0.0 : z_of(u[i][e], mx, q.inv_t);
+      const double w = u[i][e] == mx ? 1.0 : weight_of(z);
+      const int b = open_bin(z);
+      const bool in = z >= floor && w >= q.min_p;
+      sum += in && b < border ? w : 0.0;
+      listed |= in && b == border ? 1u << e : 0u;
+    }
+    if (__any(listed)) {
+      const int c = __builtin_popcount(listed), upto = wave_upto(c);
+      int at = 0;
+      if (lane == 63) at = atomicAdd(&count, upto);
+      at = __builtin_amdgcn_readlane(at, 63) + upto - c;
+#pragma unroll
+      for (int e = 0; e < kUnit; ++e)
+        if (listed >> e & 1) {
+          if (at < kList) mine[at] = key_of(u[i][e], ((b0 + i) * 64 + lane) * kUnit + e - row.lo);
+          ++at;
+        }
+    }
+    sum = wave_sum(sum);
+    if (lane == 0) a.bmass[(size_t)t * a.nb + b0 + i] = sum;
+  }
+  __syncthreads();
+  if (threadIdx.x == 0 && count) place = atomicAdd(&a.open[t].n, count);
+  __syncthreads();
+  for (int i = threadIdx.x; i < min(count, kList); i += kScanThreads)
+    if (place + i < kList) a.list[(size_t)t * kList + place + i] = mine[i];
 }
 
 template <int DT>
-hipError_t launch(const SampleArgs& a, hipStream_t stream) {
+__global__ __launch_bounds__(kPickThreads) __attribute__((amdgpu_waves_per_eu(4))) void finish_kernel(
+    SampleArgs a) {
+  const int t = blockIdx.x;
+  const OpenRow o = a.open[t];
+  if (o.state == 0) return;
+  __shared__ PickShared sh;
+  const Row row = row_of<DT>(a, t);
+  const Params q = params_of(a, t);
+  const bool border = q.p < 1.0;
+  if (o.state == 2 || (border && (o.bin >= kBins - 1 || o.n > kList || o.limit <= 0.0))) {
+    for (int g = threadIdx.x; g < a.ng; g += kPickThreads) sh.gmax[g] = a.gmax[(size_t)t * a.ng + g];
+    whole_row<DT>(a, t, row, q, o.mx, sh);
+    return;
+  }
+  uint64_t last = 0;
+  if (border) {
+    for (int i = threadIdx.x; i < o.n; i += kPickThreads)
+      sh.l.list[i] = a.list[(size_t)t * kList + i];
+    last = last_of_list(o.n, o.base, o.limit, o.mx, q, sh);
+  }
+  // The border's kept logits join their blocks' sums, as whole numbers of 2^-42 of the
+  // weight at the bin's top.
+  unsigned long long* fixed = (unsigned long long*)sh.l.w;
+  const double top = o.bin * (-1.0 / 64.0);
+  __syncthreads();
+  for (int b = threadIdx.x; b < a.nb; b += kPickThreads) fixed[b] = 0;
+  __syncthreads();
+  for (int i = threadIdx.x; border && i < o.n; i += kPickThreads) {
+    const uint64_t k = sh.l.list[i];
+    if (k < last) break;
+    const float v = logit_of(k);
+    const double z = v == o.mx ? 0.0 : z_of(v, o.mx, q.inv_t);
+    atomicAdd(&fixed[(index_of(k) + row.lo) / kBlock],
+              (unsigned long long)(weight_of(fmin(z - top, 0.0)) * 0x1p42));
+  }
+  __syncthreads();
+  const double unit = border ? weight_of(top) * 0x1p-42 : 0.0;
+  for (int b = threadIdx.x; b < a.nb; b += kPickThreads)
+    sh.l.w[b] = a.bmass[(size_t)t * a.nb + b] + (double)fixed[b] * unit;
+  draw_from_blocks<DT>(a, t, row, q, o.mx, sh,
+                       [&](float v, int i, double w) { return key_of(v, i) >= last && w >= q.min_p; });
+}
+
+// Calls of at least this many rows leave open rows to launches of their own.  Those
+// take 3 us where no row is open; one workgroup takes 10 times as long as they do for an
+// open row of 150,000 logits.
+constexpr int kDeferRows = 4;
+// Rows of one round of launches (the workspace is this many rows' at most).
+constexpr int kRoundRows = 1024;
+
+template <int DT>
+hipError_t launch(SampleArgs a, hipStream_t stream) {
   constexpr int W = kScanThreads / 64;
-  // few rows: more workgroups of less each
-  const int bpw = (long long)a.T * a.nb < 4096 * W ? 2 : 8;
-  const int segs = (a.nb + W * bpw - 1) / (W * bpw);
-  if (bpw == 2)
-    scan_kernel<DT, 2><<<(unsigned)(a.T * segs), kScanThreads, 0, stream>>>(a, segs);
-  else
-    scan_kernel<DT, 8><<<(unsigned)(a.T * segs), kScanThreads, 0, stream>>>(a, segs);
-  const hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  pick_kernel<DT><<<(unsigned)a.T, kPickThreads, 0, stream>>>(a);
-  return hipGetLastError();
+  constexpr int ES = DT == PCTREE_F32 ? 4 : 2;
+  const int rows = a.T;
+  const bool defer = a.open && (a.has & (kHasTopP | kHasTopK | kHasMinP));
+  for (int t0 = 0; t0 < rows; t0 += kRoundRows) {
+    a.T = rows - t0 < kRoundRows ? rows - t0 : kRoundRows;
+    // few rows: more workgroups of less each
+    const int bpw = (long long)a.T * a.nb < 4096 * W ? 2 : 8;
+    const int segs = (a.nb + W * bpw - 1) / (W * bpw);
+    const unsigned grid = (unsigned)(a.T * segs);
+    if (bpw == 2)
+      scan_kernel<DT, 2><<<grid, kScanThreads, 0, stream>>>(a, segs);
+    else
+      scan_kernel<DT, 8><<<grid, kScanThreads, 0, stream>>>(a, segs);
+    if (defer) {
+      pick_kernel<DT, true><<<(unsigned)a.T, kPickThreads, 0, stream>>>(a);
+      if (bpw == 2) {
+        hist_kernel<DT, 2><<<grid, kScanThreads, 0, stream>>>(a, segs);
+        mark_kernel<DT, 2><<<grid, kScanThreads, 0, stream>>>(a, segs);
+      } else {
+        hist_kernel<DT, 8><<<grid, kScanThreads, 0, stream>>>(a, segs);
+        mark_kernel<DT, 8><<<grid, kScanThreads, 0, stream>>>(a, segs);
+      }
+      finish_kernel<DT><<<(unsigned)a.T, kPickThreads, 0, stream>>>(a);
+    } else {
+      pick_kernel<DT, false><<<(unsigned)a.T, kPickThreads, 0, stream>>>(a);
+    }
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    a.logits = (const char*)a.logits + (long long)a.T * a.row_stride * ES;
+    a.uniform += a.T;
+    a.temperature += a.T;
+    a.top_k += a.T;
+    a.top_p += a.T;
+    a.min_p += a.T;
+    a.token += a.T;
+    if (a.logprob) a.logprob += a.T;
+  }
+  return hipSuccess;
 }
 
 }  // namespace
 
 void plan_sample(int V, int* ng, int* nb, int* gshift) {
   const int span = V + kUnit - 1;  // elements from the 16-byte boundary on
-  int s = 0;
-  while ((span + (64 << s) - 1) / (64 << s) > kMaxGroups - 1) ++s;
+  int s = 0;                       // (a group: the units of 1 << s lanes)
+  while ((span + (kUnit << s) - 1) / (kUnit << s) > kMaxGroups - 1) ++s;
   *gshift = s;
-  *ng = (span + (64 << s) - 1) / (64 << s);
+  *ng = (span + (kUnit << s) - 1) / (kUnit << s);
   *nb = (span + kBlock - 1) / kBlock;
 }
+
+namespace {
+int round_rows(int T) { return T < kRoundRows ? T : kRoundRows; }
+bool deferring(int T, int V) { return T >= kDeferRows && V > kList; }
+}  // namespace
 
 size_t sample_bytes(int T, int V) {
   int ng, nb, s;
   plan_sample(V, &ng, &nb, &s);
-  return ((size_t)T * ((size_t)nb * 12 + (size_t)ng * 4) + 511) / 256 * 256;
+  size_t row = (size_t)nb * 12 + (size_t)ng * 4;
+  if (deferring(T, V)) row += (kBins + kList) * sizeof(uint64_t) + sizeof(OpenRow);
+  return ((size_t)round_rows(T) * row + 511) / 256 * 256;
 }
 
 void place_sample(SampleArgs* a, void* workspace) {
   plan_sample(a->V, &a->ng, &a->nb, &a->gshift);
-  a->bmass = (double*)workspace;
-  a->bref = (float*)(a->bmass + (size_t)a->T * a->nb);
-  a->gmax = a->bref + (size_t)a->T * a->nb;
+  const size_t T = (size_t)round_rows(a->T);
+  char* w = (char*)workspace;
+  a->hist = a->list = nullptr;
+  a->open = nullptr;
+  if (deferring(a->T, a->V)) {
+    a->hist = (unsigned long long*)w;
+    a->list = a->hist + T * kBins;
+    a->open = (OpenRow*)(a->list + T * kList);
+    w = (char*)(a->open + T);
+  }
+  a->bmass = (double*)w;
+  a->bref = (float*)(a->bmass + T * a->nb);
+  a->gmax = a->bref + T * a->nb;
 }
 
 hipError_t launch_sample(const SampleArgs& a, int dtype, hipStream_t stream) {

@@ -96,12 +96,13 @@ def test_each_row_has_its_own_parameters(dt):
     check(x, rng.random(T), **par)
 
 
-def test_open_rows():
-    """Rows whose kept set is large: nearly flat logits, top_p and large top_k."""
+@pytest.mark.parametrize("T", [2, 5])
+def test_open_rows(T):
+    """Rows whose kept set is large: nearly flat logits, top_p and large top_k; few rows
+    are cut by one workgroup, more by launches of their own."""
     rng = np.random.default_rng(5)
     for dt, V, sigma in (("f32", 151936, 1.0), ("bf16", 151936, 0.3), ("f32", 151936, 1e-3), ("f32", 30000, 1e-6),
                          ("bf16", 151936, 1e-3), ("f16", 50000, 0.1)):
-        T = 4
         x = rows(7, T, V, dt, sigma=sigma, head=0.0)
         for f in (dict(top_p=0.9), dict(top_p=0.5, temperature=2.0), dict(top_k=20000, top_p=0.7),
                   dict(top_k=V // 2), dict(min_p=0.9, top_p=0.6), dict()):
@@ -189,6 +190,14 @@ def test_rows_at_any_alignment(dt, off, gap):
     u = np.random.default_rng(off).random(T)
     for f in FILTERS:
         check(view, u, **f)
+
+
+def test_more_rows_than_one_round():
+    """Calls of more rows than the workspace holds go round by round."""
+    T, V = 2100, 2500
+    x = rows(15, T, V, "bf16", sigma=1.0, head=4.0)
+    rng = np.random.default_rng(4)
+    check(x, rng.random(T), top_p=rng.choice([0.9, 1.0, 0.5], T), top_k=rng.choice([0, 0, 40, 1200], T))
 
 
 def test_fewer_rows_than_the_sampler_has():
