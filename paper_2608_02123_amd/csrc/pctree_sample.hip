@@ -34,6 +34,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "pctree_sample.h"
 #include "pctree_tile.h"
 
@@ -53,6 +55,7 @@ constexpr int kManyParts = 2048;      // ... and where k is more than a quarter 
 constexpr int kMaxBound = 1024;       // the largest k that is bounded so
 constexpr int kTry = 256;             // (top_p alone) the rank of the bound that is tried first
 constexpr int kBins = 2048;           // of 1/64 in log weight
+constexpr double kBinStep = 0.98449643700540841;  // e^(-1/64)
 constexpr double kLowest = -700.0;    // weights below e^-700 are 0
 constexpr double kLog2e = 1.4426950408889634074;
 
@@ -76,10 +79,17 @@ __device__ __forceinline__ double exp2_small(double r) {
   s = __builtin_fma(s, r, c1);
   return __builtin_fma(s, r, 1.0);
 }
-// e^z for z in [-700, 0]; 0 below (and for NaN).
+// e^z for z in [-700, 0]; 0 below (and for NaN).  The whole part of the exponent is the
+// low bits of a float64 of step 1, and is added to the result's exponent (2^-1010 is
+// still normal): no conversions, which take four times a product's time.
 __device__ __forceinline__ double weight_of(double z) {
-  const double t = z * kLog2e, n = __builtin_rint(t);
-  const double w = __builtin_ldexp(exp2_small(t - n), (int)n);
+  constexpr double kStep = 0x1.8p52;
+  const double t = z * kLog2e, n = t + kStep;
+  const double p = exp2_small(t - (n - kStep));
+  const uint32_t lo = (uint32_t)__double_as_longlong(n);
+  const uint64_t bits = (uint64_t)__double_as_longlong(p);
+  const double w = __longlong_as_double(
+      (long long)((uint64_t)((uint32_t)(bits >> 32) + (lo << 20)) << 32 | (uint32_t)bits));
   return z >= kLowest ? w : 0.0;
 }
 
@@ -121,15 +131,47 @@ template <int DT>
 struct Raw {
   u32x4 x[DT == PCTREE_F32 ? 2 : 1];
 };
+// (A unit that is not all inside the row is put together from its elements, -inf
+// elsewhere; in a loop, since code that runs once costs its fetch: 0.1 us a line.)
 template <int DT>
 __device__ __forceinline__ Raw<DT> load_raw(const Row& r, int u) {
   Raw<DT> w;
   constexpr int N = DT == PCTREE_F32 ? 2 : 1;
+  const int j0 = u * kUnit;
+  if (j0 >= r.lo && j0 + kUnit <= r.hi) {
 #pragma unroll
-  for (int i = 0; i < N; ++i) w.x[i] = ((const u32x4*)r.base)[(size_t)u * N + i];
+    for (int i = 0; i < N; ++i) w.x[i] = ((const u32x4*)r.base)[(size_t)u * N + i];
+    return w;
+  }
+  constexpr uint32_t low = DT == PCTREE_F32 ? 0xff800000u : (DT == PCTREE_F16 ? 0xfc00fc00u : 0xff80ff80u);
+#pragma unroll
+  for (int i = 0; i < N; ++i) w.x[i] = u32x4{low, low, low, low};
+#pragma unroll 1
+  for (int j = max(j0, r.lo); j < min(j0 + kUnit, r.hi); ++j) {
+    const int e = j - j0;
+#pragma unroll
+    for (int i = 0; i < 4 * N; ++i) {
+      const uint32_t x = w.x[i / 4][i % 4];
+      if constexpr (DT == PCTREE_F32) {
+        w.x[i / 4][i % 4] = i == e ? ((const uint32_t*)r.base)[j] : x;
+      } else {
+        const uint32_t h = ((const uint16_t*)r.base)[j];
+        w.x[i / 4][i % 4] =
+            i == e / 2 ? (e & 1 ? (x & 0xffffu) | h << 16 : (x & 0xffff0000u) | h) : x;
+      }
+    }
+  }
   return w;
 }
-template <int DT>
+// A queue of raws: drops the first, appends one.  (A loop that takes the first each
+// time has one copy of its body; indexing registers would need one each.)
+template <int DT, int N>
+__device__ __forceinline__ void next_raw(Raw<DT> (&w)[N], const Raw<DT>& x) {
+#pragma unroll
+  for (int i = 0; i + 1 < N; ++i) w[i] = w[i + 1];
+  w[N - 1] = x;
+}
+template <int DT, bool MEND = true>
 __device__ __forceinline__ void unpack(const Raw<DT>& w, float (&v)[kUnit]) {
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
@@ -141,42 +183,33 @@ __device__ __forceinline__ void unpack(const Raw<DT>& w, float (&v)[kUnit]) {
       v[2 * e + 1] = hi16<DT == PCTREE_F16>(w.x[0][e]);
     }
   }
+  if constexpr (MEND) {
 #pragma unroll
-  for (int e = 0; e < kUnit; ++e) v[e] = v[e] == v[e] ? v[e] : kNegInf;
+    for (int e = 0; e < kUnit; ++e) v[e] = v[e] == v[e] ? v[e] : kNegInf;
+  }
 }
 template <int DT>
 __device__ __forceinline__ void load_unit(const Row& r, int u, float (&v)[kUnit]) {
-  const int j0 = u * kUnit;
-  if (j0 >= r.lo && j0 + kUnit <= r.hi) {
-    unpack<DT>(load_raw<DT>(r, u), v);
-    return;
-  }
-#pragma unroll
-  for (int e = 0; e < kUnit; ++e) {
-    v[e] = kNegInf;
-    if (j0 + e >= r.lo && j0 + e < r.hi) {
-      if constexpr (DT == PCTREE_F32)
-        v[e] = ((const float*)r.base)[j0 + e];
-      else
-        v[e] = lo16<DT == PCTREE_F16>(((const uint16_t*)r.base)[j0 + e]);
-    }
-    v[e] = v[e] == v[e] ? v[e] : kNegInf;
-  }
+  unpack<DT>(load_raw<DT>(r, u), v);
 }
 // The units u0 + 64 i + lane, i < N, of a wave: all loads before the first use where
 // the wave is inside the row.
 template <int DT, int N>
-__device__ __forceinline__ void load_units(const Row& r, int u0, float (&v)[N][kUnit]) {
+__device__ __forceinline__ void load_raws(const Row& r, int u0, Raw<DT> (&w)[N]) {
   const int lane = threadIdx.x & 63;
   if (u0 * kUnit >= r.lo && (u0 + 64 * N) * kUnit <= r.hi) {
-    Raw<DT> w[N];
+    constexpr int X = DT == PCTREE_F32 ? 2 : 1;
 #pragma unroll
-    for (int i = 0; i < N; ++i) w[i] = load_raw<DT>(r, u0 + 64 * i + lane);
+    for (int i = 0; i < N; ++i)
 #pragma unroll
-    for (int i = 0; i < N; ++i) unpack<DT>(w[i], v[i]);
-  } else {
-#pragma unroll
-    for (int i = 0; i < N; ++i) load_unit<DT>(r, u0 + 64 * i + lane, v[i]);
+      for (int j = 0; j < X; ++j)
+        w[i].x[j] = ((const u32x4*)r.base)[(size_t)(u0 + 64 * i + lane) * X + j];
+    return;
+  }
+#pragma unroll 1
+  for (int i = 0; i < N; ++i) {
+    const Raw<DT> x = load_raw<DT>(r, u0 + 64 * i + lane);
+    next_raw(w, x);
   }
 }
 
@@ -204,41 +237,105 @@ __device__ __forceinline__ bool bounded(const SampleArgs& a, const Params& q) {
   return q.greedy || q.min_p > 0.0 || (q.k > 0 && q.k <= min(a.ng, kMaxBound));
 }
 
-// Sums over the lanes up to each one, and over the wave.
-template <int CTRL, int ROWS>
-__device__ __forceinline__ int dpp_add(int x) {
-  return x + __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xf, false);
+// The value of the lane whose index differs in bit D (row operations and lane swaps:
+// a tenth of the latency of an exchange through LDS).
+template <int D>
+__device__ __forceinline__ uint32_t xor_lane(uint32_t x) {
+  if constexpr (D == 1) return __builtin_amdgcn_mov_dpp((int)x, 0xb1, 0xf, 0xf, true);
+  if constexpr (D == 2) return __builtin_amdgcn_mov_dpp((int)x, 0x4e, 0xf, 0xf, true);
+  if constexpr (D == 4)  // (7 - i in each eight, then 3 - i in each four)
+    return __builtin_amdgcn_mov_dpp(__builtin_amdgcn_mov_dpp((int)x, 0x141, 0xf, 0xf, true), 0x1b,
+                                    0xf, 0xf, true);
+  if constexpr (D == 8) return __builtin_amdgcn_mov_dpp((int)x, 0x128, 0xf, 0xf, true);
+  if constexpr (D == 16) {
+    const auto s = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    return threadIdx.x & 16 ? s[0] : s[1];
+  }
+  const auto s = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+  return threadIdx.x & 32 ? s[0] : s[1];
 }
-__device__ __forceinline__ int wave_upto(int x) {  // (the lane's own among it)
-  x = dpp_add<0x111, 0xf>(x);  // row_shr:1, 2, 4, 8
-  x = dpp_add<0x112, 0xf>(x);
-  x = dpp_add<0x114, 0xf>(x);
-  x = dpp_add<0x118, 0xf>(x);
-  x = dpp_add<0x142, 0xa>(x);  // row_bcast:15 into rows 1 and 3
-  x = dpp_add<0x143, 0xc>(x);  // row_bcast:31 into rows 2 and 3
+template <int D>
+__device__ __forceinline__ uint64_t xor_lane(uint64_t x) {
+  return (uint64_t)xor_lane<D>((uint32_t)(x >> 32)) << 32 | xor_lane<D>((uint32_t)x);
+}
+template <int D>
+__device__ __forceinline__ double xor_lane(double x) {
+  return __longlong_as_double((long long)xor_lane<D>((uint64_t)__double_as_longlong(x)));
+}
+
+// Sums over the lanes up to each one (its own among them), and over the wave: row
+// shifts by 1, 2, 4, 8, then the rows' last lanes into the rows after them.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int dpp_from(int x) {  // (0 where there is no such lane)
+  return __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xf, false);
+}
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double dpp_from(double x) {
+  const long long b = __double_as_longlong(x);
+  const uint32_t hi = (uint32_t)dpp_from<CTRL, ROWS>((int)(b >> 32)), lo = (uint32_t)dpp_from<CTRL, ROWS>((int)b);
+  return __longlong_as_double((long long)((uint64_t)hi << 32 | lo));
+}
+template <typename T>
+__device__ __forceinline__ T wave_upto(T x) {
+  x += dpp_from<0x111, 0xf>(x);
+  x += dpp_from<0x112, 0xf>(x);
+  x += dpp_from<0x114, 0xf>(x);
+  x += dpp_from<0x118, 0xf>(x);
+  x += dpp_from<0x142, 0xa>(x);
+  x += dpp_from<0x143, 0xc>(x);
   return x;
 }
-template <int CTRL, int ROWS>
-__device__ __forceinline__ uint32_t dpp_most(uint32_t x) {
-  return max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, ROWS, 0xf, false));
-}
 __device__ __forceinline__ uint32_t wave_most(uint32_t x) {
-  x = dpp_most<0x111, 0xf>(x);
-  x = dpp_most<0x112, 0xf>(x);
-  x = dpp_most<0x114, 0xf>(x);
-  x = dpp_most<0x118, 0xf>(x);
-  x = dpp_most<0x142, 0xa>(x);
-  x = dpp_most<0x143, 0xc>(x);
-  return (uint32_t)__builtin_amdgcn_readlane((int)x, 63);
+  auto step = [&](uint32_t y) { x = max(x, y); };
+  step(xor_lane<1>(x));
+  step(xor_lane<2>(x));
+  step(xor_lane<4>(x));
+  step(xor_lane<8>(x));
+  step(xor_lane<16>(x));
+  step(xor_lane<32>(x));
+  return (uint32_t)__builtin_amdgcn_readfirstlane((int)x);
 }
 __device__ __forceinline__ int wave_count(int x) {
   return __builtin_amdgcn_readlane(wave_upto(x), 63);
 }
-
+__device__ __forceinline__ uint64_t lane_of(uint64_t x, int lane) {
+  return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(x >> 32), lane) << 32 |
+         (uint32_t)__builtin_amdgcn_readlane((int)x, lane);
+}
+__device__ __forceinline__ double lane_of(double x, int lane) {
+  return __longlong_as_double((long long)lane_of((uint64_t)__double_as_longlong(x), lane));
+}
 __device__ __forceinline__ double wave_sum(double v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+  v += xor_lane<32>(v);
+  v += xor_lane<16>(v);
+  v += xor_lane<8>(v);
+  v += xor_lane<4>(v);
+  v += xor_lane<2>(v);
+  v += xor_lane<1>(v);
   return v;
+}
+
+// The sums of N values over the wave, N a power of two: lane l gets that of value l /
+// (64 / N).  Halves of the values go to the lanes' halves first.
+template <int N, int D = 32>
+__device__ __forceinline__ double wave_sums(double (&v)[N]) {
+  if constexpr (N == 1) {
+    double x = v[0];
+    if constexpr (D >= 32) x += xor_lane<32>(x);
+    if constexpr (D >= 16) x += xor_lane<16>(x);
+    if constexpr (D >= 8) x += xor_lane<8>(x);
+    if constexpr (D >= 4) x += xor_lane<4>(x);
+    if constexpr (D >= 2) x += xor_lane<2>(x);
+    if constexpr (D >= 1) x += xor_lane<1>(x);
+    return x;
+  } else {
+    double h[N / 2];
+    const bool upper = threadIdx.x & D;
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i)
+      h[i] = (upper ? v[i + N / 2] : v[i]) + xor_lane<D>(upper ? v[i] : v[i + N / 2]);
+    return wave_sums<N / 2, D / 2>(h);
+  }
 }
 
 template <int DT, int BPW>
@@ -248,34 +345,53 @@ __global__ __launch_bounds__(kScanThreads) void scan_kernel(SampleArgs a, int se
   const int b0 = (seg * (kScanThreads / 64) + threadIdx.x / 64) * BPW;
   if (b0 >= a.nb) return;
   const Row row = row_of<DT>(a, t);
-  float v[BPW][kUnit], mx[BPW];
-  load_units<DT, BPW>(row, b0 * 64, v);
-  const int lanes = 1 << a.gshift;  // of a group
+  Raw<DT> raw[BPW];
+  load_raws<DT, BPW>(row, b0 * 64, raw);
+  const Params q = params_of(a, t);
+  const int s = a.gshift;  // a group is the units of 1 << s lanes
   float all = kNegInf;
 #pragma unroll
   for (int i = 0; i < BPW; ++i) {
-    mx[i] = v[i][0];
+    float v[kUnit];
+    unpack<DT, false>(raw[i], v);  // (a maximum passes over NaN by itself)
+    float m = v[0];
 #pragma unroll
-    for (int e = 1; e < kUnit; ++e) mx[i] = fmaxf(mx[i], v[i][e]);
-    all = fmaxf(all, mx[i]);
-    for (int o = 1; o < lanes; o <<= 1) mx[i] = fmaxf(mx[i], __shfl_xor(mx[i], o, 64));
-    const int g = ((b0 + i) * 64 + lane) / lanes;
-    if (lane % lanes == 0 && g < a.ng) a.gmax[(size_t)t * a.ng + g] = mx[i];
+    for (int e = 1; e < kUnit; ++e) m = fmaxf(m, v[e]);
+    m = m == m ? m : kNegInf;
+    auto join = [&](uint32_t o) { m = fmaxf(m, __uint_as_float(o)); };
+    if (s >= 1) join(xor_lane<1>(__float_as_uint(m)));
+    if (s >= 2) join(xor_lane<2>(__float_as_uint(m)));
+    if (s >= 3) join(xor_lane<4>(__float_as_uint(m)));
+    if (s >= 4) join(xor_lane<8>(__float_as_uint(m)));
+    if (s >= 5) join(xor_lane<16>(__float_as_uint(m)));
+    if (s >= 6) join(xor_lane<32>(__float_as_uint(m)));
+    all = fmaxf(all, m);
+    const int g = ((b0 + i) * 64 + lane) >> s;
+    if ((lane & ((1 << s) - 1)) == 0 && g < a.ng) a.gmax[(size_t)t * a.ng + g] = m;
   }
-  const Params q = params_of(a, t);
   if (bounded(a, q)) return;
   const float ref = of_ord(wave_most(ord_of(all)));
-#pragma unroll
+  double sums[BPW];
+#pragma unroll 1
   for (int i = 0; i < BPW; ++i) {
-    double s = 0.0;
+    float v[kUnit];
+    unpack<DT, false>(raw[0], v);
+    next_raw(raw, raw[0]);
+    double sum = 0.0;
 #pragma unroll
-    for (int e = 0; e < kUnit; ++e)
-      s += v[i][e] == ref ? 1.0 : weight_of(((double)v[i][e] - (double)ref) * q.inv_t);
-    s = wave_sum(s);
-    if (lane == 0 && b0 + i < a.nb) {
-      a.bmass[(size_t)t * a.nb + b0 + i] = ref == kNegInf ? 0.0 : s;
-      a.bref[(size_t)t * a.nb + b0 + i] = ref;
+    for (int e = 0; e < kUnit; ++e) {
+      const double w = weight_of(((double)v[e] - (double)ref) * q.inv_t);  // (NaN: 0)
+      sum += v[e] == ref ? 1.0 : w;
     }
+#pragma unroll
+    for (int j = 0; j + 1 < BPW; ++j) sums[j] = sums[j + 1];
+    sums[BPW - 1] = sum;
+  }
+  const double sum = wave_sums<BPW>(sums);
+  const int b = b0 + lane / (64 / BPW);
+  if (lane % (64 / BPW) == 0 && b < a.nb) {
+    a.bmass[(size_t)t * a.nb + b] = ref == kNegInf ? 0.0 : sum;
+    a.bref[(size_t)t * a.nb + b] = ref;
   }
 }
 
@@ -301,6 +417,7 @@ struct PickShared {
   uint16_t group[kMaxGroups + 3];
   double part[kPickWaves];
   int parti[kPickWaves];
+  int counts[3][kPickWaves];
   int n, groups, found, extra;
   uint32_t lo, hi;
 };
@@ -316,8 +433,7 @@ __device__ __forceinline__ double block_sum(double v, PickShared& sh) {
   return s;
 }
 __device__ __forceinline__ int block_sum(int v, PickShared& sh) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+  v = wave_count(v);
   __syncthreads();
   if ((threadIdx.x & 63) == 0) sh.parti[threadIdx.x >> 6] = v;
   __syncthreads();
@@ -329,83 +445,87 @@ __device__ __forceinline__ int block_sum(int v, PickShared& sh) {
 // Sum over the threads before this one (always added in the same order).
 __device__ __forceinline__ double block_before(double v, PickShared& sh) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  double x = v;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const double y = __shfl_up(x, o, 64);
-    if (lane >= o) x += y;
-  }
+  const double x = wave_upto(v);
   __syncthreads();
   if (lane == 63) sh.part[wave] = x;
   __syncthreads();
-  double b = __shfl_up(x, 1, 64);
-  if (lane == 0) b = 0.0;
-  double base = 0.0;
-  for (int w = 0; w < wave; ++w) base += sh.part[w];
-  return base + b;
+  // (the lane before: wave_shr:1)
+  double base = dpp_from<0x138, 0xf>(x);
+#pragma unroll
+  for (int w = 0; w < kPickWaves; ++w) base += w < wave ? sh.part[w] : 0.0;
+  return base;
 }
 __device__ __forceinline__ int block_before(int v, PickShared& sh) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  int x = v;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int y = __shfl_up(x, o, 64);
-    if (lane >= o) x += y;
-  }
+  const int x = wave_upto(v);
   __syncthreads();
   if (lane == 63) sh.parti[wave] = x;
   __syncthreads();
   int base = x - v;
-  for (int w = 0; w < wave; ++w) base += sh.parti[w];
+#pragma unroll
+  for (int w = 0; w < kPickWaves; ++w) base += w < wave ? sh.parti[w] : 0;
   return base;
 }
 
 // A lower bound of the row's j-th largest logit, j <= min(groups, kMaxBound): the j-th
 // largest of the maxima of parts of the row, its order's low 12 bits rounded down.
 // With P parts and logits in any order about P log(P / (P - j)) logits reach it: 52 of
-// 512 parts for j = 50, 450 of 2048 for j = 400 (777 with 512).  Each wave searches by
-// itself, P / 64 maxima to a lane.
+// 512 parts for j = 50, 450 of 2048 for j = 400 (777 with 512).  The search is by bits,
+// from the first in which the largest and the smallest maximum differ: 512 parts by
+// each wave for itself, 8 to a lane; 2048 by the workgroup, 4 to a thread.
 template <int P>
-__device__ __forceinline__ float rank_bound(const SampleArgs& a, int j, const PickShared& sh) {
-  const int lane = threadIdx.x & 63;
-  uint32_t o[P / 64];
+__device__ __forceinline__ float rank_bound(const SampleArgs& a, int j, float mx, PickShared& sh) {
+  constexpr bool ALONE = P == kParts;
+  constexpr int N = ALONE ? P / 64 : P / kPickThreads, STEP = ALONE ? 64 : kPickThreads;
+  const int at = ALONE ? threadIdx.x & 63 : threadIdx.x;
+  uint32_t o[N];
 #pragma unroll
-  for (int i = 0; i < P / 64; ++i) {
+  for (int i = 0; i < N; ++i) {
     float m = kNegInf;
-    for (int g = i * 64 + lane; g < a.ng; g += P) m = fmaxf(m, sh.gmax[g]);
+    for (int g = i * STEP + at; g < a.ng; g += P) m = fmaxf(m, sh.gmax[g]);
     o[i] = ord_of(m);
   }
-  // (from the first bit in which the largest and the smallest differ)
-  uint32_t least = o[0], most = o[0];
+  uint32_t least = o[0];
 #pragma unroll
-  for (int i = 1; i < P / 64; ++i) {
-    least = min(least, o[i]);
-    most = max(most, o[i]);
-  }
+  for (int i = 1; i < N; ++i) least = min(least, o[i]);
   least = ~wave_most(~least);
-  most = wave_most(most);
+  if constexpr (!ALONE) {
+    if ((threadIdx.x & 63) == 0) sh.counts[0][threadIdx.x >> 6] = (int)least;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kPickWaves; ++w) least = min(least, (uint32_t)sh.counts[0][w]);
+  }
+  const uint32_t most = ord_of(mx);
   const int top = least == most ? 11 : 31 - __builtin_clz(least ^ most);
   uint32_t lo = most & ~((2u << top) - 1);  // at least j maxima are >= lo
   for (int bit = top; bit >= 12; --bit) {
     const uint32_t mid = lo | (1u << bit);
     int c = 0;
 #pragma unroll
-    for (int i = 0; i < P / 64; ++i) c += o[i] >= mid;
+    for (int i = 0; i < N; ++i) c += o[i] >= mid;
     c = wave_count(c);
+    if constexpr (!ALONE) {  // (two places in turn: one barrier a step)
+      int* counts = sh.counts[1 + (bit & 1)];
+      if ((threadIdx.x & 63) == 0) counts[threadIdx.x >> 6] = c;
+      __syncthreads();
+      c = 0;
+#pragma unroll
+      for (int w = 0; w < kPickWaves; ++w) c += counts[w];
+    }
     if (c >= j) lo = mid;
     if (c >= j && c <= j + j / 8 + 2) break;  // (close enough)
   }
   return lo < 0x00800000u ? kNegInf : of_ord(lo);
 }
-__device__ __forceinline__ float bound_of(const SampleArgs& a, int j, const PickShared& sh) {
-  return j <= kParts / 4 ? rank_bound<kParts>(a, j, sh) : rank_bound<kManyParts>(a, j, sh);
+__device__ __forceinline__ float bound_of(const SampleArgs& a, int j, float mx, PickShared& sh) {
+  return j <= kParts / 4 ? rank_bound<kParts>(a, j, mx, sh) : rank_bound<kManyParts>(a, j, mx, sh);
 }
 
 // Logits >= bound into the list (unordered), as (order, lowest index first);
 // returns how many there are (more than kList: not all are in the list).
 template <int DT>
 __device__ int gather(const SampleArgs& a, const Row& row, float bound, PickShared& sh) {
-  constexpr int B = 4;  // groups whose loads are in flight together
+  constexpr int B = 4;  // units whose loads are in flight together
   if (threadIdx.x == 0) sh.n = sh.groups = 0;
   __syncthreads();
   {
@@ -428,31 +548,32 @@ __device__ int gather(const SampleArgs& a, const Row& row, float bound, PickShar
   const int per = 1 << a.gshift, units = sh.groups << a.gshift;
   for (int i1 = 0; i1 < units; i1 += B * kPickThreads) {
     const int i0 = i1 + threadIdx.x;
-    float v[B][kUnit];
-    int u[B];
-#pragma unroll
-    for (int k = 0; k < B; ++k) {
+    Raw<DT> raw[B];
+    auto unit = [&](int k) {  // (past the end: a unit outside the row)
       const int i = i0 + k * kPickThreads;
-      // (past the end: a unit outside the row)
-      u[k] = i < units ? sh.group[i >> a.gshift] * per + (i & (per - 1)) : row.hi / kUnit + 1;
-      load_unit<DT>(row, u[k], v[k]);
-    }
+      return i < units ? sh.group[i >> a.gshift] * per + (i & (per - 1)) : row.hi / kUnit + 1;
+    };
 #pragma unroll
+    for (int k = 0; k < B; ++k) raw[k] = load_raw<DT>(row, unit(k));
+#pragma unroll 1
     for (int k = 0; k < B; ++k) {
+      float v[kUnit];
+      unpack<DT>(raw[0], v);
+      next_raw(raw, raw[0]);
       uint32_t hits = 0;
 #pragma unroll
       for (int e = 0; e < kUnit; ++e)
-        hits |= v[k][e] >= bound && v[k][e] != kNegInf ? 1u << e : 0u;
+        hits |= v[e] >= bound && v[e] != kNegInf ? 1u << e : 0u;
       if (!__any(hits)) continue;
       // the lane's place: one atomic for the wave
-      const int c = __builtin_popcount(hits), upto = wave_upto(c);
+      const int c = __builtin_popcount(hits), upto = wave_upto(c), u = unit(k);
       int at = 0;
       if ((threadIdx.x & 63) == 63) at = atomicAdd(&sh.n, upto);
       at = __builtin_amdgcn_readlane(at, 63) + upto - c;
 #pragma unroll
       for (int e = 0; e < kUnit; ++e)
         if (hits >> e & 1) {
-          if (at < kList) sh.l.list[at] = key_of(v[k][e], u[k] * kUnit + e - row.lo);
+          if (at < kList) sh.l.list[at] = key_of(v[e], u * kUnit + e - row.lo);
           ++at;
         }
     }
@@ -506,12 +627,19 @@ __device__ void sort_network(uint64_t* list, int n) {
 #pragma unroll
       for (int e = 0; e < E; ++e) keep(e, list[e * kPickThreads + (tid ^ d)], d, size);
     }
-#pragma unroll 1
-    for (int d = min(size, 64) >> 1; d > 0; d >>= 1) {
+    auto lanes = [&](auto dist) {
+      constexpr int d = decltype(dist)::value;
+      if (d < size) {
 #pragma unroll
-      for (int e = 0; e < E; ++e)
-        keep(e, (uint64_t)__shfl_xor((unsigned long long)r[e], d, 64), d, size);
-    }
+        for (int e = 0; e < E; ++e) keep(e, xor_lane<d>(r[e]), d, size);
+      }
+    };
+    lanes(std::integral_constant<int, 32>());
+    lanes(std::integral_constant<int, 16>());
+    lanes(std::integral_constant<int, 8>());
+    lanes(std::integral_constant<int, 4>());
+    lanes(std::integral_constant<int, 2>());
+    lanes(std::integral_constant<int, 1>());
   }
   __syncthreads();
 #pragma unroll
@@ -882,13 +1010,16 @@ __device__ __noinline__ void whole_row(const SampleArgs& a, int t, const Row& ro
       double m = base + block_before(s, sh);
       if (threadIdx.x == 0) sh.found = kBins;
       __syncthreads();
+      uint32_t first = 0;  // the complement of the thread's first such bin
 #pragma unroll
       for (int i = 0; i < PER; ++i) {
         const int b = threadIdx.x * PER + i;
         m += mass[i];
-        if (m >= limit && sh.h.count[b] > 0) atomicMin(&sh.found, b);
+        if (m >= limit && sh.h.count[b] > 0) first = max(first, ~(uint32_t)b);
         sh.h.mass[b] = (unsigned long long)__double_as_longlong(m);
       }
+      first = wave_most(first);
+      if ((threadIdx.x & 63) == 0 && first) atomicMin(&sh.found, (int)~first);
       __syncthreads();
       const int b = sh.found;
       const double all = __longlong_as_double((long long)sh.h.mass[kBins - 1]);
@@ -916,8 +1047,14 @@ __device__ __noinline__ void whole_row(const SampleArgs& a, int t, const Row& ro
         if (threadIdx.x == 0) sh.n = 0;
         __syncthreads();
         each_logit<DT>(row, [&](float v, int i) {
-          if (bin_of(v) != b || !kept(v, weight(v, mx, q.inv_t))) return;
-          const int at = atomicAdd(&sh.n, 1);
+          const bool in = bin_of(v) == b && kept(v, weight(v, mx, q.inv_t));
+          const uint64_t all_in = __ballot(in);
+          if (!in) return;
+          // (the first of them takes the places)
+          const int lane = threadIdx.x & 63, lead = (int)__builtin_ctzll(all_in);
+          int at = 0;
+          if (lane == lead) at = atomicAdd(&sh.n, __builtin_popcountll(all_in));
+          at = __builtin_amdgcn_readlane(at, lead) + __builtin_popcountll(all_in & ((1ull << lane) - 1));
           if (at < kList) sh.l.list[at] = key_of(v, i);
         });
         __syncthreads();
@@ -938,8 +1075,12 @@ __device__ __noinline__ void whole_row(const SampleArgs& a, int t, const Row& ro
           lo = min(lo, ord_of(v));
           hi = max(hi, ord_of(v));
         });
-        atomicMin(&sh.lo, lo);
-        atomicMax(&sh.hi, hi);
+        lo = ~wave_most(~lo);
+        hi = wave_most(hi);
+        if ((threadIdx.x & 63) == 0) {
+          atomicMin(&sh.lo, lo);
+          atomicMax(&sh.hi, hi);
+        }
       }
       __syncthreads();
       const uint32_t lo = sh.lo, hi = sh.hi;
@@ -1013,11 +1154,6 @@ __device__ void pick_largest(const SampleArgs& a, int t, const Row& row, float m
   }
 }
 
-__device__ __forceinline__ uint64_t lane_of(uint64_t x, int lane) {
-  return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(x >> 32), lane) << 32 |
-         (uint32_t)__builtin_amdgcn_readlane((int)x, lane);
-}
-
 // The rest of a row whose list has at most 64 logits: filters (total: of all weights,
 // where the list is only part of them; 0: the list's) and draw.  Wave w compares with
 // the logits 8 w .. 8 w + 7, and wave 0 joins the parts.  Returns whether the list was
@@ -1044,27 +1180,21 @@ __device__ bool pick_of_64(const SampleArgs& a, int t, const Params& q, float mx
   const double w = in ? weight(v, mx, q.inv_t) : 0.0;
   int m = q.min_p > 0.0 ? max(__builtin_popcountll(__ballot(in && w >= q.min_p)), 1) : n;
   if (q.k > 0) m = min(m, q.k);
-  double run = lane < m ? w : 0.0;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const double y = __shfl_up(run, o, 64);
-    if (lane >= o) run += y;
-  }
+  const double run = wave_upto(lane < m ? w : 0.0);
   if (q.p < 1.0) {
-    const double sum = __shfl(run, m - 1, 64), limit = q.p * (total > 0.0 ? total : sum);
+    const double sum = lane_of(run, m - 1), limit = q.p * (total > 0.0 ? total : sum);
     if (total > 0.0 && sum < limit) return false;
-    double before = __shfl_up(run, 1, 64);
-    if (lane == 0) before = 0.0;
+    const double before = dpp_from<0x138, 0xf>(run);
     m = max(__builtin_popcountll(__ballot(lane < m && before < limit)), 1);
   }
-  const double all = __shfl(run, m - 1, 64), target = q.u * all;
+  const double all = lane_of(run, m - 1), target = q.u * all;
   // the kept weights up to the lane's logit, by index (added in the list's order)
   const int at = index_of(key);
   double part = 0.0;
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
     const int i = wave * 8 + j;
-    const double wj = __longlong_as_double((long long)lane_of((uint64_t)__double_as_longlong(w), i));
+    const double wj = lane_of(w, i);
     part += i < m && __builtin_amdgcn_readlane(at, i) <= at ? wj : 0.0;
   }
   sh.l.w[512 + wave * 64 + lane] = part;
@@ -1129,7 +1259,7 @@ __global__ __launch_bounds__(kPickThreads) __attribute__((amdgpu_waves_per_eu(4)
     float bound = kNegInf;
     double total = 0.0;  // of all weights, where top_p is the only filter
     if (bnd) {
-      if (q.k > 0 && q.k <= min(a.ng, kMaxBound)) bound = bound_of(a, q.k, sh);
+      if (q.k > 0 && q.k <= min(a.ng, kMaxBound)) bound = bound_of(a, q.k, mx, sh);
       if (q.min_p > 0.0) {
         // a little below the logit of weight min_p
         const double v = (double)mx + log(q.min_p) / q.inv_t;
@@ -1142,7 +1272,7 @@ __global__ __launch_bounds__(kPickThreads) __attribute__((amdgpu_waves_per_eu(4)
         s += ref == kNegInf ? 0.0 : a.bmass[(size_t)t * a.nb + b] * weight(ref, mx, q.inv_t);
       }
       total = block_sum(s, sh);
-      bound = bound_of(a, min(a.ng, kTry), sh);
+      bound = bound_of(a, min(a.ng, kTry), mx, sh);
     }
     const bool list = bnd || all_in || q.k == 0;  // (else a top_k beyond the bounds)
     const int n = list ? gather<DT>(a, row, bound, sh) : kList + 1;
@@ -1222,7 +1352,6 @@ __global__ __launch_bounds__(kScanThreads) void hist_kernel(SampleArgs a, int se
   if (a.open[t].state != 1) return;
   __shared__ unsigned long long mass[kBins];
   for (int i = threadIdx.x; i < kBins; i += kScanThreads) mass[i] = 0;
-  __syncthreads();
   const Row row = row_of<DT>(a, t);
   const Params q = params_of(a, t);
   if (q.p >= 1.0) return;
@@ -1233,16 +1362,20 @@ __global__ __launch_bounds__(kScanThreads) void hist_kernel(SampleArgs a, int se
   const double floor = fmax(kLowest, lnp - 1e-9);
   const double floor_sure = q.min_p > 0.0 ? lnp + 1e-9 : kLowest;
   const int b0 = (seg * (kScanThreads / 64) + threadIdx.x / 64) * BPW;
-  float u[BPW][kUnit];
-  load_units<DT, BPW>(row, b0 * 64, u);
-#pragma unroll
+  Raw<DT> raw[BPW];
+  load_raws<DT, BPW>(row, b0 * 64, raw);
+  __syncthreads();
+#pragma unroll 1
   for (int i = 0; i < BPW; ++i) {
+    float u[kUnit];
+    unpack<DT>(raw[0], u);
+    next_raw(raw, raw[0]);
     int bin[kUnit];
     double w[kUnit];
     bool in[kUnit], rest = false;
 #pragma unroll
     for (int e = 0; e < kUnit; ++e) {
-      const double z = u[i][e] == mx ? 0.0 : z_of(u[i][e], mx, q.inv_t);
+      const double z = u[e] == mx ? 0.0 : z_of(u[e], mx, q.inv_t);
       in[e] = z >= floor;
       bin[e] = open_bin(z);
       rest |= in[e] && (bin[e] == kBins - 1 || z < floor_sure);
@@ -1260,9 +1393,9 @@ __global__ __launch_bounds__(kScanThreads) void hist_kernel(SampleArgs a, int se
     if (__any(rest)) {  // the last bin, and weights next to min_p
 #pragma unroll 1
       for (int e = 0; e < kUnit; ++e) {
-        float v = u[i][0];
+        float v = u[0];
 #pragma unroll
-        for (int j = 1; j < kUnit; ++j) v = e == j ? u[i][j] : v;
+        for (int j = 1; j < kUnit; ++j) v = e == j ? u[j] : v;
         const double z = v == mx ? 0.0 : z_of(v, mx, q.inv_t);
         const bool ok = z >= floor && weight(v, mx, q.inv_t) >= q.min_p;
         const double far = weight_of(fmin(z + (kBins - 1) / 64.0, 0.0));
@@ -1300,21 +1433,27 @@ __global__ __launch_bounds__(kScanThreads) void mark_kernel(SampleArgs a, int se
   const Params q = params_of(a, t);
   const float mx = a.open[t].mx;
   const double floor = kLowest;
+  const int b0 = (seg * W + wave) * BPW;
+  Raw<DT> raw[BPW];
+  load_raws<DT, BPW>(row, b0 * 64, raw);
   // the border bin: every workgroup finds the same (without a top_p there is none)
+  unsigned long long f[PER];
+#pragma unroll
+  for (int i = 0; i < PER; ++i) f[i] = a.hist[(size_t)t * kBins + threadIdx.x * PER + i];
   double m[PER], s = 0.0;
 #pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    const int b = threadIdx.x * PER + i;
-    const unsigned long long f = q.p < 1.0 ? a.hist[(size_t)t * kBins + b] : 0;
-    m[i] = f ? (double)f * 0x1p-42 * weight_of(b * (-1.0 / 64.0)) : 0.0;
-    s += m[i];
-  }
-  double x = s;
+  for (int i = 0; i < PER; ++i) m[i] = (double)(q.p < 1.0 ? f[i] : 0) * 0x1p-42;
+  {
+    // (the bins' top weights: the first one's, then e^-1/64 apart)
+    double w = weight_of(threadIdx.x * (-PER / 64.0));
 #pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const double y = __shfl_up(x, o, 64);
-    if (lane >= o) x += y;
+    for (int i = 0; i < PER; ++i) {
+      m[i] *= w;
+      w *= kBinStep;
+      s += m[i];
+    }
   }
+  const double x = wave_upto(s);
   if (lane == 63) part[wave] = x;
   if (threadIdx.x == 0) {
     found = kBins;
@@ -1328,13 +1467,19 @@ __global__ __launch_bounds__(kScanThreads) void mark_kernel(SampleArgs a, int se
     all += part[w];
   }
   const double limit = q.p * all;
+  // (the wave's first bin before the one atomic: 64 lanes' atomics on one word take
+  // 2 us)
+  uint32_t first = 0;  // its complement
 #pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    const int b = threadIdx.x * PER + i;
-    run += m[i];
-    running[b] = run;
-    if (m[i] > 0.0 && run >= limit) atomicMin(&found, b);
+  for (int i = PER - 1; i >= 0; --i) {
+    double r = run;
+#pragma unroll
+    for (int j = 0; j <= i; ++j) r += m[j];
+    running[threadIdx.x * PER + i] = r;
+    if (m[i] > 0.0 && r >= limit) first = ~(uint32_t)(threadIdx.x * PER + i);
   }
+  first = wave_most(first);
+  if (lane == 0 && first) atomicMin(&found, (int)~first);
   __syncthreads();
   const int border = found;
   if (seg == 0 && threadIdx.x == 0) {
@@ -1343,18 +1488,18 @@ __global__ __launch_bounds__(kScanThreads) void mark_kernel(SampleArgs a, int se
     a.open[t].base = border > 0 && border < kBins ? running[border - 1] : 0.0;
   }
   if (border == kBins && q.p < 1.0) return;  // (rounding at the end: the row is done alone)
-  const int b0 = (seg * W + wave) * BPW;
-  float u[BPW][kUnit];
-  load_units<DT, BPW>(row, b0 * 64, u);
-#pragma unroll
+#pragma unroll 1
   for (int i = 0; i < BPW; ++i) {
     if (b0 + i >= a.nb) break;
+    float u[kUnit];
+    unpack<DT>(raw[0], u);
+    next_raw(raw, raw[0]);
     double sum = 0.0;
     uint32_t listed = 0;
 #pragma unroll
     for (int e = 0; e < kUnit; ++e) {
-      const double z = u[i][e] == mx ? 0.0 : z_of(u[i][e], mx, q.inv_t);
-      const double w = u[i][e] == mx ? 1.0 : weight_of(z);
+      const double z = u[e] == mx ? 0.0 : z_of(u[e], mx, q.inv_t);
+      const double w = u[e] == mx ? 1.0 : weight_of(z);
       const int b = open_bin(z);
       const bool in = z >= floor && w >= q.min_p;
       sum += in && b < border ? w : 0.0;
@@ -1368,7 +1513,7 @@ __global__ __launch_bounds__(kScanThreads) void mark_kernel(SampleArgs a, int se
 #pragma unroll
       for (int e = 0; e < kUnit; ++e)
         if (listed >> e & 1) {
-          if (at < kList) mine[at] = key_of(u[i][e], ((b0 + i) * 64 + lane) * kUnit + e - row.lo);
+          if (at < kList) mine[at] = key_of(u[e], ((b0 + i) * 64 + lane) * kUnit + e - row.lo);
           ++at;
         }
     }
