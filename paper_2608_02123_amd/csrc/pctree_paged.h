@@ -74,10 +74,14 @@ struct AppendArgs {
 hipError_t launch_append(const AppendArgs& a, int D, bool f16, hipStream_t stream);
 
 // Work split of one attention call, a pure function of sizes and the CU count.
+// Requests of at most `few` rows (row count times query heads per key/value head) go
+// to a kernel of their own (pctree_paged_attention.hip).
 struct PagedPlan {
-  int qblocks;      // row blocks per (request, kv head), for max_rows rows
-  int nsplit;       // most slot runs of a request (1: no merge pass)
-  long long blocks; // workgroups (XCD-grouped, padded)
+  int qblocks, few_qblocks;        // row blocks of a (request, kv head) at most
+  int nsplit, few_nsplit;          // most slot runs of a request (1: no merge pass)
+  long long blocks, few_blocks;    // workgroups (XCD-grouped, padded; 0: not launched)
+  int few, few_stride;             // the most rows of such a request
+  size_t parts, few_parts;         // rows of partial results
   size_t ws_bytes;
 };
 
@@ -89,16 +93,19 @@ struct PagedAttnArgs {
   const uint32_t* mask;  // [R][N][NW] or null: causal
   uint16_t* out;         // [T][Hq][D]
   float* part_o;         // [nsplit][T][Hq][D]
-  float* part_ml;        // [nsplit][T][Hq][2]
+  float* part_ml;        // [nsplit][T][Hq][2]: (max of q.k, sum of weights)
+  float* few_o;          // [few_nsplit][R][Hkv][few_stride][D]
+  float* few_ml;         // [few_nsplit][R][Hkv][few_stride][2]
   int Hq, Hkv, g, N, NW;
-  int qblocks, nsplit;
+  int qblocks, nsplit, few_qblocks, few_nsplit, few, few_stride;
   float scale_log2;
 };
 
 PagedPlan plan_paged_attention(int R, int T, int max_rows, int Hq, int Hkv, int D, int C, int cus);
 
-hipError_t launch_paged_attention(const PagedAttnArgs& a, const PagedPlan& plan, int D, bool f16,
-                                  hipStream_t stream);
+// (fills in what the plan and the workspace say)
+hipError_t launch_paged_attention(PagedAttnArgs a, const PagedPlan& plan, int D, bool f16,
+                                  void* workspace, hipStream_t stream);
 
 struct CompactPagedArgs {
   char* pool;

@@ -76,7 +76,7 @@ pctree_status check_attention(const pctree_paged_cache* c, const pctree_paged_ba
   if ((int64_t)b->rows * q_heads > INT32_MAX / 2) return PCTREE_ERR_UNSUPPORTED;
   *plan = plan_paged_attention(b->requests, b->rows, b->max_rows, q_heads, c->kv_heads,
                                c->head_dim, b->max_pages * c->page_size, kPlanCUs);
-  if (plan->blocks > INT32_MAX) return PCTREE_ERR_UNSUPPORTED;
+  if (plan->blocks > INT32_MAX || plan->few_blocks > INT32_MAX) return PCTREE_ERR_UNSUPPORTED;
   return PCTREE_OK;
 }
 
@@ -191,16 +191,10 @@ pctree_status pctree_paged_attention(const pctree_paged_cache* cache,
     a.g = q_heads / cache->kv_heads;
     a.N = mask ? budget : 0;
     a.NW = (a.N + 31) / 32;
-    a.qblocks = plan.qblocks;
-    a.nsplit = plan.nsplit;
     a.scale_log2 = scale * 1.4426950408889634f;
-    a.part_o = plan.nsplit > 1 ? (float*)workspace : nullptr;
-    a.part_ml = plan.nsplit > 1 ? (float*)workspace + (size_t)plan.nsplit * a.b.T * a.Hq *
-                                                          cache->head_dim
-                                : nullptr;
     (void)hipGetLastError();
-    const hipError_t e = launch_paged_attention(a, plan, cache->head_dim,
-                                                cache->dtype == PCTREE_F16, (hipStream_t)stream);
+    const hipError_t e = launch_paged_attention(
+        a, plan, cache->head_dim, cache->dtype == PCTREE_F16, workspace, (hipStream_t)stream);
     return e == hipSuccess ? PCTREE_OK : PCTREE_ERR_HIP;
   } catch (...) {
     return PCTREE_ERR_HIP;

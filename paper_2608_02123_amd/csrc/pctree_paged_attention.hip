@@ -7,15 +7,24 @@
 // key/value head are rows of one matrix, row rho = i * g + (h mod g) of request
 // row i, so that K and V are read once for all of them.
 //
-// One workgroup takes 128 such rows and a run of slots.  K and V of a 64-slot
-// chunk go from their pages straight into LDS, one chunk ahead; every lane holds
-// the page of one slot of the chunk, read another chunk ahead, and the lanes
-// that load a slot's row fetch its page from that lane.  A wave computes
-// S^T = K Q^T and O^T += V^T P^T on MFMA 16x16x32 for its 32 rows, with an online
-// softmax in base 2 (32-bit maximum, sum and output); the two K tiles of a pair
-// are arranged so that a lane ends with 8 consecutive slots of its row, the B
-// operand of the second product.  The weights are rounded to 16 bits there, an
-// operand of the matrix units; their sum is not.
+// Two kernels, by a request's rows (row count times g):
+//
+// * More than kFewRows: a workgroup takes 128 rows and a run of slots.  K and V of a
+//   64-slot chunk go from their pages straight into LDS, one chunk ahead; every lane
+//   holds the page of one slot of the chunk, read another chunk ahead, and the lanes
+//   that load a slot's row fetch its page from that lane.  A wave computes S^T = K Q^T
+//   and O^T += V^T P^T on MFMA 16x16x32 for its 32 rows, with an online softmax in base
+//   2 (32-bit maximum, sum and output); the two K tiles of a pair are arranged so that
+//   a lane ends with 8 consecutive slots of its row, the B operand of the second
+//   product.  The weights are rounded to 16 bits there, an operand of the matrix units;
+//   their sum is not.
+// * Others (single tokens): bytes bound them.  A workgroup takes 16 rows and a run of
+//   slots; each of its waves takes 32-slot chunks by itself, K straight into
+//   registers, V into an LDS tile of its own, and 16 waves a compute unit keep 16 KB
+//   each in flight.  The waves' results are joined in LDS.
+//
+// Runs leave (maximum, sum, unnormalised output) per row for a merging kernel; a
+// request short enough for one run is written at once.
 //
 // Masked slots: scores are replaced, not added to, so K may hold anything.  A
 // weight of zero times an infinite or NaN value would still be NaN, so in chunks
@@ -40,6 +49,9 @@ constexpr int kColTiles = 2;
 constexpr int kRowsPerWave = 16 * kColTiles;
 constexpr int kRowsPerBlock = kWaves * kRowsPerWave;
 constexpr int kMaxSplits = 32;
+constexpr int kFewRows = 64;         // rows (times g) of a request that go 16 to a workgroup
+constexpr int kFewChunk = 32;        // slots of a wave's step there
+constexpr int kFewRun = 4 * kFewChunk;  // the shortest run there, a chunk to each wave
 constexpr int kMergeThreads = 256;
 constexpr int kMergeBatch = 8;
 // float16 weights are 2^12 times the softmax's (as is their sum): weights down
@@ -47,11 +59,15 @@ constexpr int kMergeBatch = 8;
 // the largest is 4096.
 constexpr float kHalfLift = 12.0f;
 
-// Slots per run of a request whose rows end at slot `end`.
-__device__ __forceinline__ int run_slots(int end, int nsplit) {
-  const int chunks = (end + kChunk - 1) / kChunk;
-  const int ns = min(nsplit, max(1, chunks / 2));
-  return (chunks + ns - 1) / ns * kChunk;
+// Slots per run of a request whose rows end at slot `end`, at most `nsplit` runs of at
+// least `least` slots (a multiple of 64).
+__device__ __forceinline__ int run_slots(int end, int nsplit, int least) {
+  const int units = (end + least - 1) / least;
+  const int ns = min(nsplit, units);
+  return (units + ns - 1) / ns * least;
+}
+__device__ __forceinline__ bool few_rows(const PagedAttnArgs& a, int cnt) {
+  return cnt * a.g <= a.few;
 }
 
 // End of the slots that row i may admit.
@@ -66,28 +82,33 @@ struct Work {
 // Row blocks of one (request, kv head, run) read the same K and V: they are
 // given block ids that land on one XCD (ids are dealt round-robin).  Blocks of
 // later rows, which see more slots, come first.
-__device__ __forceinline__ Work work_of(const PagedAttnArgs& a) {
+__device__ __forceinline__ Work work_of(const PagedAttnArgs& a, int qblocks, int nsplit) {
   const int b = blockIdx.x, j = b / kXcds;
-  const int grp = (j / a.qblocks) * kXcds + b % kXcds;
+  const int grp = (j / qblocks) * kXcds + b % kXcds;
   Work w;
-  w.ok = grp < a.b.R * a.Hkv * a.nsplit;
-  w.qb = a.qblocks - 1 - j % a.qblocks;
-  w.split = grp % a.nsplit;
-  w.kvh = grp / a.nsplit % a.Hkv;
-  w.r = grp / a.nsplit / a.Hkv;
+  w.ok = grp < a.b.R * a.Hkv * nsplit;
+  w.qb = qblocks - 1 - j % qblocks;
+  w.split = grp % nsplit;
+  w.kvh = grp / nsplit % a.Hkv;
+  w.r = grp / nsplit / a.Hkv;
   return w;
 }
+__device__ __forceinline__ PagedReq attn_req(const PagedAttnArgs& a, int r) {
+  PagedReq q = paged_req(a.b, r);
+  if (a.mask) q.cnt = min(q.cnt, a.N);
+  return q;
+}
 
-// Online softmax of one 16-row column tile over a chunk: s[h][t] holds the raw
-// scores of half h, tile t (slots 32 h + 8 grp + 4 t + e); bit 8 h + i of `adm` is
-// set when slot 32 h + 8 grp + i is admitted (ignored when `all`).  Writes the
-// weights as B operands and returns the factor for the output so far.
-template <bool H>
-__device__ __forceinline__ float softmax_chunk(const f32x4 (&s)[2][2], uint32_t adm, bool all,
-                                               float c, float& m, float& l, u32x4 (&bp)[2]) {
-  float v[16];
+// Online softmax of one 16-row column tile over a chunk of NH halves of 32 slots:
+// s[h][t] holds the raw scores of half h, tile t (slots 32 h + 8 grp + 4 t + e); bit 8 h
+// + i of `adm` is set when slot 32 h + 8 grp + i is admitted (ignored when `all`).
+// Writes the weights as B operands and returns the factor for the output so far.
+template <bool H, int NH>
+__device__ __forceinline__ float softmax_chunk(const f32x4 (&s)[NH][2], uint32_t adm, bool all,
+                                               float c, float& m, float& l, u32x4 (&bp)[NH]) {
+  float v[8 * NH];
 #pragma unroll
-  for (int h = 0; h < 2; ++h)
+  for (int h = 0; h < NH; ++h)
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       v[8 * h + e] = s[h][0][e];
@@ -95,11 +116,11 @@ __device__ __forceinline__ float softmax_chunk(const f32x4 (&s)[2][2], uint32_t 
     }
   if (!all) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) v[i] = ((adm >> i) & 1u) ? v[i] : kNegInf;
+    for (int i = 0; i < 8 * NH; ++i) v[i] = ((adm >> i) & 1u) ? v[i] : kNegInf;
   }
   float cmax = v[0];
 #pragma unroll
-  for (int i = 1; i < 16; ++i) cmax = fmaxf(cmax, v[i]);
+  for (int i = 1; i < 8 * NH; ++i) cmax = fmaxf(cmax, v[i]);
   const float mx = row_max4(cmax);
   float alpha = 1.0f;
   if (__any(mx > m)) {
@@ -111,13 +132,13 @@ __device__ __forceinline__ float softmax_chunk(const f32x4 (&s)[2][2], uint32_t 
   const float off = (m == kNegInf ? 0.0f : m * c) - (H ? kHalfLift : 0.0f);
   float ps = 0.0f;
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
+  for (int i = 0; i < 8 * NH; ++i) {
     v[i] = exp2_hw(__builtin_fmaf(v[i], c, -off));
     ps += v[i];
   }
   l += ps;
 #pragma unroll
-  for (int h = 0; h < 2; ++h)
+  for (int h = 0; h < NH; ++h)
 #pragma unroll
     for (int i = 0; i < 4; ++i) bp[h][i] = pack16<H>(v[8 * h + 2 * i], v[8 * h + 2 * i + 1]);
   return alpha;
@@ -157,6 +178,46 @@ __device__ __forceinline__ uint32_t fine_pair(uint32_t w) {
   return (odd16<H>(w) ? 0u : w & 0xffffu) | (odd16<H>(w >> 16) ? 0u : w & 0xffff0000u);
 }
 
+// Where the run of a request of few rows leaves row rho.
+__device__ __forceinline__ size_t few_part(const PagedAttnArgs& a, int split, int r, int kvh,
+                                           int rho) {
+  return (((size_t)split * a.b.R + r) * a.Hkv + kvh) * a.few_stride + rho;
+}
+
+// Infinite and NaN values that were set to zero: they make the outputs of the rows
+// that do admit them NaN.  Rows ri[c] of a lane, their elements 16 t + d .. + 3 in
+// o[c][t]; slots [first, kend).  Rare, so slot by slot from memory.
+template <int D, bool H, int CT, int DT>
+__device__ __forceinline__ void mend_odd(const PagedAttnArgs& a, const PagedReq& q, int r, int kvh,
+                                         const int (&ri)[CT], int i_first, const uint32_t* mask,
+                                         int first, int kend, int d, f32x4 (&o)[CT][DT]) {
+  const int* table = a.b.page_table + (size_t)r * a.b.max_pages;
+  const int pmask = (1 << a.b.page_shift) - 1;
+#pragma unroll 1
+  for (int s = first; s < kend; ++s) {
+    const int p = table[s >> a.b.page_shift], j = s - q.prefix;
+    if ((unsigned)p >= (unsigned)a.b.pages) continue;
+    const uint16_t* vrow = a.v + ((size_t)p * a.b.page_units + (size_t)kvh * a.b.head_units) * 8 +
+                           (size_t)(s & pmask) * D + d;
+    bool sees[CT];
+#pragma unroll
+    for (int c = 0; c < CT; ++c)
+      sees[c] = j < 0 || (a.mask ? (mask[(ri[c] - i_first) * a.NW + (j >> 5)] >> (j & 31)) & 1
+                                 : j <= ri[c]);
+#pragma unroll
+    for (int t = 0; t < DT; ++t) {
+      const u32x2 w = *(const u32x2*)(vrow + 16 * t);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const bool odd = odd16<H>(w[e / 2] >> (16 * (e & 1)));
+#pragma unroll
+        for (int c = 0; c < CT; ++c)
+          if (odd && sees[c]) o[c][t][e] = __builtin_nanf("");
+      }
+    }
+  }
+}
+
 template <int D, bool H>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) void paged_attn_kernel(
     PagedAttnArgs a) {
@@ -167,12 +228,11 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
   __shared__ int sOdd;  // values were set to zero because some row may not admit them
   extern __shared__ uint32_t sMask[];
 
-  const Work wk = work_of(a);
+  const Work wk = work_of(a, a.qblocks, a.nsplit);
   if (!wk.ok) return;
-  const PagedReq rq = paged_req(a.b, wk.r);
-  const int cnt = a.mask ? min(rq.cnt, a.N) : rq.cnt;
-  PagedReq q = rq;
-  q.cnt = cnt;
+  const PagedReq q = attn_req(a, wk.r);
+  const int cnt = q.cnt;
+  if (few_rows(a, cnt)) return;  // (the other kernel's)
   const int rows = cnt * a.g, rho0 = wk.qb * kRowsPerBlock;
   if (rho0 >= rows) return;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x & 63;
@@ -180,7 +240,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
   const int i_first = rho0 / a.g;  // request rows of the block
   const int i_last = min((rho0 + kRowsPerBlock - 1) / a.g, cnt - 1);
   const int end = min(q.prefix + cnt, a.b.C);
-  const int run = run_slots(end, a.nsplit);
+  const int run = run_slots(end, a.nsplit, 2 * kChunk);
   const bool direct = run >= end;  // one run: no merge
   const int kbeg = wk.split * run, kend = min(kbeg + run, row_end(a, q, i_last));
   if (kbeg >= kend) return;
@@ -322,7 +382,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
     for (int c = 0; c < CT; ++c) {
       const uint32_t adm =
           full ? 0u : admitted(a, q, sMask + (ri[c] - i_first) * a.NW, ri[c], c0, kend, bad, grp);
-      const float alpha = softmax_chunk<H>(sacc[c], adm, full, a.scale_log2, m[c], l[c], bp[c]);
+      const float alpha = softmax_chunk<H, 2>(sacc[c], adm, full, a.scale_log2, m[c], l[c], bp[c]);
       if (__any(alpha != 1.0f)) {
 #pragma unroll
         for (int t = 0; t < DT; ++t) o[c][t] *= alpha;
@@ -348,34 +408,8 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
   }
   // (every wave is past the loop's last barrier)
   if (sOdd) {
-    // Infinite and NaN values that were set to zero: they make the outputs of the
-    // rows that do admit them NaN.  (Rare, so slot by slot from memory.)
     const int first = some_bad ? kbeg : kbeg + max(all_see - kbeg, 0) / kChunk * kChunk;
-#pragma unroll 1
-    for (int s = first; s < kend; ++s) {
-      const int p = table[s >> a.b.page_shift];
-      if ((unsigned)p >= (unsigned)a.b.pages) continue;
-      const uint16_t* vrow = a.v + ((size_t)p * a.b.page_units + (size_t)wk.kvh * a.b.head_units) * 8 +
-                             (size_t)(s & pmask) * D + 4 * grp;
-      bool sees[CT];
-#pragma unroll
-      for (int c = 0; c < CT; ++c) {
-        const int j = s - q.prefix;
-        sees[c] = j < 0 || (a.mask ? (sMask[(ri[c] - i_first) * a.NW + (j >> 5)] >> (j & 31)) & 1
-                                   : j <= ri[c]);
-      }
-#pragma unroll
-      for (int t = 0; t < DT; ++t) {
-        const u32x2 w = *(const u32x2*)(vrow + 16 * t);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const bool odd = odd16<H>(w[e / 2] >> (16 * (e & 1)));
-#pragma unroll
-          for (int c = 0; c < CT; ++c)
-            if (odd && sees[c]) o[c][t][e] = __builtin_nanf("");
-        }
-      }
-    }
+    mend_odd<D, H, CT, DT>(a, q, wk.r, wk.kvh, ri, i_first, sMask, first, kend, 4 * grp, o);
   }
 
 #pragma unroll
@@ -408,6 +442,182 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
   }
 }
 
+// Requests of few rows: 16 of one (request, kv head) to a workgroup.
+template <int D, bool H>
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3))) void paged_few_kernel(
+    PagedAttnArgs a) {
+  constexpr int KS = D / 32, DT = D / 16, UPR = D / 8;
+  constexpr int INS = kFewChunk * UPR / 64;  // load instructions of a chunk's V
+  constexpr int PART = DT * 64;              // f32x4 of a wave's output
+  __shared__ __attribute__((aligned(16))) uint16_t sV[kWaves][kFewChunk * D];
+  __shared__ float2 sML[kWaves][16];
+  __shared__ int sOdd;
+  extern __shared__ uint32_t sMask[];
+  static_assert(sizeof(uint16_t) * kFewChunk * D >= PART * sizeof(f32x4), "an output fits a tile");
+
+  const Work wk = work_of(a, a.few_qblocks, a.few_nsplit);
+  if (!wk.ok) return;
+  const PagedReq q = attn_req(a, wk.r);
+  const int rows = q.cnt * a.g, rho0 = wk.qb * 16;
+  if (rho0 >= rows || !few_rows(a, q.cnt)) return;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x & 63;
+  const int col = lane & 15, grp = lane >> 4;
+  const int i_first = rho0 / a.g, i_last = (min(rho0 + 16, rows) - 1) / a.g;
+  const int end = min(q.prefix + q.cnt, a.b.C);
+  const int run = run_slots(end, a.few_nsplit, kFewRun);
+  const bool direct = run >= end;
+  const int kbeg = wk.split * run, kend = min(kbeg + run, row_end(a, q, i_last));
+  if (kbeg >= kend) return;
+  const int all_see = min(kend, q.prefix + (a.mask ? 0 : i_first + 1));
+  const int* table = a.b.page_table + (size_t)wk.r * a.b.max_pages;
+  const int pmask = (1 << a.b.page_shift) - 1;
+  auto page_of = [&](int c0) __attribute__((always_inline)) {
+    return table[min(c0 + (lane & 31), kend - 1) >> a.b.page_shift];
+  };
+  const int c_first = kbeg + wave * kFewChunk;
+  int pg = page_of(min(c_first, kend - 1));
+
+  const int rho = min(rho0 + col, rows - 1);
+  const int ri = rho / a.g, hq = wk.kvh * a.g + rho % a.g;
+  u32x4 bq[KS];
+  {
+    const uint16_t* qrow = a.q + ((size_t)(q.start + ri) * a.Hq + hq) * D + grp * 8;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) bq[s] = *(const u32x4*)(qrow + s * 32);
+  }
+  if (threadIdx.x == 0) sOdd = 0;
+  if (a.mask) {
+    const uint32_t* mg = a.mask + ((size_t)wk.r * a.N + i_first) * a.NW;
+    for (int i = threadIdx.x; i < (i_last - i_first + 1) * a.NW; i += kThreads) sMask[i] = mg[i];
+  }
+  lds_barrier();
+  const uint32_t* mw = sMask + (ri - i_first) * a.NW;
+
+  f32x4 o[DT];
+  float m = kNegInf, l = 0.0f;
+#pragma unroll
+  for (int t = 0; t < DT; ++t) o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const int krow0 = 8 * (col >> 2) + (col & 3);
+  const int vkey = 8 * grp + (col >> 2);
+  for (int c0 = c_first; c0 < kend; c0 += kWaves * kFewChunk) {
+    const bool none = (unsigned)pg >= (unsigned)a.b.pages;
+    const uint64_t bad = __ballot(none) & 0xffffffffu;
+    const uint32_t pgc = none ? 0u : (uint32_t)pg;
+    const int last = kend - 1 - c0;  // (slots past the run repeat its last one)
+    auto at = [&](int row) __attribute__((always_inline)) {  // 16-byte units before the row
+      const uint32_t p = __builtin_amdgcn_ds_bpermute(row * 4, pgc);
+      return (size_t)p * a.b.page_units + (size_t)wk.kvh * a.b.head_units +
+             (uint32_t)((c0 + min(row, last)) & pmask) * UPR;
+    };
+#pragma unroll
+    for (int i = 0; i < INS; ++i) {
+      const int u = i * 64 + lane, row = u / UPR, pos = u % UPR;
+      load_lds16((const uint4*)a.v + at(row) + (pos ^ v_unit<D>(row)), &sV[wave][i * 512]);
+    }
+    u32x4 kf[2][KS];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const u32x4* kr = (const u32x4*)a.k + at(krow0 + 4 * t) + grp;
+#pragma unroll
+      for (int k = 0; k < KS; ++k) kf[t][k] = kr[4 * k];
+    }
+    pg = page_of(min(c0 + kWaves * kFewChunk, kend - 1));
+    f32x4 sacc[1][2] = {{f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}}};
+#pragma unroll
+    for (int k = 0; k < KS; ++k) {
+      sacc[0][0] = mfma16<H>(kf[0][k], bq[k], sacc[0][0]);
+      sacc[0][1] = mfma16<H>(kf[1][k], bq[k], sacc[0][1]);
+    }
+    const bool full = !bad && c0 + kFewChunk <= all_see;
+    const uint32_t adm = full ? 0u : admitted(a, q, mw, ri, c0, kend, bad, grp);
+    u32x4 bp[1];
+    const float alpha = softmax_chunk<H, 1>(sacc, adm, full, a.scale_log2, m, l, bp);
+    if (__any(alpha != 1.0f)) {
+#pragma unroll
+      for (int t = 0; t < DT; ++t) o[t] *= alpha;
+    }
+    wait_loads();
+    if (!full) {  // infinite and NaN values, and those of no page, become zeros
+      bool odd = false;
+#pragma unroll 1
+      for (int i = 0; i < INS; ++i) {
+        const int u = i * 64 + lane;
+        u32x4 w = *(const u32x4*)(sV[wave] + u * 8);
+        const bool gone = (bad >> (u / UPR)) & 1;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t f = gone ? 0u : fine_pair<H>(w[e]);
+          odd |= !gone && f != w[e];
+          w[e] = f;
+        }
+        *(u32x4*)(sV[wave] + u * 8) = w;
+      }
+      if (odd) sOdd = 1;
+    }
+#pragma unroll
+    for (int t = 0; t < DT; ++t) {
+      const uint16_t* vr = sV[wave] + vkey * D +
+                           ((2 * t + ((col >> 1) & 1)) ^ v_unit<D>(vkey)) * 8 + (col & 1) * 4;
+      const u32x2 lo = read_tr(vr), hi = read_tr(vr + 4 * D);
+      o[t] = mfma16<H>(u32x4{lo[0], lo[1], hi[0], hi[1]}, bp[0], o[t]);
+    }
+    // (the tile's reads are back before the next chunk's loads overwrite it)
+    __atomic_signal_fence(__ATOMIC_SEQ_CST);
+    __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
+    __atomic_signal_fence(__ATOMIC_SEQ_CST);
+  }
+  // the waves' results, each in its own tile's place
+  l += __shfl_xor(l, 16, 64);
+  l += __shfl_xor(l, 32, 64);
+  if (grp == 0) sML[wave][col] = make_float2(m, l);
+  f32x4* sO = (f32x4*)sV[wave];
+#pragma unroll
+  for (int t = 0; t < DT; ++t) sO[t * 64 + lane] = o[t];
+  lds_barrier();
+  const bool odd = sOdd != 0;
+  for (int e = threadIdx.x; e < PART; e += kThreads) {  // (e % 64 == lane)
+    if (rho0 + col >= rows) break;
+    const int t = e / 64;
+    float M = kNegInf;
+    float2 ml[kWaves];
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      ml[w] = sML[w][col];
+      M = fmaxf(M, ml[w].x);
+    }
+    float L = 0.0f;
+    f32x4 O = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      // (equal maxima, -inf among them: factor 1)
+      const float wt = ml[w].x == M ? 1.0f : exp2_hw((ml[w].x - M) * a.scale_log2);
+      L += wt * ml[w].y;
+      O += ((const f32x4*)sV[w])[e] * wt;
+    }
+    const int d = t * 16 + 4 * grp;
+    if (odd) {
+      const int rows1[1] = {ri};
+      f32x4 one[1][1] = {{O}};
+      mend_odd<D, H, 1, 1>(a, q, wk.r, wk.kvh, rows1, i_first, sMask, kbeg, kend, d, one);
+      O = one[0][0];
+    }
+    if (direct) {
+      const float inv = L == 0.0f ? 0.0f : 1.0f / L;
+      u32x2 wv;
+      wv[0] = pack16<H>(O[0] * inv, O[1] * inv);
+      wv[1] = pack16<H>(O[2] * inv, O[3] * inv);
+      *(u32x2*)(a.out + ((size_t)(q.start + ri) * a.Hq + hq) * D + d) = wv;
+    } else {
+      const size_t prow = few_part(a, wk.split, wk.r, wk.kvh, rho);
+      *(f32x4*)(a.few_o + prow * D + d) = O;
+      if (d == 0) {
+        a.few_ml[2 * prow] = M;
+        a.few_ml[2 * prow + 1] = L;
+      }
+    }
+  }
+}
+
 // Merge of the runs: a wave takes 256 / D heads of one row, D / 4 threads each,
 // 4 consecutive elements apiece.  Requests of one run are already written.
 template <int D, bool H>
@@ -421,14 +631,20 @@ __global__ __launch_bounds__(kMergeThreads) void paged_merge_kernel(PagedAttnArg
   if (t >= a.b.T) return;
   const int r = request_of_row(a.b, t);
   if (r < 0) return;
-  PagedReq q = paged_req(a.b, r);
-  if (a.mask) q.cnt = min(q.cnt, a.N);
+  const PagedReq q = attn_req(a, r);
   const int i = t - q.start, h = wave % per_row * HPW + lane / TPR, d = lane % TPR * 4;
-  if (i >= q.cnt) return;
-  const int end = min(q.prefix + q.cnt, a.b.C), run = run_slots(end, a.nsplit);
-  if (run >= end || h >= a.Hq) return;
+  if (i >= q.cnt || h >= a.Hq) return;
+  const int end = min(q.prefix + q.cnt, a.b.C);
+  const bool few = few_rows(a, q.cnt);
+  const int run = few ? run_slots(end, a.few_nsplit, kFewRun) : run_slots(end, a.nsplit, 2 * kChunk);
+  if (run >= end) return;
   const int ns = (row_end(a, q, i) + run - 1) / run;
-  const size_t rows = (size_t)a.b.T * a.Hq, qidx = (size_t)t * a.Hq + h;
+  const size_t qidx = (size_t)t * a.Hq + h;
+  // the row's parts, `rows` apart
+  const size_t first = few ? few_part(a, 0, r, h / a.g, i * a.g + h % a.g) : qidx;
+  const size_t rows = few ? (size_t)a.b.R * a.Hkv * a.few_stride : (size_t)a.b.T * a.Hq;
+  const float* part_o = few ? a.few_o : a.part_o;
+  const float* part_ml = few ? a.few_ml : a.part_ml;
   float M = kNegInf, L = 0.0f;
   f32x4 O = {0.f, 0.f, 0.f, 0.f};
   for (int s0 = 0; s0 < ns; s0 += kMergeBatch) {
@@ -436,10 +652,10 @@ __global__ __launch_bounds__(kMergeThreads) void paged_merge_kernel(PagedAttnArg
     f32x4 os[kMergeBatch];
 #pragma unroll
     for (int j = 0; j < kMergeBatch; ++j) {
-      const size_t prow = (size_t)min(s0 + j, ns - 1) * rows + qidx;
-      ms[j] = a.part_ml[2 * prow];
-      ls[j] = a.part_ml[2 * prow + 1];
-      os[j] = *(const f32x4*)(a.part_o + prow * D + d);
+      const size_t prow = (size_t)min(s0 + j, ns - 1) * rows + first;
+      ms[j] = part_ml[2 * prow];
+      ls[j] = part_ml[2 * prow + 1];
+      os[j] = *(const f32x4*)(part_o + prow * D + d);
     }
     float Mn = M;
 #pragma unroll
@@ -466,20 +682,25 @@ __global__ __launch_bounds__(kMergeThreads) void paged_merge_kernel(PagedAttnArg
   *(u32x2*)(a.out + qidx * D + d) = w;
 }
 
+// The mask rows of a workgroup of `rows` rows: at most (rows - 1) / g + 2 request rows.
+unsigned mask_bytes(const PagedAttnArgs& a, int rows) {
+  if (!a.mask) return 0;
+  const int nodes = (rows - 1) / a.g + 2;
+  return (unsigned)((nodes < a.N ? nodes : a.N) * a.NW * sizeof(uint32_t));
+}
+
 template <int D, bool H>
 hipError_t launch(const PagedAttnArgs& a, const PagedPlan& p, hipStream_t stream) {
-  unsigned mask_bytes = 0;
-  if (a.mask) {  // 128 rows touch at most 127 / g + 2 request rows
-    const int nodes = (kRowsPerBlock - 1) / a.g + 2;
-    mask_bytes = (unsigned)((nodes < a.N ? nodes : a.N) * a.NW * sizeof(uint32_t));
-  }
-  paged_attn_kernel<D, H><<<(unsigned)p.blocks, kThreads, mask_bytes, stream>>>(a);
+  if (p.blocks)
+    paged_attn_kernel<D, H>
+        <<<(unsigned)p.blocks, kThreads, mask_bytes(a, kRowsPerBlock), stream>>>(a);
+  if (p.few_blocks)
+    paged_few_kernel<D, H><<<(unsigned)p.few_blocks, kThreads, mask_bytes(a, 16), stream>>>(a);
   const hipError_t e = hipGetLastError();
-  if (e != hipSuccess || a.nsplit == 1) return e;
+  if (e != hipSuccess || (p.nsplit == 1 && p.few_nsplit == 1)) return e;
   constexpr int HPW = 256 / D;
   const long long waves = (long long)a.b.T * ((a.Hq + HPW - 1) / HPW);
-  paged_merge_kernel<D, H>
-      <<<(unsigned)((waves + 3) / 4), kMergeThreads, 0, stream>>>(a);
+  paged_merge_kernel<D, H><<<(unsigned)((waves + 3) / 4), kMergeThreads, 0, stream>>>(a);
   return hipGetLastError();
 }
 
@@ -489,24 +710,47 @@ PagedPlan plan_paged_attention(int R, int T, int max_rows, int Hq, int Hkv, int 
                                int cus) {
   PagedPlan p;
   const int g = Hq / Hkv;
-  const long long qb = ((long long)max_rows * g + kRowsPerBlock - 1) / kRowsPerBlock;
+  const long long most = (long long)max_rows * g;  // rows of a request
+  // Which kernels: requests of few rows have their own, unless none can have few (one
+  // request of more) or nearly all must have many (a padded batch of trees).
+  p.few = most <= kFewRows || (R > 1 && (long long)T * 2 < (long long)R * max_rows) ? kFewRows : 0;
+  const bool many = most > kFewRows;
+  p.few_stride = (int)(most < kFewRows ? most : kFewRows);
+  p.few_qblocks = (p.few_stride + 15) / 16;
+  const long long pairs = (long long)R * Hkv;
+  const auto runs = [&](long long base, int target, int least) {
+    const int units = (C + least - 1) / least;
+    long long ns = base < target ? (target + base - 1) / base : 1;
+    ns = ns < units ? ns : units;
+    return (int)(ns < kMaxSplits ? ns : kMaxSplits);
+  };
+  p.few_nsplit = p.few ? runs(pairs * p.few_qblocks, 8 * cus, kFewRun) : 1;
+  p.few_blocks = p.few ? (pairs * p.few_nsplit + kXcds - 1) / kXcds * kXcds * p.few_qblocks : 0;
+  const long long qb = (most + kRowsPerBlock - 1) / kRowsPerBlock;
   p.qblocks = (int)qb;
   // row blocks that can hold rows: all of a request's, or by the rows there are
   const long long some = (long long)T * g / kRowsPerBlock + R;
-  const long long base = Hkv * (some < qb * R ? some : qb * R);
-  const int chunks = (C + kChunk - 1) / kChunk;
-  long long ns = base < 2 * cus ? (2 * cus + base - 1) / base : 1;
-  ns = ns < (chunks + 1) / 2 ? ns : (chunks + 1) / 2;
-  ns = ns < kMaxSplits ? ns : kMaxSplits;
-  p.nsplit = (int)(ns < 1 ? 1 : ns);
-  const long long groups = (long long)R * Hkv * p.nsplit;
-  p.blocks = (groups + kXcds - 1) / kXcds * kXcds * qb;
-  p.ws_bytes = p.nsplit > 1 ? (size_t)p.nsplit * T * Hq * (D + 2) * sizeof(float) + 256 : 0;
+  p.nsplit = many ? runs(Hkv * (some < qb * R ? some : qb * R), cus / 2, 2 * kChunk) : 1;
+  p.blocks = many ? (pairs * p.nsplit + kXcds - 1) / kXcds * kXcds * qb : 0;
+  p.parts = p.nsplit > 1 ? (size_t)p.nsplit * T * Hq : 0;
+  p.few_parts = p.few_nsplit > 1 ? (size_t)p.few_nsplit * pairs * p.few_stride : 0;
+  const size_t parts = p.parts + p.few_parts;
+  p.ws_bytes = parts ? parts * (D + 2) * sizeof(float) + 256 : 0;
   return p;
 }
 
-hipError_t launch_paged_attention(const PagedAttnArgs& a, const PagedPlan& p, int D, bool f16,
-                                  hipStream_t stream) {
+hipError_t launch_paged_attention(PagedAttnArgs a, const PagedPlan& p, int D, bool f16,
+                                  void* workspace, hipStream_t stream) {
+  a.qblocks = p.qblocks;
+  a.nsplit = p.nsplit;
+  a.few = p.few;
+  a.few_qblocks = p.few_qblocks;
+  a.few_nsplit = p.few_nsplit;
+  a.few_stride = p.few_stride;
+  a.part_o = (float*)workspace;
+  a.few_o = a.part_o + p.parts * D;
+  a.part_ml = a.few_o + p.few_parts * D;
+  a.few_ml = a.part_ml + p.parts * 2;
   if (D == 128) return f16 ? launch<128, true>(a, p, stream) : launch<128, false>(a, p, stream);
   return f16 ? launch<64, true>(a, p, stream) : launch<64, false>(a, p, stream);
 }
