@@ -396,9 +396,9 @@ size_t pctree_paged_attention_workspace_bytes(const pctree_paged_cache* cache,
  * q and out [T][Hq][D] dtype, contiguous; float32 scores, softmax and sums, the
  * weights rounded to dtype before the weighted sum.  Rows that admit no slot
  * are zero.  The pages must already hold the new rows' keys and values
- * (pctree_append_paged).  Slots past the request's last row are never read; a
- * slot before it that a row does not admit adds nothing to that row, whatever
- * it holds (infinities and NaN included).
+ * (pctree_append_paged).  A slot that a row does not admit adds nothing to that
+ * row, whatever it holds (infinities and NaN included); an infinite or NaN
+ * value that a row admits makes that element of it non-finite.
  * Errors: as for pctree_tree_attention; UNSUPPORTED also for a page_size that
  * is no power of two or beyond its limit, R > 65535, and
  * max_pages * page_size > PCTREE_MAX_PAGED_SLOTS. */

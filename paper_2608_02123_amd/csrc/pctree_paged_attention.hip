@@ -16,8 +16,7 @@
 //   and O^T += V^T P^T on MFMA 16x16x32 for its 32 rows, with an online softmax in base
 //   2 (32-bit maximum, sum and output); the two K tiles of a pair are arranged so that
 //   a lane ends with 8 consecutive slots of its row, the B operand of the second
-//   product.  The weights are rounded to 16 bits there, an operand of the matrix units;
-//   their sum is not.
+//   product.  The weights are rounded to 16 bits there, an operand of the matrix units.
 // * Others (single tokens): bytes bound them.  A workgroup takes 16 rows and a run of
 //   slots; each of its waves takes 32-slot chunks by itself, K straight into
 //   registers, V into an LDS tile of its own, and 16 waves a compute unit keep 16 KB
@@ -103,9 +102,12 @@ __device__ __forceinline__ PagedReq attn_req(const PagedAttnArgs& a, int r) {
 // s[h][t] holds the raw scores of half h, tile t (slots 32 h + 8 grp + 4 t + e); bit 8 h
 // + i of `adm` is set when slot 32 h + 8 grp + i is admitted (ignored when `all`).
 // Writes the weights as B operands and returns the factor for the output so far.
+// (Their sum is a product of its own, a row of ones with the weights: 32 clocks of the
+// matrix unit for 64 of the vector unit, which is the busier one, and the sum is that
+// of the rounded weights.)
 template <bool H, int NH>
 __device__ __forceinline__ float softmax_chunk(const f32x4 (&s)[NH][2], uint32_t adm, bool all,
-                                               float c, float& m, float& l, u32x4 (&bp)[NH]) {
+                                               float c, float& m, u32x4 (&bp)[NH]) {
   float v[8 * NH];
 #pragma unroll
   for (int h = 0; h < NH; ++h)
@@ -127,16 +129,10 @@ __device__ __forceinline__ float softmax_chunk(const f32x4 (&s)[NH][2], uint32_t
     const float mn = fmaxf(m, mx);
     alpha = mn == m ? 1.0f : exp2_hw((m - mn) * c);  // m = -inf: 0
     m = mn;
-    l *= alpha;
   }
   const float off = (m == kNegInf ? 0.0f : m * c) - (H ? kHalfLift : 0.0f);
-  float ps = 0.0f;
 #pragma unroll
-  for (int i = 0; i < 8 * NH; ++i) {
-    v[i] = exp2_hw(__builtin_fmaf(v[i], c, -off));
-    ps += v[i];
-  }
-  l += ps;
+  for (int i = 0; i < 8 * NH; ++i) v[i] = exp2_hw(__builtin_fmaf(v[i], c, -off));
 #pragma unroll
   for (int h = 0; h < NH; ++h)
 #pragma unroll
@@ -271,11 +267,11 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
 
   const int* table = a.b.page_table + (size_t)wk.r * a.b.max_pages;
   const int pmask = (1 << a.b.page_shift) - 1;
-  // (slots past the run repeat its last one)
+  constexpr int RPI = 64 / UPR;  // slots of a load instruction
   auto page_of = [&](int c0) __attribute__((always_inline)) {
     return table[min(c0 + lane, kend - 1) >> a.b.page_shift];
   };
-  // The chunk's K and V into a buffer; the slots without a page.
+  // The chunk's K and V into a buffer; returns the slots without a page.
   auto fetch = [&](int c0, int pg, int buf) __attribute__((always_inline)) -> uint64_t {
     const bool none = (unsigned)pg >= (unsigned)a.b.pages;
     const uint64_t bad = __ballot(none);
@@ -283,16 +279,45 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
     const int last = kend - 1 - c0;
 #pragma unroll
     for (int i = 0; i < IPW; ++i) {
-      const int u = (wave * IPW + i) * 64 + lane;
-      const int row = u / UPR, pos = u % UPR;
-      const uint32_t p = __builtin_amdgcn_ds_bpermute(row * 4, pgc);
-      const int slot = (c0 + min(row, last)) & pmask;
+      const int row = (wave * IPW + i) * RPI + lane / UPR, pos = lane % UPR;
+      const uint32_t p = __builtin_amdgcn_ds_bpermute(min(row, last) * 4, pgc);
       const size_t base = (size_t)p * a.b.page_units + (size_t)wk.kvh * a.b.head_units +
-                          (uint32_t)slot * UPR;
+                          (uint32_t)((c0 + min(row, last)) & pmask) * UPR;
       load_lds16((const uint4*)a.k + base + (pos ^ k_unit<D>(row)),
                  &sKV[buf][0][(wave * IPW + i) * 512]);
       load_lds16((const uint4*)a.v + base + (pos ^ v_unit<D>(row)),
                  &sKV[buf][1][(wave * IPW + i) * 512]);
+    }
+    return bad;
+  };
+  // The same with scalar bases, for pages of at least 8 slots, where the slots of one
+  // load instruction (4, or 8 of a smaller head) share a page; the lanes' offsets are
+  // the same for every chunk.  (Slots past the run in its last page are loaded and
+  // masked.)
+  uint32_t koff[IPW], voff[IPW];
+#pragma unroll
+  for (int i = 0; i < IPW; ++i) {
+    const int row = (wave * IPW + i) * RPI + lane / UPR, pos = lane % UPR;
+    koff[i] = (uint32_t)(row * UPR + (pos ^ k_unit<D>(row))) * 16;
+    voff[i] = (uint32_t)(row * UPR + (pos ^ v_unit<D>(row))) * 16;
+  }
+  const size_t head_base = (size_t)wk.kvh * a.b.head_units;
+  auto fetch_scalar = [&](int c0, int pg, int buf) __attribute__((always_inline)) -> uint64_t {
+    const bool none = (unsigned)pg >= (unsigned)a.b.pages;
+    const uint64_t bad = __ballot(none);
+    const uint32_t pgc = none ? 0u : (uint32_t)pg;
+    const bool one_page = a.b.page_shift >= 6;
+    size_t base = (size_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)pgc) * a.b.page_units +
+                  head_base + (uint32_t)(c0 & pmask) * UPR;
+#pragma unroll
+    for (int i = 0; i < IPW; ++i) {
+      if (!one_page) {
+        const int row = (wave * IPW + i) * RPI;
+        base = (size_t)(uint32_t)__builtin_amdgcn_readlane((int)pgc, row) * a.b.page_units +
+               head_base + (size_t)(((c0 + row) & pmask) - row) * UPR;
+      }
+      load_lds16((const uint4*)a.k + base, koff[i], &sKV[buf][0][(wave * IPW + i) * 512]);
+      load_lds16((const uint4*)a.v + base, voff[i], &sKV[buf][1][(wave * IPW + i) * 512]);
     }
     return bad;
   };
@@ -306,22 +331,118 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
     for (int i = threadIdx.x; i < (i_last - i_first + 1) * a.NW; i += kThreads) sMask[i] = mg[i];
   }
 
-  f32x4 o[CT][DT];
-  float m[CT], l[CT];
+  f32x4 o[CT][DT], l[CT];  // (the four elements of l are the same)
+  float m[CT];
 #pragma unroll
   for (int c = 0; c < CT; ++c) {
     m[c] = kNegInf;
-    l[c] = 0.0f;
+    l[c] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int t = 0; t < DT; ++t) o[c][t] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
   // A rows of a tile pair: tile 0 holds keys 8c + e, tile 1 keys 8c + 4 + e
   const int krow0 = 8 * (col >> 2) + (col & 3);
+  constexpr uint32_t one = H ? 0x3c003c00u : 0x3f803f80u;
+  const u32x4 ones = {one, one, one, one};
   const int vkey = 8 * grp + (col >> 2);  // the key this lane addresses (of the first four)
 
-  int buf = 0;
+  // S^T of the chunk, both halves and column tiles: 8 independent chains.
+  auto scores = [&](const uint16_t* sK, f32x4 (&sacc)[CT][2][2]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int c = 0; c < CT; ++c)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) sacc[c][h][0] = sacc[c][h][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < KS; ++k) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const uint16_t* kr = sK + (32 * h + krow0) * D + ((4 * k + grp) ^ k_unit<D>(krow0)) * 8;
+        const u32x4 a0 = *(const u32x4*)kr;
+        const u32x4 a1 = *(const u32x4*)(kr + 4 * D);
+#pragma unroll
+        for (int c = 0; c < CT; ++c) {
+          sacc[c][h][0] = mfma16<H>(a0, bq[c][k], sacc[c][h][0]);
+          sacc[c][h][1] = mfma16<H>(a1, bq[c][k], sacc[c][h][1]);
+        }
+      }
+    }
+  };
+  // O^T += V^T P^T of one half.
+  auto weigh = [&](const uint16_t* sV, int h, const u32x4 (&bp)[CT]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int t = 0; t < DT; ++t) {
+      const uint16_t* vr = sV + (32 * h + vkey) * D +
+                           ((2 * t + ((col >> 1) & 1)) ^ v_unit<D>(vkey)) * 8 + (col & 1) * 4;
+      const u32x2 lo = read_tr(vr), hi = read_tr(vr + 4 * D);
+      const u32x4 av = {lo[0], lo[1], hi[0], hi[1]};
+#pragma unroll
+      for (int c = 0; c < CT; ++c) o[c][t] = mfma16<H>(av, bp[c], o[c][t]);
+    }
+#pragma unroll
+    for (int c = 0; c < CT; ++c) l[c] = mfma16<H>(ones, bp[c], l[c]);
+  };
+
+  int buf = 0, c0 = kbeg;
   bool some_bad = false;
-  for (int c0 = kbeg; c0 < kend; c0 += kChunk, buf ^= 1) {
+  // Chunks that every row of the block sees whole: no masks, one test for both column
+  // tiles' maxima, and the second half's weights computed beside the first half's
+  // product.
+  const int whole = a.b.page_shift >= 3 ? all_see : kbeg;
+  for (; c0 + kChunk <= whole && !bad_next; c0 += kChunk, buf ^= 1) {
+    wait_loads();
+    lds_barrier();  // the chunk is complete; the other buffer is no longer read
+    if (c0 + kChunk < kend) {
+      bad_next = fetch_scalar(c0 + kChunk, pg, buf ^ 1);
+      pg = page_of(min(c0 + 2 * kChunk, kend - 1));
+    }
+    if (!w_live) continue;
+    f32x4 sacc[CT][2][2];
+    scores(sKV[buf][0], sacc);
+    float mx[CT];
+    bool grows = false;
+#pragma unroll
+    for (int c = 0; c < CT; ++c) {
+      mx[c] = sacc[c][0][0][0];
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) mx[c] = fmaxf(mx[c], sacc[c][h][t][e]);
+      mx[c] = row_max4(mx[c]);
+      grows |= mx[c] > m[c];
+    }
+    if (__any(grows)) {
+#pragma unroll
+      for (int c = 0; c < CT; ++c) {
+        const float mn = fmaxf(m[c], mx[c]);
+        const float alpha = mn == m[c] ? 1.0f : exp2_hw((m[c] - mn) * a.scale_log2);
+        m[c] = mn;
+        l[c] *= alpha;
+#pragma unroll
+        for (int t = 0; t < DT; ++t) o[c][t] *= alpha;
+      }
+    }
+    float off[CT];
+#pragma unroll
+    for (int c = 0; c < CT; ++c)
+      off[c] = (m[c] == kNegInf ? 0.0f : m[c] * a.scale_log2) - (H ? kHalfLift : 0.0f);
+    u32x4 bp[2][CT];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int c = 0; c < CT; ++c) {
+        float w[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          w[e] = exp2_hw(__builtin_fmaf(sacc[c][h][e / 4][e % 4], a.scale_log2, -off[c]));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) bp[h][c][e] = pack16<H>(w[2 * e], w[2 * e + 1]);
+      }
+    weigh(sKV[buf][1], 0, bp[0]);
+    weigh(sKV[buf][1], 1, bp[1]);
+  }
+  for (; c0 < kend; c0 += kChunk, buf ^= 1) {
     wait_loads();
     lds_barrier();  // the chunk is complete; the other buffer is no longer read
     const uint64_t bad = bad_next;
@@ -345,7 +466,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const uint32_t f = none ? 0u : fine_pair<H>(w[e]);
-          odd |= !none && f != w[e];
+          odd |= !none && f != w[e] && c0 + u / UPR < kend;
           any |= f != w[e];
           w[e] = f;
         }
@@ -359,52 +480,24 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
     const bool full = !bad && c0 + kChunk <= min(kend, q.prefix + (a.mask ? 0 : w_first + 1));
 
     f32x4 sacc[CT][2][2];
-#pragma unroll
-    for (int c = 0; c < CT; ++c)
-#pragma unroll
-      for (int h = 0; h < 2; ++h) sacc[c][h][0] = sacc[c][h][1] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int k = 0; k < KS; ++k) {
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const uint16_t* kr = sK + (32 * h + krow0) * D + ((4 * k + grp) ^ k_unit<D>(krow0)) * 8;
-        const u32x4 a0 = *(const u32x4*)kr;
-        const u32x4 a1 = *(const u32x4*)(kr + 4 * D);
-#pragma unroll
-        for (int c = 0; c < CT; ++c) {
-          sacc[c][h][0] = mfma16<H>(a0, bq[c][k], sacc[c][h][0]);
-          sacc[c][h][1] = mfma16<H>(a1, bq[c][k], sacc[c][h][1]);
-        }
-      }
-    }
-    u32x4 bp[CT][2];
+    scores(sK, sacc);
+    u32x4 bp[2][CT];
 #pragma unroll
     for (int c = 0; c < CT; ++c) {
       const uint32_t adm =
           full ? 0u : admitted(a, q, sMask + (ri[c] - i_first) * a.NW, ri[c], c0, kend, bad, grp);
-      const float alpha = softmax_chunk<H, 2>(sacc[c], adm, full, a.scale_log2, m[c], l[c], bp[c]);
+      u32x4 w[2];
+      const float alpha = softmax_chunk<H, 2>(sacc[c], adm, full, a.scale_log2, m[c], w);
+      bp[0][c] = w[0];
+      bp[1][c] = w[1];
       if (__any(alpha != 1.0f)) {
+        l[c] *= alpha;
 #pragma unroll
         for (int t = 0; t < DT; ++t) o[c][t] *= alpha;
       }
     }
-    auto value = [&](int t, int h) __attribute__((always_inline)) {
-      const uint16_t* vr = sV + (32 * h + vkey) * D +
-                           ((2 * t + ((col >> 1) & 1)) ^ v_unit<D>(vkey)) * 8 + (col & 1) * 4;
-      const u32x2 lo = read_tr(vr), hi = read_tr(vr + 4 * D);
-      return u32x4{lo[0], lo[1], hi[0], hi[1]};
-    };
-#pragma unroll
-    for (int t = 0; t < DT; ++t)
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const uint16_t* vr = sV + (32 * h + vkey) * D +
-                             ((2 * t + ((col >> 1) & 1)) ^ v_unit<D>(vkey)) * 8 + (col & 1) * 4;
-        const u32x2 lo = read_tr(vr), hi = read_tr(vr + 4 * D);
-        const u32x4 av = {lo[0], lo[1], hi[0], hi[1]};
-#pragma unroll
-        for (int c = 0; c < CT; ++c) o[c][t] = mfma16<H>(av, bp[c][h], o[c][t]);
-      }
+    weigh(sV, 0, bp[0]);
+    weigh(sV, 1, bp[1]);
   }
   // (every wave is past the loop's last barrier)
   if (sOdd) {
@@ -414,12 +507,10 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
 
 #pragma unroll
   for (int c = 0; c < CT; ++c) {
-    l[c] += __shfl_xor(l[c], 16, 64);
-    l[c] += __shfl_xor(l[c], 32, 64);
     if (!row_in[c]) continue;
     const size_t qidx = (size_t)(q.start + ri[c]) * a.Hq + hq[c];
     if (direct) {
-      const float inv = l[c] == 0.0f ? 0.0f : 1.0f / l[c];  // (no admitted slot)
+      const float inv = l[c][0] == 0.0f ? 0.0f : 1.0f / l[c][0];  // (no admitted slot)
       uint16_t* orow = a.out + qidx * D;
 #pragma unroll
       for (int t = 0; t < DT; ++t) {
@@ -436,7 +527,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
       for (int t = 0; t < DT; ++t) *(f32x4*)(po + t * 16 + 4 * grp) = o[c][t];
       if (grp == 0) {
         a.part_ml[2 * prow] = m[c];
-        a.part_ml[2 * prow + 1] = l[c];
+        a.part_ml[2 * prow + 1] = l[c][0];
       }
     }
   }
@@ -493,12 +584,14 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3))) v
   lds_barrier();
   const uint32_t* mw = sMask + (ri - i_first) * a.NW;
 
-  f32x4 o[DT];
-  float m = kNegInf, l = 0.0f;
+  f32x4 o[DT], l = {0.f, 0.f, 0.f, 0.f};
+  float m = kNegInf;
 #pragma unroll
   for (int t = 0; t < DT; ++t) o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
   const int krow0 = 8 * (col >> 2) + (col & 3);
   const int vkey = 8 * grp + (col >> 2);
+  constexpr uint32_t one = H ? 0x3c003c00u : 0x3f803f80u;
+  const u32x4 ones = {one, one, one, one};
   for (int c0 = c_first; c0 < kend; c0 += kWaves * kFewChunk) {
     const bool none = (unsigned)pg >= (unsigned)a.b.pages;
     const uint64_t bad = __ballot(none) & 0xffffffffu;
@@ -531,11 +624,13 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3))) v
     const bool full = !bad && c0 + kFewChunk <= all_see;
     const uint32_t adm = full ? 0u : admitted(a, q, mw, ri, c0, kend, bad, grp);
     u32x4 bp[1];
-    const float alpha = softmax_chunk<H, 1>(sacc, adm, full, a.scale_log2, m, l, bp);
+    const float alpha = softmax_chunk<H, 1>(sacc, adm, full, a.scale_log2, m, bp);
     if (__any(alpha != 1.0f)) {
+      l *= alpha;
 #pragma unroll
       for (int t = 0; t < DT; ++t) o[t] *= alpha;
     }
+    l = mfma16<H>(ones, bp[0], l);
     wait_loads();
     if (!full) {  // infinite and NaN values, and those of no page, become zeros
       bool odd = false;
@@ -567,9 +662,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3))) v
     __atomic_signal_fence(__ATOMIC_SEQ_CST);
   }
   // the waves' results, each in its own tile's place
-  l += __shfl_xor(l, 16, 64);
-  l += __shfl_xor(l, 32, 64);
-  if (grp == 0) sML[wave][col] = make_float2(m, l);
+  if (grp == 0) sML[wave][col] = make_float2(m, l[0]);
   f32x4* sO = (f32x4*)sV[wave];
 #pragma unroll
   for (int t = 0; t < DT; ++t) sO[t * 64 + lane] = o[t];
