@@ -14,7 +14,7 @@
 //   holds the page of one slot of the chunk, read another chunk ahead, and the lanes
 //   that load a slot's row fetch its page from that lane.  A wave computes S^T = K Q^T
 //   and O^T += V^T P^T on MFMA 16x16x32 for its 32 rows, with an online softmax in base
-//   2 (32-bit maximum, sum and output); the two K tiles of a pair are arranged so that
+//   2 (32-bit reference, sum and output); the two K tiles of a pair are arranged so that
 //   a lane ends with 8 consecutive slots of its row, the B operand of the second
 //   product.  The weights are rounded to 16 bits there, an operand of the matrix units.
 // * Others (single tokens): bytes bound them.  A workgroup takes 16 rows and a run of
@@ -41,7 +41,8 @@
 namespace pctree {
 namespace {
 
-constexpr int kChunk = 64;
+constexpr int kChunk = 64;        // slots of an LDS stage, in halves of 32
+constexpr int kHalves = kChunk / 32;
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
 constexpr int kColTiles = 2;
@@ -57,6 +58,13 @@ constexpr int kMergeBatch = 8;
 // to 2^-36 of the row's largest then stay above float16's smallest, 2^-24, and
 // the largest is 4096.
 constexpr float kHalfLift = 12.0f;
+// The reference that scores are taken relative to follows a row's maximum only when
+// that has grown past it by more than this many powers of two: until then weights are
+// at most 2^8 (2^15 for a lifted float16), rounded as precisely as below 1, and the
+// output so far need not be scaled (72 products a chunk, in about half the chunks of a
+// long row).
+template <bool H>
+constexpr float kSlack = H ? 3.0f : 8.0f;
 
 // Slots per run of a request whose rows end at slot `end`, at most `nsplit` runs of at
 // least `least` slots (a multiple of 64).
@@ -125,7 +133,7 @@ __device__ __forceinline__ float softmax_chunk(const f32x4 (&s)[NH][2], uint32_t
   for (int i = 1; i < 8 * NH; ++i) cmax = fmaxf(cmax, v[i]);
   const float mx = row_max4(cmax);
   float alpha = 1.0f;
-  if (__any(mx > m)) {
+  if (__any((mx - m) * c > kSlack<H>)) {
     const float mn = fmaxf(m, mx);
     alpha = mn == m ? 1.0f : exp2_hw((m - mn) * c);  // m = -inf: 0
     m = mn;
@@ -274,7 +282,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
   // The chunk's K and V into a buffer; returns the slots without a page.
   auto fetch = [&](int c0, int pg, int buf) __attribute__((always_inline)) -> uint64_t {
     const bool none = (unsigned)pg >= (unsigned)a.b.pages;
-    const uint64_t bad = __ballot(none);
+    const uint64_t bad = __ballot(none) & low_bits(kChunk);
     const uint32_t pgc = none ? 0u : (uint32_t)pg;
     const int last = kend - 1 - c0;
 #pragma unroll
@@ -304,20 +312,26 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
   const size_t head_base = (size_t)wk.kvh * a.b.head_units;
   auto fetch_scalar = [&](int c0, int pg, int buf) __attribute__((always_inline)) -> uint64_t {
     const bool none = (unsigned)pg >= (unsigned)a.b.pages;
-    const uint64_t bad = __ballot(none);
+    const uint64_t bad = __ballot(none) & low_bits(kChunk);
     const uint32_t pgc = none ? 0u : (uint32_t)pg;
-    const bool one_page = a.b.page_shift >= 6;
-    size_t base = (size_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)pgc) * a.b.page_units +
-                  head_base + (uint32_t)(c0 & pmask) * UPR;
+    const bool one_page = (1 << a.b.page_shift) >= kChunk;
+    if (one_page) {
+      const size_t base = (size_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)pgc) * a.b.page_units +
+                          head_base + (uint32_t)(c0 & pmask) * UPR;
 #pragma unroll
-    for (int i = 0; i < IPW; ++i) {
-      if (!one_page) {
-        const int row = (wave * IPW + i) * RPI;
-        base = (size_t)(uint32_t)__builtin_amdgcn_readlane((int)pgc, row) * a.b.page_units +
-               head_base + (size_t)(((c0 + row) & pmask) - row) * UPR;
+      for (int i = 0; i < IPW; ++i) {
+        load_lds16((const uint4*)a.k + base, koff[i], &sKV[buf][0][(wave * IPW + i) * 512]);
+        load_lds16((const uint4*)a.v + base, voff[i], &sKV[buf][1][(wave * IPW + i) * 512]);
       }
-      load_lds16((const uint4*)a.k + base, koff[i], &sKV[buf][0][(wave * IPW + i) * 512]);
-      load_lds16((const uint4*)a.v + base, voff[i], &sKV[buf][1][(wave * IPW + i) * 512]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < IPW; ++i) {
+        const int row = (wave * IPW + i) * RPI;
+        const size_t base = (size_t)(uint32_t)__builtin_amdgcn_readlane((int)pgc, row) * a.b.page_units +
+                            head_base + (size_t)(((c0 + row) & pmask) - row) * UPR;
+        load_lds16((const uint4*)a.k + base, koff[i], &sKV[buf][0][(wave * IPW + i) * 512]);
+        load_lds16((const uint4*)a.v + base, voff[i], &sKV[buf][1][(wave * IPW + i) * 512]);
+      }
     }
     return bad;
   };
@@ -347,15 +361,15 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
   const int vkey = 8 * grp + (col >> 2);  // the key this lane addresses (of the first four)
 
   // S^T of the chunk, both halves and column tiles: 8 independent chains.
-  auto scores = [&](const uint16_t* sK, f32x4 (&sacc)[CT][2][2]) __attribute__((always_inline)) {
+  auto scores = [&](const uint16_t* sK, f32x4 (&sacc)[CT][kHalves][2]) __attribute__((always_inline)) {
 #pragma unroll
     for (int c = 0; c < CT; ++c)
 #pragma unroll
-      for (int h = 0; h < 2; ++h) sacc[c][h][0] = sacc[c][h][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int h = 0; h < kHalves; ++h) sacc[c][h][0] = sacc[c][h][1] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int k = 0; k < KS; ++k) {
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
+      for (int h = 0; h < kHalves; ++h) {
         const uint16_t* kr = sK + (32 * h + krow0) * D + ((4 * k + grp) ^ k_unit<D>(krow0)) * 8;
         const u32x4 a0 = *(const u32x4*)kr;
         const u32x4 a1 = *(const u32x4*)(kr + 4 * D);
@@ -396,7 +410,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
       pg = page_of(min(c0 + 2 * kChunk, kend - 1));
     }
     if (!w_live) continue;
-    f32x4 sacc[CT][2][2];
+    f32x4 sacc[CT][kHalves][2];
     scores(sKV[buf][0], sacc);
     float mx[CT];
     bool grows = false;
@@ -404,13 +418,13 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
     for (int c = 0; c < CT; ++c) {
       mx[c] = sacc[c][0][0][0];
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
+      for (int h = 0; h < kHalves; ++h)
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
           for (int e = 0; e < 4; ++e) mx[c] = fmaxf(mx[c], sacc[c][h][t][e]);
       mx[c] = row_max4(mx[c]);
-      grows |= mx[c] > m[c];
+      grows |= (mx[c] - m[c]) * a.scale_log2 > kSlack<H>;
     }
     if (__any(grows)) {
 #pragma unroll
@@ -427,9 +441,9 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
 #pragma unroll
     for (int c = 0; c < CT; ++c)
       off[c] = (m[c] == kNegInf ? 0.0f : m[c] * a.scale_log2) - (H ? kHalfLift : 0.0f);
-    u32x4 bp[2][CT];
+    u32x4 bp[kHalves][CT];
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
+    for (int h = 0; h < kHalves; ++h)
 #pragma unroll
       for (int c = 0; c < CT; ++c) {
         float w[8];
@@ -439,8 +453,8 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
 #pragma unroll
         for (int e = 0; e < 4; ++e) bp[h][c][e] = pack16<H>(w[2 * e], w[2 * e + 1]);
       }
-    weigh(sKV[buf][1], 0, bp[0]);
-    weigh(sKV[buf][1], 1, bp[1]);
+#pragma unroll
+    for (int h = 0; h < kHalves; ++h) weigh(sKV[buf][1], h, bp[h]);
   }
   for (; c0 < kend; c0 += kChunk, buf ^= 1) {
     wait_loads();
@@ -479,25 +493,25 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
     // every row of the wave admits every slot
     const bool full = !bad && c0 + kChunk <= min(kend, q.prefix + (a.mask ? 0 : w_first + 1));
 
-    f32x4 sacc[CT][2][2];
+    f32x4 sacc[CT][kHalves][2];
     scores(sK, sacc);
-    u32x4 bp[2][CT];
+    u32x4 bp[kHalves][CT];
 #pragma unroll
     for (int c = 0; c < CT; ++c) {
       const uint32_t adm =
           full ? 0u : admitted(a, q, sMask + (ri[c] - i_first) * a.NW, ri[c], c0, kend, bad, grp);
-      u32x4 w[2];
-      const float alpha = softmax_chunk<H, 2>(sacc[c], adm, full, a.scale_log2, m[c], w);
-      bp[0][c] = w[0];
-      bp[1][c] = w[1];
+      u32x4 w[kHalves];
+      const float alpha = softmax_chunk<H, kHalves>(sacc[c], adm, full, a.scale_log2, m[c], w);
+#pragma unroll
+      for (int h = 0; h < kHalves; ++h) bp[h][c] = w[h];
       if (__any(alpha != 1.0f)) {
         l[c] *= alpha;
 #pragma unroll
         for (int t = 0; t < DT; ++t) o[c][t] *= alpha;
       }
     }
-    weigh(sV, 0, bp[0]);
-    weigh(sV, 1, bp[1]);
+#pragma unroll
+    for (int h = 0; h < kHalves; ++h) weigh(sV, h, bp[h]);
   }
   // (every wave is past the loop's last barrier)
   if (sOdd) {
