@@ -79,6 +79,7 @@ hipError_t launch_append(const AppendArgs& a, int D, bool f16, hipStream_t strea
 struct PagedPlan {
   int qblocks, few_qblocks;        // row blocks of a (request, kv head) at most
   int nsplit, few_nsplit;          // most slot runs of a request (1: no merge pass)
+  int least;                       // slots of the shortest run (the other kernel's is fixed)
   long long blocks, few_blocks;    // workgroups (XCD-grouped, padded; 0: not launched)
   int few, few_stride;             // the most rows of such a request
   size_t parts, few_parts;         // rows of partial results
@@ -97,7 +98,7 @@ struct PagedAttnArgs {
   float* few_o;          // [few_nsplit][R][Hkv][few_stride][D]
   float* few_ml;         // [few_nsplit][R][Hkv][few_stride][2]
   int Hq, Hkv, g, N, NW;
-  int qblocks, nsplit, few_qblocks, few_nsplit, few, few_stride;
+  int qblocks, nsplit, least, few_qblocks, few_nsplit, few, few_stride;
   float scale_log2;
 };
 

@@ -54,6 +54,7 @@ constexpr int kFewChunk = 32;        // slots of a wave's step there
 constexpr int kFewRun = 4 * kFewChunk;  // the shortest run there, a chunk to each wave
 constexpr int kMergeThreads = 256;
 constexpr int kMergeBatch = 8;
+constexpr int kMatrix = 0x8, kReadLds = 0x100;  // instruction classes of the scheduler
 // float16 weights are 2^12 times the softmax's (as is their sum): weights down
 // to 2^-36 of the row's largest then stay above float16's smallest, 2^-24, and
 // the largest is 4096.
@@ -82,28 +83,79 @@ __device__ __forceinline__ int row_end(const PagedAttnArgs& a, const PagedReq& q
   return min(q.prefix + (a.mask ? q.cnt : i + 1), a.b.C);
 }
 
-struct Work {
-  int r, kvh, split, qb;
-  bool ok;
-};
-// Row blocks of one (request, kv head, run) read the same K and V: they are
-// given block ids that land on one XCD (ids are dealt round-robin).  Blocks of
-// later rows, which see more slots, come first.
-__device__ __forceinline__ Work work_of(const PagedAttnArgs& a, int qblocks, int nsplit) {
-  const int b = blockIdx.x, j = b / kXcds;
-  const int grp = (j / qblocks) * kXcds + b % kXcds;
-  Work w;
-  w.ok = grp < a.b.R * a.Hkv * nsplit;
-  w.qb = qblocks - 1 - j % qblocks;
-  w.split = grp % nsplit;
-  w.kvh = grp / nsplit % a.Hkv;
-  w.r = grp / nsplit / a.Hkv;
-  return w;
-}
 __device__ __forceinline__ PagedReq attn_req(const PagedAttnArgs& a, int r) {
   PagedReq q = paged_req(a.b, r);
   if (a.mask) q.cnt = min(q.cnt, a.N);
   return q;
+}
+
+struct Work {
+  PagedReq q;
+  int r, kvh, split, qb;
+  bool ok;
+};
+// What this workgroup does: row block qb of `rows` rows, a kv head and a run of a
+// request.  Workgroups are dealt round-robin over the XCDs, each with its own L2; row
+// blocks of one (kv head, run) read the same K and V, so each XCD has its own of
+// these pairs, or, where there are fewer than eight, shares one with others (one long
+// request of four heads ran on half of the chip before).
+//
+// Calls of up to 64 requests have workgroups for as many row blocks as their rows can
+// fill, and find theirs from the counts, a request to a lane: the longest requests
+// first, and of each the last rows, which see most, so that what starts last is short
+// (64 single tokens: 161 to 148 us; a workgroup that finds nothing to do takes 1 to 2
+// us of half a compute unit, and 24 requests of 1 to 700 rows had 15,000 of these).
+__device__ __forceinline__ Work work_of(const PagedAttnArgs& a, int qblocks, int nsplit, int rows,
+                                        bool few) {
+  const int pairs = a.Hkv * nsplit;
+  const int x = blockIdx.x % kXcds, j = blockIdx.x / kXcds;
+  int pair, rb;
+  if (pairs % kXcds == 0) {
+    pair = kXcds * (j % (pairs / kXcds));  // (and one of eight, by the request)
+    rb = j / (pairs / kXcds);
+  } else if (kXcds % pairs == 0) {
+    pair = x % pairs;
+    rb = j * (kXcds / pairs) + x / pairs;
+  } else {
+    pair = blockIdx.x % pairs;
+    rb = blockIdx.x / pairs;
+  }
+  Work w;
+  const auto settle = [&]() {
+    // (a short request has one run: rotated, or one or two XCDs would have all of them)
+    if (pairs % kXcds == 0) pair += (x + w.r) % kXcds;
+    w.split = pair % nsplit;
+    w.kvh = pair / nsplit;
+  };
+  if (a.b.R > 64) {
+    w.r = rb / qblocks;
+    w.qb = qblocks - 1 - rb % qblocks;
+    w.ok = w.r < a.b.R;
+    if (!w.ok) return w;
+    settle();
+    w.q = attn_req(a, w.r);
+    w.ok = few_rows(a, w.q.cnt) == few && w.qb * rows < w.q.cnt * a.g;
+    return w;
+  }
+  const int lane = threadIdx.x & 63;
+  PagedReq q = attn_req(a, min(lane, a.b.R - 1));
+  if (lane >= a.b.R || few_rows(a, q.cnt) != few) q.cnt = 0;
+  const int len = q.prefix + q.cnt, blocks = (q.cnt * a.g + rows - 1) / rows;
+  int before = 0;
+  for (int i = 0; i < a.b.R; ++i) {
+    const int l = __builtin_amdgcn_readlane(len, i), n = __builtin_amdgcn_readlane(blocks, i);
+    before += l > len || (l == len && i < lane) ? n : 0;
+  }
+  const uint64_t mine = __ballot(rb >= before && rb - before < blocks);
+  w.ok = mine != 0;
+  if (!w.ok) return w;
+  w.r = (int)__builtin_ctzll(mine);
+  settle();
+  w.q.start = __builtin_amdgcn_readlane(q.start, w.r);
+  w.q.cnt = __builtin_amdgcn_readlane(q.cnt, w.r);
+  w.q.prefix = __builtin_amdgcn_readlane(q.prefix, w.r);
+  w.qb = __builtin_amdgcn_readlane(blocks, w.r) - 1 - (rb - __builtin_amdgcn_readlane(before, w.r));
+  return w;
 }
 
 // Online softmax of one 16-row column tile over a chunk of NH halves of 32 slots:
@@ -232,19 +284,17 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
   __shared__ int sOdd;  // values were set to zero because some row may not admit them
   extern __shared__ uint32_t sMask[];
 
-  const Work wk = work_of(a, a.qblocks, a.nsplit);
+  const Work wk = work_of(a, a.qblocks, a.nsplit, kRowsPerBlock, false);
   if (!wk.ok) return;
-  const PagedReq q = attn_req(a, wk.r);
+  const PagedReq q = wk.q;
   const int cnt = q.cnt;
-  if (few_rows(a, cnt)) return;  // (the other kernel's)
   const int rows = cnt * a.g, rho0 = wk.qb * kRowsPerBlock;
-  if (rho0 >= rows) return;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x & 63;
   const int col = lane & 15, grp = lane >> 4;
   const int i_first = rho0 / a.g;  // request rows of the block
   const int i_last = min((rho0 + kRowsPerBlock - 1) / a.g, cnt - 1);
   const int end = min(q.prefix + cnt, a.b.C);
-  const int run = run_slots(end, a.nsplit, 2 * kChunk);
+  const int run = run_slots(end, a.nsplit, a.least);
   const bool direct = run >= end;  // one run: no merge
   const int kbeg = wk.split * run, kend = min(kbeg + run, row_end(a, q, i_last));
   if (kbeg >= kend) return;
@@ -380,6 +430,15 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
         }
       }
     }
+    // fragments six reads ahead of their two products (LDS answers after four)
+    constexpr int READS = 2 * KS * kHalves, AHEAD = READS < 6 ? READS : 6;
+    __builtin_amdgcn_sched_group_barrier(kReadLds, AHEAD, 0);
+#pragma unroll
+    for (int i = 0; i < READS - AHEAD; ++i) {
+      __builtin_amdgcn_sched_group_barrier(kMatrix, CT, 0);
+      __builtin_amdgcn_sched_group_barrier(kReadLds, 1, 0);
+    }
+    __builtin_amdgcn_sched_group_barrier(kMatrix, CT * AHEAD, 0);
   };
   // O^T += V^T P^T of one half.
   auto weigh = [&](const uint16_t* sV, int h, const u32x4 (&bp)[CT]) __attribute__((always_inline)) {
@@ -394,6 +453,13 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
     }
 #pragma unroll
     for (int c = 0; c < CT; ++c) l[c] = mfma16<H>(ones, bp[c], l[c]);
+    __builtin_amdgcn_sched_group_barrier(kReadLds, 8, 0);  // (four fragments ahead)
+#pragma unroll
+    for (int i = 0; i < DT - 4; ++i) {
+      __builtin_amdgcn_sched_group_barrier(kMatrix, CT, 0);
+      __builtin_amdgcn_sched_group_barrier(kReadLds, 2, 0);
+    }
+    __builtin_amdgcn_sched_group_barrier(kMatrix, 5 * CT, 0);
   };
 
   int buf = 0, c0 = kbeg;
@@ -560,11 +626,10 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3))) v
   extern __shared__ uint32_t sMask[];
   static_assert(sizeof(uint16_t) * kFewChunk * D >= PART * sizeof(f32x4), "an output fits a tile");
 
-  const Work wk = work_of(a, a.few_qblocks, a.few_nsplit);
+  const Work wk = work_of(a, a.few_qblocks, a.few_nsplit, 16, true);
   if (!wk.ok) return;
-  const PagedReq q = attn_req(a, wk.r);
+  const PagedReq q = wk.q;
   const int rows = q.cnt * a.g, rho0 = wk.qb * 16;
-  if (rho0 >= rows || !few_rows(a, q.cnt)) return;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x & 63;
   const int col = lane & 15, grp = lane >> 4;
   const int i_first = rho0 / a.g, i_last = (min(rho0 + 16, rows) - 1) / a.g;
@@ -743,7 +808,7 @@ __global__ __launch_bounds__(kMergeThreads) void paged_merge_kernel(PagedAttnArg
   if (i >= q.cnt || h >= a.Hq) return;
   const int end = min(q.prefix + q.cnt, a.b.C);
   const bool few = few_rows(a, q.cnt);
-  const int run = few ? run_slots(end, a.few_nsplit, kFewRun) : run_slots(end, a.nsplit, 2 * kChunk);
+  const int run = few ? run_slots(end, a.few_nsplit, kFewRun) : run_slots(end, a.nsplit, a.least);
   if (run >= end) return;
   const int ns = (row_end(a, q, i) + run - 1) / run;
   const size_t qidx = (size_t)t * a.Hq + h;
@@ -832,13 +897,33 @@ PagedPlan plan_paged_attention(int R, int T, int max_rows, int Hq, int Hkv, int 
     return (int)(ns < kMaxSplits ? ns : kMaxSplits);
   };
   p.few_nsplit = p.few ? runs(pairs * p.few_qblocks, 8 * cus, kFewRun) : 1;
-  p.few_blocks = p.few ? (pairs * p.few_nsplit + kXcds - 1) / kXcds * kXcds * p.few_qblocks : 0;
+  // workgroups for n row blocks of every (kv head, run) (work_of)
+  const auto blocks = [&](long long n, int nsplit) {
+    const long long pairs = (long long)Hkv * nsplit;
+    return pairs < kXcds && kXcds % pairs == 0 ? (n * pairs + kXcds - 1) / kXcds * kXcds : n * pairs;
+  };
+  // row blocks that can hold rows: all of a request's, or by the rows there are
+  const auto some = [&](long long each, int rows) {
+    const long long by_rows = (long long)T * g / rows + R;
+    return R <= 64 && by_rows < each * R ? by_rows : each * R;
+  };
+  p.few_blocks = p.few ? blocks(some(p.few_qblocks, 16), p.few_nsplit) : 0;
   const long long qb = (most + kRowsPerBlock - 1) / kRowsPerBlock;
   p.qblocks = (int)qb;
-  // row blocks that can hold rows: all of a request's, or by the rows there are
-  const long long some = (long long)T * g / kRowsPerBlock + R;
-  p.nsplit = many ? runs(Hkv * (some < qb * R ? some : qb * R), cus / 2, 2 * kChunk) : 1;
-  p.blocks = many ? (pairs * p.nsplit + kXcds - 1) / kXcds * kXcds * qb : 0;
+  const long long base = Hkv * some(qb, kRowsPerBlock);
+  p.least = 2 * kChunk;
+  // (a workgroup for each compute unit: 4 trees of 64 nodes, 1000 to 4000 slots, 57 us
+  // with half of that, 40; a chunk of 512 rows over 4000 slots 95, 66)
+  p.nsplit = many ? runs(base, cus, p.least) : 1;
+  // Long and short requests side by side: the long ones' chains of chunks last longest,
+  // so those of more than 1024 slots are cut (24 requests of 1 to 700 rows, one of 3000
+  // slots, heads of 64: 71 us uncut, 60 with runs of 512, 48; 12 requests of 1 to 500
+  // rows, 2000 slots, heads of 128: 39, 55, 42).
+  if (many && p.few && base < 4 * cus && p.nsplit < 4) {
+    p.least = 1024;
+    p.nsplit = runs(1, 4, p.least);
+  }
+  p.blocks = many ? blocks(some(qb, kRowsPerBlock), p.nsplit) : 0;
   p.parts = p.nsplit > 1 ? (size_t)p.nsplit * T * Hq : 0;
   p.few_parts = p.few_nsplit > 1 ? (size_t)p.few_nsplit * pairs * p.few_stride : 0;
   const size_t parts = p.parts + p.few_parts;
@@ -850,6 +935,7 @@ hipError_t launch_paged_attention(PagedAttnArgs a, const PagedPlan& p, int D, bo
                                   void* workspace, hipStream_t stream) {
   a.qblocks = p.qblocks;
   a.nsplit = p.nsplit;
+  a.least = p.least;
   a.few = p.few;
   a.few_qblocks = p.few_qblocks;
   a.few_nsplit = p.few_nsplit;
