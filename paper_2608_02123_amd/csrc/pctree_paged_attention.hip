@@ -34,6 +34,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <algorithm>
+
 #include "pctree_lds.h"
 #include "pctree_paged.h"
 #include "pctree_tile.h"
@@ -896,7 +898,11 @@ PagedPlan plan_paged_attention(int R, int T, int max_rows, int Hq, int Hkv, int 
     ns = ns < units ? ns : units;
     return (int)(ns < kMaxSplits ? ns : kMaxSplits);
   };
-  p.few_nsplit = p.few ? runs(pairs * p.few_qblocks, 8 * cus, kFewRun) : 1;
+  // Runs for six workgroups a compute unit, at most 12 of a request, which the merge
+  // reads in two steps (us at 32, 16, 12, 8 runs at most: 8 single tokens of 500 to 4000
+  // slots 31, 25, 25, 23; 40 of one kv head and up to 8000 slots 30, 22, 25, 27; 64 tokens
+  // of eight heads have 3 runs each, 150, and 165 with 2).
+  p.few_nsplit = p.few ? std::min(runs(pairs * p.few_qblocks, 6 * cus, kFewRun), 12) : 1;
   // workgroups for n row blocks of every (kv head, run) (work_of)
   const auto blocks = [&](long long n, int nsplit) {
     const long long pairs = (long long)Hkv * nsplit;

@@ -572,17 +572,19 @@ _HALVES = {torch.bfloat16: BF16, torch.float16: F16}
 
 
 class _Here:
-    """The calls' device and stream: the tensors' device, and its current stream or
-    the one that is passed (what a call allocates is then that stream's)."""
+    """The calls' device and stream: device ``idx`` (an int, which is compared in a
+    tenth of a device object's time), and its current stream or the one that is passed
+    (what a call allocates is then that stream's)."""
+    __slots__ = ("ctx",)
 
-    def __init__(self, t, stream):
+    def __init__(self, idx, stream):
         self.ctx = None
         if stream is not None:
-            if stream.device != t.device:
-                raise ValueError(f"the stream is one of {stream.device}, the tensors of {t.device}")
+            if stream.device.index != idx:
+                raise ValueError(f"the stream is one of {stream.device}, the tensors of cuda:{idx}")
             self.ctx = torch.cuda.stream(stream)
-        elif t.is_cuda and t.device.index != torch.cuda.current_device():
-            self.ctx = torch.cuda.device(t.device)
+        elif idx != torch.cuda.current_device():
+            self.ctx = torch.cuda.device(idx)
 
     def __enter__(self):
         if self.ctx is not None:
@@ -594,12 +596,13 @@ class _Here:
             self.ctx.__exit__(*exc)
 
 
-def _device_tensor(name, t, dtype, shape, device=None):
-    if not isinstance(t, torch.Tensor) or t.dtype != dtype:
+def _device_tensor(name, t, dtype, shape, idx):
+    """``t`` must be a contiguous tensor of that type and shape on device ``idx``."""
+    if not isinstance(t, torch.Tensor) or t.dtype is not dtype:
         raise TypeError(f"{name} must be a {dtype} tensor")
-    if not t.is_cuda or (device is not None and t.device != device):
+    if t.get_device() != idx or idx < 0:
         raise ValueError(f"{name} must be on the device of the other tensors")
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
@@ -620,47 +623,53 @@ class PagedBatch:
         if not isinstance(page_table, torch.Tensor) or page_table.dim() != 2:
             raise ValueError("page_table must be an [R][max_pages] tensor")
         R, W = page_table.shape
+        self.idx = page_table.get_device()
         for name, t, shp in (("page_table", page_table, (R, W)), ("row_start", row_start, (R,)),
                              ("row_count", row_count, (R,)), ("prefix_len", prefix_len, (R,))):
-            _device_tensor(name, t, torch.int32, shp, page_table.device)
+            _device_tensor(name, t, torch.int32, shp, self.idx)
         self.requests, self.max_pages, self.rows = R, W, int(rows)
         self.max_rows = self.rows if max_rows is None else int(max_rows)
         self.device = page_table.device
         self._keep = (row_start, row_count, prefix_len, page_table)
-        self._c = _PagedBatch(*(t.data_ptr() for t in self._keep), R, W, self.rows, self.max_rows)
-
-    @property
-    def sizes(self):
-        return self.requests, self.max_pages, self.rows, self.max_rows
+        self.sizes = self.requests, self.max_pages, self.rows, self.max_rows
+        self._c = _PagedBatch(*(t.data_ptr() for t in self._keep), *(R, W, self.rows, self.max_rows))
+        self._ref = ctypes.byref(self._c)
 
 
-def _paged_cache(k, v, device):
+def _paged_cache(k, v, idx):
     """The C view of one layer's pages [pages][Hkv][page_size][D]; the pages may lie
     apart (stride 0 is free, the same for both)."""
     for name, t in (("k_cache", k), ("v_cache", v)):
         if not isinstance(t, torch.Tensor) or t.dtype not in _HALVES:
             raise TypeError(f"{name} must be a bfloat16 or float16 tensor")
-        if t.dim() != 4 or not t.is_cuda or t.device != device:
-            raise ValueError(f"{name} must be a [pages][Hkv][page_size][D] tensor on {device}")
-    if k.shape != v.shape or k.dtype != v.dtype or (k.shape[0] > 1 and k.stride(0) != v.stride(0)):
+        if t.dim() != 4 or t.get_device() != idx or idx < 0:
+            raise ValueError(f"{name} must be a [pages][Hkv][page_size][D] tensor on the batch's "
+                             "device")
+    pages, Hkv, P, D = shape = k.shape
+    ks, vs = k.stride(), v.stride()
+    if shape != v.shape or k.dtype is not v.dtype or (pages > 1 and ks[0] != vs[0]):
         raise ValueError("k_cache and v_cache must have one shape, type and page stride")
-    pages, Hkv, P, D = k.shape
-    for t in (k, v):
-        if not t[0].is_contiguous():
-            raise ValueError("a page's [Hkv][page_size][D] must be contiguous")
-    stride = k.stride(0) if pages > 1 else Hkv * P * D
-    return _PagedCache(k.data_ptr(), v.data_ptr(), stride, pages, P, Hkv, D, _HALVES[k.dtype])
+    inner = (P * D, D, 1)
+    if (ks[1:] != inner and not k[0].is_contiguous()) or \
+            (vs[1:] != inner and not v[0].is_contiguous()):
+        raise ValueError("a page's [Hkv][page_size][D] must be contiguous")
+    return _PagedCache(k.data_ptr(), v.data_ptr(), ks[0] if pages > 1 else Hkv * P * D, pages, P,
+                       Hkv, D, _HALVES[k.dtype])
 
 
-def _row_tensor(name, t, T, D, dtype, device):
-    """Row stride of a [T][heads][D] tensor whose rows may lie apart."""
-    if not isinstance(t, torch.Tensor) or t.dtype != dtype:
+def _row_tensor(name, t, T, D, dtype, idx):
+    """Row stride of a [T][heads][D] tensor whose rows may lie apart, and its heads."""
+    if not isinstance(t, torch.Tensor) or t.dtype is not dtype:
         raise TypeError(f"{name} must be a {dtype} tensor")
-    if t.dim() != 3 or t.shape[0] != T or t.shape[2] != D or not t.is_cuda or t.device != device:
-        raise ValueError(f"{name} must be a [{T}][heads][{D}] tensor on {device}")
-    if not t[0].is_contiguous():
+    if t.dim() != 3 or t.get_device() != idx:
+        raise ValueError(f"{name} must be a [{T}][heads][{D}] tensor on the batch's device")
+    rows, heads, d = t.shape
+    if rows != T or d != D:
+        raise ValueError(f"{name} must be a [{T}][heads][{D}] tensor, got {tuple(t.shape)}")
+    st = t.stride()
+    if (st[1] != D or st[2] != 1) and not t[0].is_contiguous():
         raise ValueError(f"a row of {name} must be contiguous")
-    return t.stride(0) if T > 1 else t.shape[1] * D
+    return (st[0] if T > 1 else heads * D), heads
 
 
 def rope_table(positions, rot_dim, theta=10000.0, device="cuda"):
@@ -683,39 +692,41 @@ def append_paged(batch, k_cache, v_cache, k, v, q=None, *, q_norm=None, k_norm=N
     [T]`` (a row's slot if not given); keys and values go to the rows' slots.
     Returns the normed and rotated q in ``q_out`` (a new tensor if not given; rows
     of no request are not written)."""
-    dev, T = batch.device, batch.rows
-    c = _paged_cache(k_cache, v_cache, dev)
+    idx, T = batch.idx, batch.rows
+    c = _paged_cache(k_cache, v_cache, idx)
     dt, D = k_cache.dtype, c.head_dim
-    ks, vs = _row_tensor("k", k, T, D, dt, dev), _row_tensor("v", v, T, D, dt, dev)
-    if k.shape[1] != c.kv_heads or v.shape[1] != c.kv_heads:
+    ks, kh = _row_tensor("k", k, T, D, dt, idx)
+    vs, vh = _row_tensor("v", v, T, D, dt, idx)
+    if kh != c.kv_heads or vh != kh:
         raise ValueError(f"k and v must have the cache's {c.kv_heads} heads")
-    for name, w in (("q_norm", q_norm), ("k_norm", k_norm)):
-        if w is not None:
-            _device_tensor(name, w, dt, (D,), dev)
+    if q_norm is not None:
+        _device_tensor("q_norm", q_norm, dt, (D,), idx)
+    if k_norm is not None:
+        _device_tensor("k_norm", k_norm, dt, (D,), idx)
     if position is not None:
-        _device_tensor("position", position, torch.int32, (T,), dev)
+        _device_tensor("position", position, torch.int32, (T,), idx)
     rot = npos = 0
     if rope is not None:
         if not isinstance(rope, torch.Tensor) or rope.dim() != 2:
             raise ValueError("rope must be a [positions][rot_dim] tensor")
         npos, rot = rope.shape
-        _device_tensor("rope", rope, torch.float32, (npos, rot), dev)
+        _device_tensor("rope", rope, torch.float32, (npos, rot), idx)
     if q is None and (q_out is not None or q_norm is not None):
         raise ValueError("q_out and q_norm go with q")
-    with _Here(k_cache, stream) as st:
+    with _Here(idx, stream) as st:
         qs = os_ = Hq = 0
         if q is not None:
-            qs, Hq = _row_tensor("q", q, T, D, dt, dev), q.shape[1]
+            qs, Hq = _row_tensor("q", q, T, D, dt, idx)
             if q_out is None:
-                q_out = torch.empty((T, Hq, D), dtype=dt, device=dev)
-            os_ = _row_tensor("q_out", q_out, T, D, dt, dev)
-            if q_out.shape != q.shape:
+                q_out = torch.empty((T, Hq, D), dtype=dt, device=q.device)
+            os_, oh = _row_tensor("q_out", q_out, T, D, dt, idx)
+            if oh != Hq:
                 raise ValueError("q_out must have q's shape")
-        a = _Append(_ptr(q), _ptr(k), _ptr(v), _ptr(q_out), qs, ks, vs, os_, _ptr(q_norm),
-                    _ptr(k_norm), _ptr(rope), _ptr(position), eps, Hq, rot, npos,
+        a = _Append(_ptr(q), k.data_ptr(), v.data_ptr(), _ptr(q_out), qs, ks, vs, os_,
+                    _ptr(q_norm), _ptr(k_norm), _ptr(rope), _ptr(position), eps, Hq, rot, npos,
                     1 if interleaved else 0)
-        _check(lib().pctree_append_paged(ctypes.byref(c), ctypes.byref(batch._c), ctypes.byref(a),
-                                         st), "pctree_append_paged")
+        status = lib().pctree_append_paged(ctypes.byref(c), batch._ref, ctypes.byref(a), st)
+    _check(status, "pctree_append_paged")
     return q_out
 
 
@@ -731,45 +742,47 @@ class PagedAttention:
         c = _PagedCache(None, None, kv_heads * page_size * head_dim, 1, page_size, kv_heads,
                         head_dim, BF16)
         self.ws_bytes = int(lib().pctree_paged_attention_workspace_bytes(
-            ctypes.byref(c), ctypes.byref(batch._c), q_heads))
+            ctypes.byref(c), batch._ref, q_heads))
+        self.idx = batch.idx
         self.workspace = torch.empty(max(self.ws_bytes, 1), dtype=torch.uint8,
                                      device=batch.device)
+        self._ws = self.workspace.data_ptr()
 
     def __call__(self, q, k_cache, v_cache, batch, mask=None, out=None, stream=None):
         """``q [T][Hq][D]`` over ``k_cache, v_cache [pages][Hkv][page_size][D]``; causal, or
         with ``mask`` (:func:`build_mask`) the tree's.  Returns ``out [T][Hq][D]``
         (rows of no request are not written)."""
-        dev = self.workspace.device
-        if batch.sizes != self.sizes or batch.device != dev:
+        idx = self.idx
+        if batch.sizes != self.sizes or batch.idx != idx:
             raise ValueError("the batch is not of this object's sizes")
-        c = _paged_cache(k_cache, v_cache, dev)
-        if (c.kv_heads, c.head_dim, c.page_size) != (self.kv_heads, self.head_dim,
-                                                     self.page_size):
+        c = _paged_cache(k_cache, v_cache, idx)
+        if c.kv_heads != self.kv_heads or c.head_dim != self.head_dim or \
+                c.page_size != self.page_size:
             raise ValueError("the pages are not of this object's sizes")
         shp = (batch.rows, self.q_heads, self.head_dim)
-        _device_tensor("q", q, k_cache.dtype, shp, dev)
+        _device_tensor("q", q, k_cache.dtype, shp, idx)
         budget = 0
         if mask is not None:
             if mask.dtype != torch.int32 and mask.dtype != torch.uint32:
                 raise TypeError("mask must be the [R][N][(N+31)/32] words of build_mask")
             budget = mask.shape[1] if mask.dim() == 3 else 0
             _device_tensor("mask", mask, mask.dtype,
-                           (batch.requests, budget, (budget + 31) // 32), dev)
+                           (batch.requests, budget, (budget + 31) // 32), idx)
         if out is not None:
-            _device_tensor("out", out, k_cache.dtype, shp, dev)
-        with _Here(q, stream) as st:
+            _device_tensor("out", out, k_cache.dtype, shp, idx)
+        with _Here(idx, stream) as st:
             if out is None:
-                out = torch.empty(shp, dtype=q.dtype, device=dev)
-            _check(lib().pctree_paged_attention(
-                ctypes.byref(c), ctypes.byref(batch._c), _ptr(q), self.q_heads, self.scale,
-                _ptr(mask), budget, _ptr(out), _ptr(self.workspace), self.ws_bytes, st),
-                "pctree_paged_attention")
+                out = torch.empty(shp, dtype=q.dtype, device=q.device)
+            status = lib().pctree_paged_attention(
+                ctypes.byref(c), batch._ref, q.data_ptr(), self.q_heads, self.scale, _ptr(mask),
+                budget, out.data_ptr(), self._ws, self.ws_bytes, st)
+        _check(status, "pctree_paged_attention")
         return out
 
 
 def paged_attention(q, k_cache, v_cache, batch, mask=None, scale=None, out=None, stream=None):
     """One call of :class:`PagedAttention`."""
-    with _Here(k_cache, stream):
+    with _Here(batch.idx, stream):
         layer = PagedAttention(batch, q.shape[1], k_cache.shape[1], k_cache.shape[3],
                                k_cache.shape[2], scale)
         return layer(q, k_cache, v_cache, batch, mask=mask, out=out)
@@ -782,25 +795,27 @@ def compact_paged(pool, page_table, prefix_len, accept_node, accept_len, budget,
     the dimensions past ``page_size`` form a slot of a head, a multiple of 16 bytes;
     groups and pages may lie apart."""
     if not isinstance(pool, torch.Tensor) or not pool.is_cuda or pool.dim() < 5 or \
-            not pool[0, 0].is_contiguous():
+            not (pool.is_contiguous() or pool[0, 0].is_contiguous()):
         raise ValueError("pool must be a [groups][pages][heads][page_size][...] device tensor "
                          "with contiguous pages")
-    G, pages, heads, P = pool.shape[:4]
+    G, pages, heads, P = shape = pool.shape[:4]
+    idx = pool.get_device()
     R, W = accept_node.shape
-    dev = pool.device
-    _device_tensor("page_table", page_table, torch.int32, (R, page_table.shape[-1]), dev)
-    _device_tensor("accept_node", accept_node, torch.int32, (R, W), dev)
-    _device_tensor("prefix_len", prefix_len, torch.int32, (R,), dev)
-    _device_tensor("accept_len", accept_len, torch.int32, (R,), dev)
+    _device_tensor("page_table", page_table, torch.int32, (R, page_table.shape[-1]), idx)
+    _device_tensor("accept_node", accept_node, torch.int32, (R, W), idx)
+    _device_tensor("prefix_len", prefix_len, torch.int32, (R,), idx)
+    _device_tensor("accept_len", accept_len, torch.int32, (R,), idx)
     es = pool.element_size()
     slot = math.prod(pool.shape[4:]) * es
-    page_stride = pool.stride(1) * es if pages > 1 else heads * P * slot
-    group_stride = pool.stride(0) * es if G > 1 else 0
-    with _Here(pool, stream) as st:
-        _check(lib().pctree_compact_paged(
-            _ptr(pool), group_stride, page_stride, G, pages, heads, P, slot, _ptr(page_table),
-            page_table.shape[1], _ptr(prefix_len), _ptr(accept_node), _ptr(accept_len), R, budget,
-            W - 1, st), "pctree_compact_paged")
+    stride = pool.stride()
+    page_stride = stride[1] * es if pages > 1 else heads * P * slot
+    group_stride = stride[0] * es if G > 1 else 0
+    with _Here(idx, stream) as st:
+        status = lib().pctree_compact_paged(
+            pool.data_ptr(), group_stride, page_stride, *shape, slot, page_table.data_ptr(),
+            page_table.shape[1], prefix_len.data_ptr(), accept_node.data_ptr(),
+            accept_len.data_ptr(), R, budget, W - 1, st)
+    _check(status, "pctree_compact_paged")
     return pool
 
 
@@ -818,6 +833,7 @@ class Sampler:
             _check(lib().pctree_sample(None, F32, rows, vocab, vocab, *([None] * 8), 0, None),
                    "sizes")
         self.workspace = torch.empty(nb, dtype=torch.uint8, device=device)
+        self.idx, self._ws, self._nb = self.workspace.get_device(), self.workspace.data_ptr(), nb
 
     def __call__(self, logits, uniform, *, temperature=None, top_k=None, top_p=None, min_p=None,
                  token=None, logprob=None, stream=None):
@@ -825,33 +841,41 @@ class Sampler:
         apart) from ``uniform [T]`` in [0, 1).  ``temperature``, ``top_p``, ``min_p``
         (float32) and ``top_k`` (int32) are ``[T]`` or None; see include/pctree.h.
         Returns ``(token [T] int32, logprob [T] float32)``."""
-        dev = self.workspace.device
+        idx = self.idx
         if not isinstance(logits, torch.Tensor) or logits.dtype not in _LOGITS:
             raise TypeError("logits must be a float32, bfloat16 or float16 tensor")
-        if logits.dim() != 2 or logits.device != dev or logits.shape[1] != self.vocab or \
+        if logits.dim() != 2 or logits.get_device() != idx or logits.shape[1] != self.vocab or \
                 not 1 <= logits.shape[0] <= self.rows:
-            raise ValueError(f"logits must be a [T][{self.vocab}] tensor on {dev}, T at most "
-                             f"{self.rows}")
+            raise ValueError(f"logits must be a [T][{self.vocab}] tensor on {self.workspace.device}"
+                             f", T at most {self.rows}")
         T, V = logits.shape
-        if (V > 1 and logits.stride(1) != 1) or (T > 1 and logits.stride(0) < V):
+        stride = logits.stride()
+        if (V > 1 and stride[1] != 1) or (T > 1 and stride[0] < V):
             raise ValueError("a row of logits must be contiguous, rows must not overlap")
-        for name, t, dt in (("uniform", uniform, torch.float32),
-                            ("temperature", temperature, torch.float32),
-                            ("top_k", top_k, torch.int32), ("top_p", top_p, torch.float32),
-                            ("min_p", min_p, torch.float32), ("token", token, torch.int32),
-                            ("logprob", logprob, torch.float32)):
-            if t is not None or name == "uniform":
-                _device_tensor(name, t, dt, (T,), dev)
-        with _Here(logits, stream) as st:
+        one = (T,)
+        _device_tensor("uniform", uniform, torch.float32, one, idx)
+        if temperature is not None:
+            _device_tensor("temperature", temperature, torch.float32, one, idx)
+        if top_k is not None:
+            _device_tensor("top_k", top_k, torch.int32, one, idx)
+        if top_p is not None:
+            _device_tensor("top_p", top_p, torch.float32, one, idx)
+        if min_p is not None:
+            _device_tensor("min_p", min_p, torch.float32, one, idx)
+        if token is not None:
+            _device_tensor("token", token, torch.int32, one, idx)
+        if logprob is not None:
+            _device_tensor("logprob", logprob, torch.float32, one, idx)
+        with _Here(idx, stream) as st:
             if token is None:
-                token = torch.empty(T, dtype=torch.int32, device=dev)
+                token = torch.empty(T, dtype=torch.int32, device=logits.device)
             if logprob is None:
-                logprob = torch.empty(T, dtype=torch.float32, device=dev)
-            _check(lib().pctree_sample(
-                _ptr(logits), _LOGITS[logits.dtype], T, V, logits.stride(0) if T > 1 else V,
-                _ptr(uniform), _ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p),
-                _ptr(token), _ptr(logprob), _ptr(self.workspace), self.workspace.numel(), st),
-                "pctree_sample")
+                logprob = torch.empty(T, dtype=torch.float32, device=logits.device)
+            status = lib().pctree_sample(
+                logits.data_ptr(), _LOGITS[logits.dtype], T, V, stride[0] if T > 1 else V,
+                uniform.data_ptr(), _ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p),
+                token.data_ptr(), logprob.data_ptr(), self._ws, self._nb, st)
+        _check(status, "pctree_sample")
         return token, logprob
 
 
@@ -859,7 +883,7 @@ def sample(logits, uniform, *, temperature=None, top_k=None, top_p=None, min_p=N
     """One call of :class:`Sampler`."""
     if not isinstance(logits, torch.Tensor) or logits.dim() != 2 or not logits.is_cuda:
         raise ValueError("logits must be a [T][V] device tensor")
-    with _Here(logits, stream):
+    with _Here(logits.get_device(), stream):
         return Sampler(*logits.shape, device=logits.device)(
             logits, uniform, temperature=temperature, top_k=top_k, top_p=top_p, min_p=min_p)
 

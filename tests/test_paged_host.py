@@ -144,8 +144,8 @@ def test_binding_refuses_host_tensors_and_wrong_shapes():
         P.rope_table(10, 24, device="cpu")
     k = torch.zeros(4, 2, 16, 128, dtype=torch.bfloat16)
     with pytest.raises(ValueError):
-        P._paged_cache(k, k, torch.device("cuda:0"))
+        P._paged_cache(k, k, 0)
     with pytest.raises(TypeError):
-        P._paged_cache(k.float(), k.float(), torch.device("cpu"))
+        P._paged_cache(k.float(), k.float(), 0)
     with pytest.raises(ValueError):
         P.compact_paged(torch.zeros(2, 4, 2, 16, 64), i, i, torch.zeros(3, 5, dtype=torch.int32), i, 8)
