@@ -189,6 +189,56 @@ def test_mixed_rows():
     run_attention(b, 14, 2, 64, 32, torch.float16)
 
 
+@pytest.mark.parametrize("R,Hq,Hkv,D", [(70, 4, 2, 64), (130, 2, 1, 128), (64, 6, 3, 64), (65, 5, 5, 128)])
+def test_many_requests(R, Hq, Hkv, D):
+    """More requests than a wave has lanes, and kv heads that do not divide the XCDs."""
+    rng = np.random.default_rng((R, Hkv))
+    rows = rng.choice([0, 1, 1, 1, 2, 5], R)
+    rows[3] = 40
+    b = make_batch(rng, rows, rng.integers(0, 300, R), 16)
+    run_attention(b, Hq, Hkv, D, 16, torch.bfloat16)
+
+
+@pytest.mark.parametrize("Hq,Hkv,D", [(4, 1, 64), (6, 3, 64), (8, 4, 128)])
+def test_long_runs_beside_single_tokens(Hq, Hkv, D):
+    """A mixed batch whose long requests are cut into runs, in both kernels."""
+    rng = np.random.default_rng(Hkv)
+    rows = [1, 40, 1, 1, 150, 2, 1, 1, 30, 1, 1]
+    ctx = [2900, 2100, 3, 700, 1500, 1030, 0, 64, 10, 1999, 128]
+    b = make_batch(rng, rows, ctx, 32)
+    run_attention(b, Hq, Hkv, D, 32, torch.bfloat16, poison=False)
+
+
+@pytest.mark.parametrize("page", [2, 4, 8, 32])
+def test_long_chunk_in_small_pages(page):
+    rng = np.random.default_rng(page)
+    b = make_batch(rng, [200], [600], page)
+    b["page_table"][0, 40 // page] = -1
+    run_attention(b, 4, 2, 128, page, torch.bfloat16, poison=False)
+
+
+def test_growing_scores():
+    """Keys ordered so that a row's scores grow all along: the softmax reference has to
+    follow, by small and by large steps."""
+    rng = np.random.default_rng(31)
+    for dt in DTYPES:
+        for step in (0.002, 0.05, 0.5):
+            b = make_batch(rng, [40], [700], 64)
+            g = _gen(1)
+            q = torch.ones(40, 2, 128, dtype=dt, device="cuda")
+            k = torch.zeros(b["pages"], 2, 64, 128, dtype=dt, device="cuda")
+            for s in range(740):
+                p, o = PO.place(b, 0, s, 64, b["pages"])
+                k[p, :, o] = s * step / 128
+            v = torch.randn(b["pages"], 2, 64, 128, generator=g).to(dt).cuda()
+            out = P.paged_attention(q, k, v, dev_batch(b), scale=1.0)
+            # (|q k| sums up to 370 here: the score bound of the file's head, times 8)
+            ref = PO.attention(b, _np(q), _np(k), _np(v), 1.0)
+            for t, (o, mag) in ref.items():
+                tol = HALF[dt] * (mag + np.abs(o)) + 2.0 ** -7 * mag + 2.0 ** -25
+                assert (np.abs(_np(out[t]) - o) <= tol).all(), (dt, step, t)
+
+
 def test_rows_that_admit_nothing_are_zero():
     """An empty mask row without a prefix, and a request whose pages are all missing."""
     rng = np.random.default_rng(4)
@@ -496,6 +546,72 @@ def test_graph_replays():
         torch.cuda.synchronize()
         for a, b in zip(got, (out, kc, vc)):
             assert torch.equal(a, b), f"replay {i}"
+
+
+def test_a_verification_step_as_it_is_used():
+    """A drafted tree through the target's step and on: rows appended with norm and
+    rotation, tree attention over pages, a token sampled at every node, greedy walk,
+    compaction; then the next token's row over the compacted pages.  The pages must
+    then be those of a plain decoding of the accepted tokens."""
+    from paper_2608_02123_amd.synth import CONFIGS, make_inputs
+    w = CONFIGS["tiny"]
+    builder = P.TreeBuilder(w.V, w.B, w.N, w.k, w.r, w.R, P.F32)
+    inp = P.device_inputs(make_inputs(w))
+    tree = builder.run(**inp, check=True)
+    N, Hq, Hkv, D, page = w.N, 8, 2, 128, 16
+    g = _gen(77)
+    emb = torch.randn(w.V, (Hq + 2 * Hkv) * D, generator=g).to(torch.bfloat16).cuda()
+    head = (torch.randn(Hq * D, w.V, generator=g) * 0.3).cuda()
+    wn = (1 + 0.1 * torch.randn(D, generator=g)).to(torch.bfloat16).cuda()
+    rope = P.rope_table(1200, D)
+    prefix = int(inp["prefix_len"][0])
+    pages = (prefix + N + page) // page + 2
+    table = torch.randperm(pages, generator=g).to(torch.int32)[None].cuda()
+    pool = torch.randn(2, pages, Hkv, page, D, generator=g).to(torch.bfloat16).cuda()
+
+    def one(x):
+        return torch.tensor([x], dtype=torch.int32, device="cuda")
+
+    def rows(tokens):
+        q, k, v = emb[tokens.long()].split([Hq * D, Hkv * D, Hkv * D], 1)
+        return [x.unflatten(1, (-1, D)) for x in (q, k, v)]
+
+    bt = P.PagedBatch(one(0), tree["count"], inp["prefix_len"], table, N)
+    q, k, v = rows(tree["token"][0])
+    q = P.append_paged(bt, pool[0], pool[1], k, v, q=q, q_norm=wn, k_norm=wn, rope=rope, position=tree["position"][0])
+    out = P.PagedAttention(bt, Hq, Hkv, D, page)(q, pool[0], pool[1], bt, mask=tree["mask"])
+    logits = out.float().flatten(1) @ head
+    # (so that something is accepted: each node's target likes one of its children)
+    par = tree["parent"][0].cpu().numpy()
+    for i in range(1, N):
+        logits[par[i], int(tree["token"][0, i])] += 40.0 + i
+    u = torch.rand(N, generator=g).cuda()
+    target, _ = P.sample(logits, u, top_k=torch.full((N,), 20, dtype=torch.int32, device="cuda"))
+    rws, nrows = P.build_retrieve(tree["parent"], tree["count"], w.B)
+    acc = P.accept_greedy(tree["token"], rws, nrows, target[None])
+    P.compact_paged(pool, table, inp["prefix_len"], acc["accept_node"], acc["accept_len"], N)
+    n = int(acc["accept_len"][0])
+    assert n > 0
+    nodes = acc["accept_node"][0, :n + 1].long()
+    tokens = tree["token"][0][nodes]
+    # the accepted tokens, decoded one after the other into fresh pages
+    plain = pool.clone()
+    for s in range(n + 1):
+        p, o = int(table[0, (prefix + s) // page]), (prefix + s) % page
+        plain[:, p, :, o] = 0
+    for s in range(n + 1):
+        b1 = P.PagedBatch(one(0), one(1), one(prefix + s), table, 1)
+        _, k, v = rows(tokens[s:s + 1])
+        P.append_paged(b1, plain[0], plain[1], k, v, k_norm=wn, rope=rope)
+    assert torch.equal(plain, pool)
+    # the bonus token's row
+    b1 = P.PagedBatch(one(0), one(1), one(prefix + n + 1), table, 1)
+    q, k, v = rows(acc["bonus"])
+    q = P.append_paged(b1, pool[0], pool[1], k, v, q=q, q_norm=wn, k_norm=wn, rope=rope)
+    out = P.paged_attention(q, pool[0], pool[1], b1)
+    host = {"row_start": np.array([0]), "row_count": np.array([1]), "prefix_len": np.array([prefix + n + 1]),
+            "page_table": table.cpu().numpy(), "rows": 1, "max_rows": 1, "pages": pages}
+    check_attention(host, q, pool[0], pool[1], out, D ** -0.5)
 
 
 def test_results_repeat():
