@@ -33,12 +33,15 @@ struct SampleArgs {
   float* gmax;     // [T][ng] maxima of groups of 8 << gshift elements
   double* bmass;   // [T][nb] weights of blocks of 512 elements ...
   float* bref;     // [T][nb] ... relative to this logit
-  unsigned long long* hist;  // [T][bins] weights of open rows (null: none are deferred)
+  unsigned long long* hist;  // [T][bins] weights of open rows (null: no row can be open)
   unsigned long long* list;  // [T][list] keys of an open row's border bin
   OpenRow* open;             // [T]
+  int* open_n;               // how many rows are left by their histograms, ...
+  int* open_rows;            // [T] ... and which
   long long row_stride;
   int T, V;
   int ng, nb, gshift;
+  bool bins;       // open rows have histograms
 };
 
 // Groups and blocks of a row of V logits at any alignment, and the workspace of T rows.

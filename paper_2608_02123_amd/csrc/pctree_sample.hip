@@ -28,12 +28,13 @@
 // weight, mark_kernel finds the bin in which top_p is reached, sums each block's
 // weights above it and lists the bin's own logits, and finish_kernel cuts that list
 // and draws.  One workgroup could do it alone (whole_row; it does for calls of few
-// rows, and where the list does not do), which takes several times as long.
+// rows with a top_k, and where the list does not do), which takes several times as long.
 #include "pctree.h"
 
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <algorithm>
 #include <type_traits>
 
 #include "pctree_sample.h"
@@ -55,6 +56,11 @@ constexpr int kManyParts = 2048;      // ... and where k is more than a quarter 
 constexpr int kMaxBound = 1024;       // the largest k that is bounded so
 constexpr int kTry = 256;             // (top_p alone) the rank of the bound that is tried first
 constexpr int kBins = 2048;           // of 1/64 in log weight
+// A row that filters by weight alone with more groups than this in reach of its bound is
+// left to the open rows' launches at once (up to 768 groups: 512 rows' picks 42 us, 33; they
+// would read as much as those do, one workgroup a row).
+constexpr int kFewGroups = 400;
+constexpr int kOpenGrid = 1024;       // workgroups that share the open rows' items
 constexpr double kBinStep = 0.98449643700540841;  // e^(-1/64)
 constexpr double kLowest = -700.0;    // weights below e^-700 are 0
 constexpr double kLog2e = 1.4426950408889634074;
@@ -343,6 +349,7 @@ __global__ __launch_bounds__(kScanThreads) void scan_kernel(SampleArgs a, int se
   const int t = blockIdx.x / segs, seg = blockIdx.x % segs;
   const int lane = threadIdx.x & 63;
   const int b0 = (seg * (kScanThreads / 64) + threadIdx.x / 64) * BPW;
+  if (a.open_n && blockIdx.x == 0 && threadIdx.x == 0) *a.open_n = 0;
   if (b0 >= a.nb) return;
   const Row row = row_of<DT>(a, t);
   Raw<DT> raw[BPW];
@@ -523,8 +530,9 @@ __device__ __forceinline__ float bound_of(const SampleArgs& a, int j, float mx, 
 
 // Logits >= bound into the list (unordered), as (order, lowest index first);
 // returns how many there are (more than kList: not all are in the list).
+// (More than `most` groups are not looked at: kList + 1.)
 template <int DT>
-__device__ int gather(const SampleArgs& a, const Row& row, float bound, PickShared& sh) {
+__device__ int gather(const SampleArgs& a, const Row& row, float bound, int most, PickShared& sh) {
   constexpr int B = 4;  // units whose loads are in flight together
   if (threadIdx.x == 0) sh.n = sh.groups = 0;
   __syncthreads();
@@ -545,6 +553,7 @@ __device__ int gather(const SampleArgs& a, const Row& row, float bound, PickShar
       if (in >> i & 1) sh.group[at++] = (uint16_t)(i * kPickThreads + threadIdx.x);
   }
   __syncthreads();
+  if (sh.groups > most) return kList + 1;
   const int per = 1 << a.gshift, units = sh.groups << a.gshift;
   for (int i1 = 0; i1 < units; i1 += B * kPickThreads) {
     const int i0 = i1 + threadIdx.x;
@@ -1128,7 +1137,7 @@ __device__ __noinline__ void whole_row(const SampleArgs& a, int t, const Row& ro
 template <int DT>
 __device__ void pick_largest(const SampleArgs& a, int t, const Row& row, float mx,
                              PickShared& sh) {
-  const int n = gather<DT>(a, row, mx, sh);  // the largest and its equals
+  const int n = gather<DT>(a, row, mx, kMaxGroups, sh);  // the largest and its equals
   uint64_t best = 0;
   for (int i = threadIdx.x; i < min(n, kList); i += kPickThreads)
     best = best > sh.l.list[i] ? best : sh.l.list[i];
@@ -1275,7 +1284,9 @@ __global__ __launch_bounds__(kPickThreads) __attribute__((amdgpu_waves_per_eu(4)
       bound = bound_of(a, min(a.ng, kTry), mx, sh);
     }
     const bool list = bnd || all_in || q.k == 0;  // (else a top_k beyond the bounds)
-    const int n = list ? gather<DT>(a, row, bound, sh) : kList + 1;
+    // (rows that the launches after this one can take are left to them early)
+    const int most = DEFER && a.bins && q.k == 0 && !all_in ? kFewGroups : kMaxGroups;
+    const int n = list ? gather<DT>(a, row, bound, most, sh) : kList + 1;
     if (n <= 64) {
       if (pick_of_64(a, t, q, mx, n, !bnd && !all_in ? total : 0.0, sh)) return;
     } else if (n <= kList) {
@@ -1308,10 +1319,12 @@ __global__ __launch_bounds__(kPickThreads) __attribute__((amdgpu_waves_per_eu(4)
       }
     }
     if constexpr (DEFER) {
-      const bool by_bins = q.k == 0;
+      const bool by_bins = a.bins && q.k == 0;
       if (by_bins)
-        for (int i = threadIdx.x; i < kBins; i += kPickThreads) a.hist[(size_t)t * kBins + i] = 0;
+        for (int i = threadIdx.x; i < kBins; i += kPickThreads)
+          a.hist[(size_t)t * kBins + i] = 0;
       if (threadIdx.x == 0) {
+        if (by_bins) a.open_rows[atomicAdd(a.open_n, 1)] = t;
         OpenRow o;
         o.state = by_bins ? 1 : 2;
         o.n = 0;
@@ -1320,8 +1333,6 @@ __global__ __launch_bounds__(kPickThreads) __attribute__((amdgpu_waves_per_eu(4)
         o.base = o.limit = 0.0;
         a.open[t] = o;
       }
-    } else {
-      whole_row<DT>(a, t, row, q, mx, sh);
     }
     return;
   }
@@ -1339,192 +1350,203 @@ __global__ __launch_bounds__(kPickThreads) __attribute__((amdgpu_waves_per_eu(4)
 // ---------------------------------------------------------------------------
 
 // The bin of a logit: 1/64 in log weight each, the last takes the rest.  (A bin that
-// top_p is reached in is never the last: what lies below e^-32 of the largest weight
-// is less than 2^20 e^-32, under the 2^-24 that a float top_p stays below 1.)
+// top_p is reached in is never the last: what lies below e^-31.9 of the largest weight
+// is less than 2^20 e^-31.9, under the 2^-24 that a float top_p stays below 1.)
 __device__ __forceinline__ int open_bin(double z) {
   const double x = z * -64.0;
   return x < (double)(kBins - 1) ? (int)x : kBins - 1;
 }
 
+// (Both kernels share the items, segments of open rows, among kOpenGrid workgroups.  A
+// workgroup for each segment of every row would mostly find its row done: 512 rows of
+// all kinds 20 and 39 us, 18 and 34 so.)
 template <int DT, int BPW>
 __global__ __launch_bounds__(kScanThreads) void hist_kernel(SampleArgs a, int segs) {
-  const int t = blockIdx.x / segs, seg = blockIdx.x % segs;
-  if (a.open[t].state != 1) return;
   __shared__ unsigned long long mass[kBins];
-  for (int i = threadIdx.x; i < kBins; i += kScanThreads) mass[i] = 0;
-  const Row row = row_of<DT>(a, t);
-  const Params q = params_of(a, t);
-  if (q.p >= 1.0) return;
-  const float mx = a.open[t].mx;
-  // log weights of at least min_p: all from `floor` on that weigh enough, all from
-  // `floor_sure` on
-  const double lnp = q.min_p > 0.0 ? log(q.min_p) : kLowest;
-  const double floor = fmax(kLowest, lnp - 1e-9);
-  const double floor_sure = q.min_p > 0.0 ? lnp + 1e-9 : kLowest;
-  const int b0 = (seg * (kScanThreads / 64) + threadIdx.x / 64) * BPW;
-  Raw<DT> raw[BPW];
-  load_raws<DT, BPW>(row, b0 * 64, raw);
-  __syncthreads();
+  const int items = *a.open_n * segs;
 #pragma unroll 1
-  for (int i = 0; i < BPW; ++i) {
-    float u[kUnit];
-    unpack<DT>(raw[0], u);
-    next_raw(raw, raw[0]);
-    int bin[kUnit];
-    double w[kUnit];
-    bool in[kUnit], rest = false;
+  for (int item = blockIdx.x; item < items; item += gridDim.x) {
+    const int t = a.open_rows[item / segs], seg = item % segs;
+    for (int i = threadIdx.x; i < kBins; i += kScanThreads) mass[i] = 0;
+    const Row row = row_of<DT>(a, t);
+    const Params q = params_of(a, t);
+    if (q.p >= 1.0) continue;
+    const float mx = a.open[t].mx;
+    // log weights of at least min_p: all from `floor` on that weigh enough, all from
+    // `floor_sure` on
+    const double lnp = q.min_p > 0.0 ? log(q.min_p) : kLowest;
+    const double floor = fmax(kLowest, lnp - 1e-9);
+    const double floor_sure = q.min_p > 0.0 ? lnp + 1e-9 : kLowest;
+    const int b0 = (seg * (kScanThreads / 64) + threadIdx.x / 64) * BPW;
+    Raw<DT> raw[BPW];
+    load_raws<DT, BPW>(row, b0 * 64, raw);
+    __syncthreads();
+#pragma unroll 1
+    for (int i = 0; i < BPW; ++i) {
+      float u[kUnit];
+      unpack<DT>(raw[0], u);
+      next_raw(raw, raw[0]);
+      int bin[kUnit];
+      double w[kUnit];
+      bool in[kUnit], rest = false;
 #pragma unroll
-    for (int e = 0; e < kUnit; ++e) {
-      const double z = u[e] == mx ? 0.0 : z_of(u[e], mx, q.inv_t);
-      in[e] = z >= floor;
-      bin[e] = open_bin(z);
-      rest |= in[e] && (bin[e] == kBins - 1 || z < floor_sure);
-      // e^d, -1/64 < d <= 0, relative to the bin's top: the seventh term of the series
-      // is below 2^-53
-      const double d = __builtin_fma((double)bin[e], 1.0 / 64.0, z);
-      w[e] = 1.0 / 720;
-      w[e] = __builtin_fma(w[e], d, 1.0 / 120);
-      w[e] = __builtin_fma(w[e], d, 1.0 / 24);
-      w[e] = __builtin_fma(w[e], d, 1.0 / 6);
-      w[e] = __builtin_fma(w[e], d, 0.5);
-      w[e] = __builtin_fma(w[e], d, 1.0);
-      w[e] = __builtin_fma(w[e], d, 1.0);
-    }
-    if (__any(rest)) {  // the last bin, and weights next to min_p
-#pragma unroll 1
       for (int e = 0; e < kUnit; ++e) {
-        float v = u[0];
+        const double z = u[e] == mx ? 0.0 : z_of(u[e], mx, q.inv_t);
+        in[e] = z >= floor;
+        bin[e] = open_bin(z);
+        rest |= in[e] && (bin[e] == kBins - 1 || z < floor_sure);
+        // e^d, -1/64 < d <= 0, relative to the bin's top: the first term left
+        // out, d^7 / 5040, is below 2^-54
+        const double d = __builtin_fma((double)bin[e], 1.0 / 64.0, z);
+        w[e] = 1.0 / 720;
+        w[e] = __builtin_fma(w[e], d, 1.0 / 120);
+        w[e] = __builtin_fma(w[e], d, 1.0 / 24);
+        w[e] = __builtin_fma(w[e], d, 1.0 / 6);
+        w[e] = __builtin_fma(w[e], d, 0.5);
+        w[e] = __builtin_fma(w[e], d, 1.0);
+        w[e] = __builtin_fma(w[e], d, 1.0);
+      }
+      if (__any(rest)) {  // the last bin, and weights next to min_p
+#pragma unroll 1
+        for (int e = 0; e < kUnit; ++e) {
+          float v = u[0];
 #pragma unroll
-        for (int j = 1; j < kUnit; ++j) v = e == j ? u[j] : v;
-        const double z = v == mx ? 0.0 : z_of(v, mx, q.inv_t);
-        const bool ok = z >= floor && weight(v, mx, q.inv_t) >= q.min_p;
-        const double far = weight_of(fmin(z + (kBins - 1) / 64.0, 0.0));
+          for (int j = 1; j < kUnit; ++j) v = e == j ? u[j] : v;
+          const double z = v == mx ? 0.0 : z_of(v, mx, q.inv_t);
+          const bool ok = z >= floor && weight(v, mx, q.inv_t) >= q.min_p;
+          const double far = weight_of(fmin(z + (kBins - 1) / 64.0, 0.0));
 #pragma unroll
-        for (int j = 0; j < kUnit; ++j)
-          if (e == j) {
-            in[j] = ok;
-            if (bin[j] == kBins - 1) w[j] = far;
-          }
+          for (int j = 0; j < kUnit; ++j)
+            if (e == j) {
+              in[j] = ok;
+              if (bin[j] == kBins - 1) w[j] = far;
+            }
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < kUnit; ++e) {
+        // (w 2^42 as the low bits of a float64 of that step)
+        const long long fixed = __double_as_longlong(__builtin_fma(w[e], 0x1p42, 0x1p52)) & ((1ll << 52) - 1);
+        if (in[e]) atomicAdd(&mass[bin[e]], (unsigned long long)fixed);
       }
     }
-#pragma unroll
-    for (int e = 0; e < kUnit; ++e) {
-      // (w 2^42 as the low bits of a float64 of that step)
-      const long long fixed = __double_as_longlong(__builtin_fma(w[e], 0x1p42, 0x1p52)) & ((1ll << 52) - 1);
-      if (in[e]) atomicAdd(&mass[bin[e]], (unsigned long long)fixed);
-    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < kBins; i += kScanThreads)
+      if (mass[i]) atomicAdd(&a.hist[(size_t)t * kBins + i], mass[i]);
+    __syncthreads();
   }
-  __syncthreads();
-  for (int i = threadIdx.x; i < kBins; i += kScanThreads)
-    if (mass[i]) atomicAdd(&a.hist[(size_t)t * kBins + i], mass[i]);
 }
 
 template <int DT, int BPW>
 __global__ __launch_bounds__(kScanThreads) void mark_kernel(SampleArgs a, int segs) {
-  const int t = blockIdx.x / segs, seg = blockIdx.x % segs;
-  if (a.open[t].state != 1) return;
   constexpr int W = kScanThreads / 64, PER = kBins / kScanThreads;
   __shared__ double part[W];
   __shared__ double running[kBins];
   __shared__ uint64_t mine[kList];  // the workgroup's logits of the border bin
   __shared__ int found, count, place;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const Row row = row_of<DT>(a, t);
-  const Params q = params_of(a, t);
-  const float mx = a.open[t].mx;
-  const double floor = kLowest;
-  const int b0 = (seg * W + wave) * BPW;
-  Raw<DT> raw[BPW];
-  load_raws<DT, BPW>(row, b0 * 64, raw);
-  // the border bin: every workgroup finds the same (without a top_p there is none)
-  unsigned long long f[PER];
-#pragma unroll
-  for (int i = 0; i < PER; ++i) f[i] = a.hist[(size_t)t * kBins + threadIdx.x * PER + i];
-  double m[PER], s = 0.0;
-#pragma unroll
-  for (int i = 0; i < PER; ++i) m[i] = (double)(q.p < 1.0 ? f[i] : 0) * 0x1p-42;
-  {
-    // (the bins' top weights: the first one's, then e^-1/64 apart)
-    double w = weight_of(threadIdx.x * (-PER / 64.0));
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      m[i] *= w;
-      w *= kBinStep;
-      s += m[i];
-    }
-  }
-  const double x = wave_upto(s);
-  if (lane == 63) part[wave] = x;
-  if (threadIdx.x == 0) {
-    found = kBins;
-    count = 0;
-  }
-  __syncthreads();
-  double all = 0.0, run = x - s;
-#pragma unroll
-  for (int w = 0; w < W; ++w) {
-    if (w < wave) run += part[w];
-    all += part[w];
-  }
-  const double limit = q.p * all;
-  // (the wave's first bin before the one atomic: 64 lanes' atomics on one word take
-  // 2 us)
-  uint32_t first = 0;  // its complement
-#pragma unroll
-  for (int i = PER - 1; i >= 0; --i) {
-    double r = run;
-#pragma unroll
-    for (int j = 0; j <= i; ++j) r += m[j];
-    running[threadIdx.x * PER + i] = r;
-    if (m[i] > 0.0 && r >= limit) first = ~(uint32_t)(threadIdx.x * PER + i);
-  }
-  first = wave_most(first);
-  if (lane == 0 && first) atomicMin(&found, (int)~first);
-  __syncthreads();
-  const int border = found;
-  if (seg == 0 && threadIdx.x == 0) {
-    a.open[t].bin = border;
-    a.open[t].limit = limit;
-    a.open[t].base = border > 0 && border < kBins ? running[border - 1] : 0.0;
-  }
-  if (border == kBins && q.p < 1.0) return;  // (rounding at the end: the row is done alone)
+  const int items = *a.open_n * segs;
 #pragma unroll 1
-  for (int i = 0; i < BPW; ++i) {
-    if (b0 + i >= a.nb) break;
-    float u[kUnit];
-    unpack<DT>(raw[0], u);
-    next_raw(raw, raw[0]);
-    double sum = 0.0;
-    uint32_t listed = 0;
+  for (int item = blockIdx.x; item < items; item += gridDim.x) {
+    const int t = a.open_rows[item / segs], seg = item % segs;
+    __syncthreads();
+    const Row row = row_of<DT>(a, t);
+    const Params q = params_of(a, t);
+    const float mx = a.open[t].mx;
+    const double floor = kLowest;
+    const int b0 = (seg * W + wave) * BPW;
+    Raw<DT> raw[BPW];
+    load_raws<DT, BPW>(row, b0 * 64, raw);
+    // the border bin: every workgroup finds the same (without a top_p there is none)
+    unsigned long long f[PER];
 #pragma unroll
-    for (int e = 0; e < kUnit; ++e) {
-      const double z = u[e] == mx ? 0.0 : z_of(u[e], mx, q.inv_t);
-      const double w = u[e] == mx ? 1.0 : weight_of(z);
-      const int b = open_bin(z);
-      const bool in = z >= floor && w >= q.min_p;
-      sum += in && b < border ? w : 0.0;
-      listed |= in && b == border ? 1u << e : 0u;
-    }
-    if (__any(listed)) {
-      const int c = __builtin_popcount(listed), upto = wave_upto(c);
-      int at = 0;
-      if (lane == 63) at = atomicAdd(&count, upto);
-      at = __builtin_amdgcn_readlane(at, 63) + upto - c;
+    for (int i = 0; i < PER; ++i) f[i] = a.hist[(size_t)t * kBins + threadIdx.x * PER + i];
+    double m[PER], s = 0.0;
 #pragma unroll
-      for (int e = 0; e < kUnit; ++e)
-        if (listed >> e & 1) {
-          if (at < kList) mine[at] = key_of(u[e], ((b0 + i) * 64 + lane) * kUnit + e - row.lo);
-          ++at;
-        }
+    for (int i = 0; i < PER; ++i) m[i] = (double)(q.p < 1.0 ? f[i] : 0) * 0x1p-42;
+    {
+      // (the bins' top weights: the first one's, then e^-1/64 apart)
+      double w = weight_of(threadIdx.x * (-PER / 64.0));
+#pragma unroll
+      for (int i = 0; i < PER; ++i) {
+        m[i] *= w;
+        w *= kBinStep;
+        s += m[i];
+      }
     }
-    sum = wave_sum(sum);
-    if (lane == 0) a.bmass[(size_t)t * a.nb + b0 + i] = sum;
+    const double x = wave_upto(s);
+    if (lane == 63) part[wave] = x;
+    if (threadIdx.x == 0) {
+      found = kBins;
+      count = 0;
+    }
+    __syncthreads();
+    double all = 0.0, run = x - s;
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+      if (w < wave) run += part[w];
+      all += part[w];
+    }
+    const double limit = q.p * all;
+    // (the wave's first bin before the one atomic: 64 lanes' atomics on one word take
+    // 2 us)
+    uint32_t first = 0;  // its complement
+#pragma unroll
+    for (int i = PER - 1; i >= 0; --i) {
+      double r = run;
+#pragma unroll
+      for (int j = 0; j <= i; ++j) r += m[j];
+      running[threadIdx.x * PER + i] = r;
+      if (m[i] > 0.0 && r >= limit) first = ~(uint32_t)(threadIdx.x * PER + i);
+    }
+    first = wave_most(first);
+    if (lane == 0 && first) atomicMin(&found, (int)~first);
+    __syncthreads();
+    const int border = found;
+    if (seg == 0 && threadIdx.x == 0) {
+      a.open[t].bin = border;
+      a.open[t].limit = limit;
+      a.open[t].base = border > 0 && border < kBins ? running[border - 1] : 0.0;
+    }
+    if (border == kBins && q.p < 1.0) continue;  // (rounding at the end: the row is done alone)
+#pragma unroll 1
+    for (int i = 0; i < BPW; ++i) {
+      if (b0 + i >= a.nb) break;
+      float u[kUnit];
+      unpack<DT>(raw[0], u);
+      next_raw(raw, raw[0]);
+      double sum = 0.0;
+      uint32_t listed = 0;
+#pragma unroll
+      for (int e = 0; e < kUnit; ++e) {
+        const double z = u[e] == mx ? 0.0 : z_of(u[e], mx, q.inv_t);
+        const double w = u[e] == mx ? 1.0 : weight_of(z);
+        const int b = open_bin(z);
+        const bool in = z >= floor && w >= q.min_p;
+        sum += in && b < border ? w : 0.0;
+        listed |= in && b == border ? 1u << e : 0u;
+      }
+      if (__any(listed)) {
+        const int c = __builtin_popcount(listed), upto = wave_upto(c);
+        int at = 0;
+        if (lane == 63) at = atomicAdd(&count, upto);
+        at = __builtin_amdgcn_readlane(at, 63) + upto - c;
+#pragma unroll
+        for (int e = 0; e < kUnit; ++e)
+          if (listed >> e & 1) {
+            if (at < kList) mine[at] = key_of(u[e], ((b0 + i) * 64 + lane) * kUnit + e - row.lo);
+            ++at;
+          }
+      }
+      sum = wave_sum(sum);
+      if (lane == 0) a.bmass[(size_t)t * a.nb + b0 + i] = sum;
+    }
+    __syncthreads();
+    if (threadIdx.x == 0 && count) place = atomicAdd(&a.open[t].n, count);
+    __syncthreads();
+    for (int i = threadIdx.x; i < min(count, kList); i += kScanThreads)
+      if (place + i < kList) a.list[(size_t)t * kList + place + i] = mine[i];
   }
-  __syncthreads();
-  if (threadIdx.x == 0 && count) place = atomicAdd(&a.open[t].n, count);
-  __syncthreads();
-  for (int i = threadIdx.x; i < min(count, kList); i += kScanThreads)
-    if (place + i < kList) a.list[(size_t)t * kList + place + i] = mine[i];
 }
 
 template <int DT>
@@ -1571,10 +1593,15 @@ __global__ __launch_bounds__(kPickThreads) __attribute__((amdgpu_waves_per_eu(4)
                        [&](float v, int i, double w) { return key_of(v, i) >= last && w >= q.min_p; });
 }
 
-// Calls of at least this many rows leave open rows to launches of their own.  Those
-// take 3 us where no row is open; one workgroup takes 10 times as long as they do for an
-// open row of 150,000 logits.
-constexpr int kDeferRows = 4;
+// Fewer rows than this that come with a top_k have no histograms: a top_k of zero among
+// them, a row that may be left to them, is cut by one workgroup.  (One row of 150,000
+// logits, open: 60 us with, 420 without; their two launches cost 3 us where it is not.)
+constexpr int kBinRows = 4;
+// The blocks of a scanned wave, and of a wave of the histograms' kernels in calls of few
+// and of many blocks (rows of 150,000 logits, us with 2, 4: one scanned row 10.1, 11.9,
+// 512 of them 91.0, 91.5; 16 open rows 72, 75, 32 91, 87, 128 167, 155).
+constexpr int kScanBlocks = 2, kFewBlocks = 2, kManyBlocks = 4;
+constexpr int kMany = 8192;
 // Rows of one round of launches (the workspace is this many rows' at most).
 constexpr int kRoundRows = 1024;
 
@@ -1583,25 +1610,26 @@ hipError_t launch(SampleArgs a, hipStream_t stream) {
   constexpr int W = kScanThreads / 64;
   constexpr int ES = DT == PCTREE_F32 ? 4 : 2;
   const int rows = a.T;
-  const bool defer = a.open && (a.has & (kHasTopP | kHasTopK | kHasMinP));
+  const bool filters = a.open && (a.has & (kHasTopP | kHasTopK | kHasMinP));
+  a.bins = !(a.has & kHasTopK) || rows >= kBinRows;
   for (int t0 = 0; t0 < rows; t0 += kRoundRows) {
     a.T = rows - t0 < kRoundRows ? rows - t0 : kRoundRows;
-    // few rows: more workgroups of less each
-    const int bpw = (long long)a.T * a.nb < 4096 * W ? 2 : 8;
-    const int segs = (a.nb + W * bpw - 1) / (W * bpw);
-    const unsigned grid = (unsigned)(a.T * segs);
-    if (bpw == 2)
-      scan_kernel<DT, 2><<<grid, kScanThreads, 0, stream>>>(a, segs);
-    else
-      scan_kernel<DT, 8><<<grid, kScanThreads, 0, stream>>>(a, segs);
-    if (defer) {
+    const bool many = (long long)a.T * a.nb >= kMany;
+    const int segs = (a.nb + W * kScanBlocks - 1) / (W * kScanBlocks);
+    scan_kernel<DT, kScanBlocks><<<(unsigned)(a.T * segs), kScanThreads, 0, stream>>>(a, segs);
+    if (filters) {
       pick_kernel<DT, true><<<(unsigned)a.T, kPickThreads, 0, stream>>>(a);
-      if (bpw == 2) {
-        hist_kernel<DT, 2><<<grid, kScanThreads, 0, stream>>>(a, segs);
-        mark_kernel<DT, 2><<<grid, kScanThreads, 0, stream>>>(a, segs);
-      } else {
-        hist_kernel<DT, 8><<<grid, kScanThreads, 0, stream>>>(a, segs);
-        mark_kernel<DT, 8><<<grid, kScanThreads, 0, stream>>>(a, segs);
+      if (a.bins) {
+        const int per = W * (many ? kManyBlocks : kFewBlocks);
+        const int parts = (a.nb + per - 1) / per;
+        const unsigned grid = (unsigned)std::min(a.T * parts, kOpenGrid);
+        if (many) {
+          hist_kernel<DT, kManyBlocks><<<grid, kScanThreads, 0, stream>>>(a, parts);
+          mark_kernel<DT, kManyBlocks><<<grid, kScanThreads, 0, stream>>>(a, parts);
+        } else {
+          hist_kernel<DT, kFewBlocks><<<grid, kScanThreads, 0, stream>>>(a, parts);
+          mark_kernel<DT, kFewBlocks><<<grid, kScanThreads, 0, stream>>>(a, parts);
+        }
       }
       finish_kernel<DT><<<(unsigned)a.T, kPickThreads, 0, stream>>>(a);
     } else {
@@ -1634,15 +1662,16 @@ void plan_sample(int V, int* ng, int* nb, int* gshift) {
 
 namespace {
 int round_rows(int T) { return T < kRoundRows ? T : kRoundRows; }
-bool deferring(int T, int V) { return T >= kDeferRows && V > kList; }
+bool deferring(int V) { return V > kList; }
 }  // namespace
 
 size_t sample_bytes(int T, int V) {
   int ng, nb, s;
   plan_sample(V, &ng, &nb, &s);
   size_t row = (size_t)nb * 12 + (size_t)ng * 4;
-  if (deferring(T, V)) row += (kBins + kList) * sizeof(uint64_t) + sizeof(OpenRow);
-  return ((size_t)round_rows(T) * row + 511) / 256 * 256;
+  if (deferring(V))
+    row += (kBins + kList) * sizeof(uint64_t) + sizeof(OpenRow) + sizeof(int);
+  return ((size_t)round_rows(T) * row + 16 + 511) / 256 * 256;
 }
 
 void place_sample(SampleArgs* a, void* workspace) {
@@ -1651,7 +1680,8 @@ void place_sample(SampleArgs* a, void* workspace) {
   char* w = (char*)workspace;
   a->hist = a->list = nullptr;
   a->open = nullptr;
-  if (deferring(a->T, a->V)) {
+  a->open_n = a->open_rows = nullptr;
+  if (deferring(a->V)) {
     a->hist = (unsigned long long*)w;
     a->list = a->hist + T * kBins;
     a->open = (OpenRow*)(a->list + T * kList);
@@ -1660,6 +1690,10 @@ void place_sample(SampleArgs* a, void* workspace) {
   a->bmass = (double*)w;
   a->bref = (float*)(a->bmass + T * a->nb);
   a->gmax = a->bref + T * a->nb;
+  if (a->open) {
+    a->open_n = (int*)(a->gmax + T * a->ng);
+    a->open_rows = a->open_n + 1;
+  }
 }
 
 hipError_t launch_sample(const SampleArgs& a, int dtype, hipStream_t stream) {
