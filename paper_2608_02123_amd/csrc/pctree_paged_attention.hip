@@ -51,7 +51,11 @@ constexpr int kColTiles = 2;
 constexpr int kRowsPerWave = 16 * kColTiles;
 constexpr int kRowsPerBlock = kWaves * kRowsPerWave;
 constexpr int kMaxSplits = 32;
-constexpr int kFewRows = 64;         // rows (times g) of a request that go 16 to a workgroup
+// Rows (times g) of a request that go 16 to a workgroup, which read K and V again for
+// every 16.  (32 requests over 1000 to 4000 slots of 8 heads, us so and in blocks of 128
+// rows: 32 rows 87, 88, 48 rows 108, 89, 64 rows 137, 90; 8 requests 32, 31, 38, 32, 42,
+// 33; one 13.4, 14.3, 15.4, 14.7, 15.6, 15.2.)
+constexpr int kFewRows = 32;
 constexpr int kFewChunk = 32;        // slots of a wave's step there
 constexpr int kFewRun = 4 * kFewChunk;  // the shortest run there, a chunk to each wave
 constexpr int kMergeThreads = 256;
