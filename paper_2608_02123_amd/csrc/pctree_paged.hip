@@ -11,6 +11,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <algorithm>
+
 #include "pctree_paged.h"
 #include "pctree_tile.h"
 
@@ -190,7 +192,11 @@ __global__ __launch_bounds__(kCompactThreads) void compact_paged_kernel(CompactP
 template <int D, bool H>
 hipError_t append(const AppendArgs& a, hipStream_t stream) {
   const int units = ((a.q ? a.Hq : 0) + 2 * a.Hkv + 512 / D - 1) / (512 / D);
-  const int split = a.b.T >= 2048 ? 1 : units;
+  // About 8192 waves, from one a row that goes over all its heads to one for every 512
+  // elements (32 and 8 heads of 128; us at 1, 2, 4, 12 waves a row: one row 12.9, 8.0,
+  // 5.6, 3.9; 1024 rows 15.6, 10.2, 8.5, 9.3; 3000 rows 21.2, 17.5, 18.2, 21.2; 8192
+  // rows 35.7, 35.7, 37.7, 48.7).
+  const int split = std::max(1, std::min(units, 8192 / a.b.T));
   const long long waves = (long long)a.b.T * split;
   const unsigned blocks = (unsigned)((waves + kAppendWaves - 1) / kAppendWaves);
   append_kernel<D, H><<<blocks, kAppendThreads, 0, stream>>>(a, split);
