@@ -344,7 +344,7 @@ typedef struct pctree_paged_batch {
   const int32_t* page_table; /* [R][max_pages]                               */
   int32_t requests;          /* R                                            */
   int32_t max_pages;         /* width of the page table                      */
-  int32_t rows;              /* T: rows of q, k, v and out                   */
+  int32_t rows;              /* T: rows of q, k, v and out, below 2^24       */
   int32_t max_rows;          /* the most rows that a request has, <= rows    */
 } pctree_paged_batch;
 
@@ -453,7 +453,7 @@ pctree_status pctree_sample(const void* logits, int32_t dtype, int32_t rows, int
  * prefix_len[r] + 0..a.  Other slots keep their contents.  A request is left
  * untouched if its accepted nodes are not strictly increasing, not below
  * budget, or lie on (or move to) slots that do not exist.  slot_bytes and the
- * strides are multiples of 16. */
+ * strides are multiples of 16; no page of a group overlaps one of another. */
 pctree_status pctree_compact_paged(void* pool, int64_t group_stride, int64_t page_stride,
                                    int32_t groups, int32_t pages, int32_t heads,
                                    int32_t page_size, int32_t slot_bytes,

@@ -14,6 +14,9 @@ bool aligned(const void* ptr, size_t a) { return ((uintptr_t)ptr & (a - 1)) == 0
 // workspace size is a function of the arguments alone.
 constexpr int kPlanCUs = 256;
 
+// A launch has at most 2^32 - 1 threads along x, in workgroups of 256.
+constexpr int64_t kMaxGrid = (1 << 24) - 1;
+
 pctree_status check_cache(const pctree_paged_cache* c) {
   if (!c || c->pages < 1 || c->page_size < 1 || c->kv_heads < 1 || c->head_dim < 1)
     return PCTREE_ERR_INVALID_ARGUMENT;
@@ -32,7 +35,8 @@ pctree_status check_batch(const pctree_paged_cache* c, const pctree_paged_batch*
   if (!b || b->requests < 1 || b->max_pages < 1 || b->rows < 1 || b->max_rows < 1 ||
       b->max_rows > b->rows)
     return PCTREE_ERR_INVALID_ARGUMENT;
-  if (b->requests > 65535 || (int64_t)b->max_pages * c->page_size > PCTREE_MAX_PAGED_SLOTS)
+  if (b->requests > 65535 || b->rows > kMaxGrid ||
+      (int64_t)b->max_pages * c->page_size > PCTREE_MAX_PAGED_SLOTS)
     return PCTREE_ERR_UNSUPPORTED;
   return PCTREE_OK;
 }
@@ -72,11 +76,14 @@ pctree_status check_attention(const pctree_paged_cache* c, const pctree_paged_ba
   st = check_batch(c, b);
   if (st != PCTREE_OK) return st;
   if (q_heads < 1 || q_heads % c->kv_heads != 0) return PCTREE_ERR_INVALID_ARGUMENT;
-  // rows of (row, head) pairs are counted in 31 bits, and so is the grid
+  // (row, head) pairs are counted in 31 bits
   if ((int64_t)b->rows * q_heads > INT32_MAX / 2) return PCTREE_ERR_UNSUPPORTED;
   *plan = plan_paged_attention(b->requests, b->rows, b->max_rows, q_heads, c->kv_heads,
                                c->head_dim, b->max_pages * c->page_size, kPlanCUs);
-  if (plan->blocks > INT32_MAX || plan->few_blocks > INT32_MAX) return PCTREE_ERR_UNSUPPORTED;
+  const int hpw = 256 / c->head_dim;  // heads of a merging wave
+  const int64_t row_waves = (int64_t)b->rows * ((q_heads + hpw - 1) / hpw);
+  if (plan->blocks > kMaxGrid || plan->few_blocks > kMaxGrid || (row_waves + 3) / 4 > kMaxGrid)
+    return PCTREE_ERR_UNSUPPORTED;
   return PCTREE_OK;
 }
 
@@ -269,6 +276,12 @@ pctree_status pctree_compact_paged(void* pool, int64_t group_stride, int64_t pag
     // a thread for every 16 bytes of a slot in every group
     if (heads > 65535 || (int64_t)heads * (slot_bytes / 16) > INT32_MAX / groups)
       return PCTREE_ERR_UNSUPPORTED;
+    // pages in groups or groups in pages, none on another (a path's slots would be read
+    // while the same slots of another group are written)
+    const int64_t block = (int64_t)heads * page_size * slot_bytes;
+    if (groups > 1 && (group_stride < block || ((group_stride - block) / page_stride < pages - 1 &&
+                                                (page_stride - block) / group_stride < groups - 1)))
+      return PCTREE_ERR_INVALID_ARGUMENT;
     CompactPagedArgs a;
     a.pool = (char*)pool;
     a.group_stride = group_stride;

@@ -149,3 +149,22 @@ def test_binding_refuses_host_tensors_and_wrong_shapes():
         P._paged_cache(k.float(), k.float(), 0)
     with pytest.raises(ValueError):
         P.compact_paged(torch.zeros(2, 4, 2, 16, 64), i, i, torch.zeros(3, 5, dtype=torch.int32), i, 8)
+
+
+def test_calls_past_a_launch_are_refused():
+    wide = dict(rows=1 << 24, max_rows=1 << 24)
+    assert do_append(b=batch(**wide)) == P.ERR_UNSUPPORTED
+    assert do_attention(b=batch(**wide)) == P.ERR_UNSUPPORTED
+    # few rows, but blocks for every request, head and run
+    assert do_attention(c=cache(kv_heads=4096), b=batch(rows=8192, max_rows=8192, requests=60000),
+                        heads=4096) == P.ERR_UNSUPPORTED
+
+
+@pytest.mark.parametrize("kw", [dict(group_stride=0), dict(group_stride=4096), dict(group_stride=1 << 15),
+                                dict(group_stride=9 * (1 << 15)), dict(group_stride=1 << 15, page_stride=1 << 16)])
+def test_compaction_refuses_groups_that_overlap(kw):
+    block = 8 * 16 * 256
+    a = {**dict(group_stride=10 * block, page_stride=block), **kw}
+    st = P.lib().pctree_compact_paged(A, a["group_stride"], a["page_stride"], 4, 10, 8, 16, 256, A, 20, A, A, A, 2,
+                                      64, 16, None)
+    assert st == P.ERR_INVALID_ARGUMENT
