@@ -437,6 +437,28 @@ def test_append_many_rows_in_place():
             assert (np.abs(_np(a[t, h]) - z) <= 2.0 ** -8 * np.abs(z) + 2.0 ** -17 * mag).all()
 
 
+@pytest.mark.parametrize("T", [1300, 3500, 9000])
+@pytest.mark.parametrize("D", [64, 128])
+def test_append_of_many_rows_is_that_of_few(T, D):
+    """However many waves share a row: the same bits as 100 rows a call."""
+    Hq, Hkv, page = 12, 4, 32
+    g = _gen(T + D)
+    b = make_batch(np.random.default_rng(T), [T], [17], page)
+    q, k, v = ((torch.randn(T, h, D, generator=g) * 2).to(torch.bfloat16).cuda() for h in (Hq, Hkv, Hkv))
+    w = (1 + 0.2 * torch.randn(D, generator=g)).to(torch.bfloat16).cuda()
+    rope = P.rope_table(T + 20, D)
+    caches = [torch.zeros(b["pages"], Hkv, page, D, dtype=torch.bfloat16, device="cuda") for _ in range(4)]
+    out = P.append_paged(dev_batch(b), caches[0], caches[1], k, v, q=q, q_norm=w, k_norm=w, rope=rope)
+    for t0 in range(0, T, 100):
+        n = min(100, T - t0)
+        few = dev_batch({**b, "rows": n, "row_count": np.array([n], np.int32),
+                         "prefix_len": np.array([17 + t0], np.int32), "max_rows": n})
+        part = P.append_paged(few, caches[2], caches[3], k[t0:t0 + n], v[t0:t0 + n], q=q[t0:t0 + n], q_norm=w,
+                              k_norm=w, rope=rope)
+        assert torch.equal(out[t0:t0 + n], part), t0
+    assert torch.equal(caches[0], caches[2]) and torch.equal(caches[1], caches[3])
+
+
 def test_far_positions():
     """Rotation angles of positions past 2^20 keep their fractions of a turn."""
     rope = P.rope_table((1 << 20) + 5, 64, theta=1e4)

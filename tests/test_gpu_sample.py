@@ -110,6 +110,25 @@ def test_open_rows(T):
             check(x, rng.random(T), **f)
 
 
+@pytest.mark.parametrize("T", [1, 3, 4])
+def test_open_rows_beside_rows_of_a_top_k(T):
+    """A top_k of zero in a call that has the others': few rows come without histograms."""
+    rng = np.random.default_rng(T)
+    for dt, V, sigma in (("bf16", 151936, 1.0), ("f32", 40001, 0.2)):
+        x = rows(T, T, V, dt, sigma=sigma, head=0.0)
+        for f in (dict(top_p=0.9), dict(min_p=0.05), dict(min_p=0.05, top_p=0.7)):
+            for k in (np.zeros(T), np.arange(T) * 30, -np.ones(T)):
+                print(f"[sample] {dt} {V} {f} {k}", flush=True)
+                check(x, rng.random(T), top_k=k, **f)
+
+
+def test_open_rows_in_two_rounds():
+    T, V = 1100, 4000
+    x = rows(8, T, V, "bf16", sigma=0.5, head=3.0)
+    rng = np.random.default_rng(12)
+    check(x, rng.random(T), top_p=rng.choice([0.9, 0.99, 1.0], T), min_p=rng.choice([0.0, 0.1], T))
+
+
 @pytest.mark.parametrize("V", [100, 5000, 151936])
 def test_equal_logits(V):
     """Ties go by token: the weights are whole numbers and the sums exact."""
