@@ -596,6 +596,23 @@ class _Here:
             self.ctx.__exit__(*exc)
 
 
+class _Workspace:
+    """An object's workspace.  On a stream other than the one that it was made on the
+    allocator is told, or a freed object's memory could have a new owner while that
+    stream's kernels still use it."""
+    __slots__ = ("tensor", "ptr", "bytes", "home")
+
+    def __init__(self, nbytes, device):
+        self.tensor = torch.empty(max(nbytes, 1), dtype=torch.uint8, device=device)
+        self.ptr, self.bytes = self.tensor.data_ptr(), nbytes
+        self.home = torch.cuda.current_stream(self.tensor.device).cuda_stream
+
+    def on(self, st):
+        if st != self.home:
+            self.tensor.record_stream(torch.cuda.current_stream())
+        return self.ptr
+
+
 def _device_tensor(name, t, dtype, shape, idx):
     """``t`` must be a contiguous tensor of that type and shape on device ``idx``."""
     if not isinstance(t, torch.Tensor) or t.dtype is not dtype:
@@ -744,9 +761,8 @@ class PagedAttention:
         self.ws_bytes = int(lib().pctree_paged_attention_workspace_bytes(
             ctypes.byref(c), batch._ref, q_heads))
         self.idx = batch.idx
-        self.workspace = torch.empty(max(self.ws_bytes, 1), dtype=torch.uint8,
-                                     device=batch.device)
-        self._ws = self.workspace.data_ptr()
+        self._ws = _Workspace(self.ws_bytes, batch.device)
+        self.workspace = self._ws.tensor
 
     def __call__(self, q, k_cache, v_cache, batch, mask=None, out=None, stream=None):
         """``q [T][Hq][D]`` over ``k_cache, v_cache [pages][Hkv][page_size][D]``; causal, or
@@ -775,7 +791,7 @@ class PagedAttention:
                 out = torch.empty(shp, dtype=q.dtype, device=q.device)
             status = lib().pctree_paged_attention(
                 ctypes.byref(c), batch._ref, q.data_ptr(), self.q_heads, self.scale, _ptr(mask),
-                budget, out.data_ptr(), self._ws, self.ws_bytes, st)
+                budget, out.data_ptr(), self._ws.on(st), self.ws_bytes, st)
         _check(status, "pctree_paged_attention")
         return out
 
@@ -832,8 +848,9 @@ class Sampler:
         if nb == 0:
             _check(lib().pctree_sample(None, F32, rows, vocab, vocab, *([None] * 8), 0, None),
                    "sizes")
-        self.workspace = torch.empty(nb, dtype=torch.uint8, device=device)
-        self.idx, self._ws, self._nb = self.workspace.get_device(), self.workspace.data_ptr(), nb
+        self._ws = _Workspace(nb, device)
+        self.workspace = self._ws.tensor
+        self.idx = self.workspace.get_device()
 
     def __call__(self, logits, uniform, *, temperature=None, top_k=None, top_p=None, min_p=None,
                  token=None, logprob=None, stream=None):
@@ -874,7 +891,7 @@ class Sampler:
             status = lib().pctree_sample(
                 logits.data_ptr(), _LOGITS[logits.dtype], T, V, stride[0] if T > 1 else V,
                 uniform.data_ptr(), _ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p),
-                token.data_ptr(), logprob.data_ptr(), self._ws, self._nb, st)
+                token.data_ptr(), logprob.data_ptr(), self._ws.on(st), self._ws.bytes, st)
         _check(status, "pctree_sample")
         return token, logprob
 

@@ -548,6 +548,33 @@ def test_another_stream():
     assert torch.equal(out, want)
 
 
+@pytest.mark.parametrize("passed", [True, False])
+def test_a_workspace_outlives_its_object_on_another_stream(passed):
+    """Freed while another stream's call is still queued, it has no new owner yet."""
+    b = make_batch(np.random.default_rng(3), [1, 1], [2000, 900], 16)
+    q = torch.randn(2, 8, 128).to(torch.bfloat16).cuda()
+    kc = torch.randn(b["pages"], 2, 16, 128).to(torch.bfloat16).cuda()
+    x, u = torch.randn(2, 30000).cuda(), torch.rand(2).cuda()
+    bt, s = dev_batch(b), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for make in (lambda: P.PagedAttention(bt, 8, 2, 128, 16), lambda: P.Sampler(2, 30000)):
+        layer = make()
+        ptr, n = layer.workspace.data_ptr(), layer.workspace.numel()
+        s.wait_stream(torch.cuda.current_stream())
+        args = (q, kc, kc, bt) if isinstance(layer, P.PagedAttention) else (x, u)
+        with torch.cuda.stream(s):
+            torch.cuda._sleep(200_000_000)  # about 0.1 s
+            if not passed:
+                layer(*args)
+        if passed:
+            layer(*args, stream=s)
+        del layer
+        again = [torch.empty(n, dtype=torch.uint8, device="cuda") for _ in range(3)]
+        assert not s.query(), "the other stream's work has ended"
+        assert ptr not in [t.data_ptr() for t in again]
+        s.synchronize()
+
+
 def test_graph_replays():
     """A captured step, replayed with other inputs, lengths and work between."""
     step, t, kc, vc, out, bt = _small_step()
