@@ -605,7 +605,8 @@ class _Workspace:
     def __init__(self, nbytes, device):
         self.tensor = torch.empty(max(nbytes, 1), dtype=torch.uint8, device=device)
         self.ptr, self.bytes = self.tensor.data_ptr(), nbytes
-        self.home = torch.cuda.current_stream(self.tensor.device).cuda_stream
+        self.home = (torch.cuda.current_stream(self.tensor.device).cuda_stream
+                     if self.tensor.is_cuda else None)  # (without, calls are refused)
 
     def on(self, st):
         if st != self.home:
