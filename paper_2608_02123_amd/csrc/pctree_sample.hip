@@ -238,7 +238,8 @@ __device__ __forceinline__ Params params_of(const SampleArgs& a, int t) {
   q.k = (a.has & kHasTopK) && k > 0 && k < a.V ? k : 0;
   q.p = (a.has & kHasTopP) && p < 1.0f ? (double)p : 1.0;  // (NaN: off)
   q.min_p = (a.has & kHasMinP) && m > 0.0f ? (double)fminf(m, 1.0f) : 0.0;
-  q.u = u > 0.0f ? (double)u : 0.0;
+  // (1 and more: infinite, so that no running sum passes it, however that was rounded)
+  q.u = u >= 1.0f ? (double)__builtin_inff() : (u > 0.0f ? (double)u : 0.0);
   return q;
 }
 // Whether the row is settled from its largest logits, without the sum of all.
@@ -737,15 +738,23 @@ __device__ void draw_from_list(const SampleArgs& a, int t, const Params& q, floa
   __syncthreads();
   running_sums(sh.l.w, n, sh);
   const double total = sh.l.w[n - 1], target = q.u * total;
-  int before = 0, live = 0;  // sums that do not pass the target; sums below the total
-  for (int i = threadIdx.x; i < n; i += kPickThreads) {
-    before += sh.l.w[i] <= target;
-    live += sh.l.w[i] < total;
+  int at = 0;  // sums that do not pass the target
+  for (int i = threadIdx.x; i < n; i += kPickThreads) at += sh.l.w[i] <= target;
+  at = block_sum(at, sh);
+  if (at == n) {  // (a uniform of 1) the last of positive weight, which the sums may have lost
+    uint32_t last = 0;
+    for (int i = threadIdx.x; i < n; i += kPickThreads)
+      if (weight(of_ord((uint32_t)sh.l.list[i]), mx, q.inv_t) > 0.0) last = (uint32_t)i;
+    last = wave_most(last);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) sh.parti[threadIdx.x >> 6] = (int)last;
+    __syncthreads();
+    at = 0;
+#pragma unroll
+    for (int w = 0; w < kPickWaves; ++w) at = max(at, sh.parti[w]);
   }
-  before = block_sum(before, sh);
-  live = block_sum(live, sh);
   if (threadIdx.x == 0) {
-    const uint64_t k = sh.l.list[before < n ? before : live];
+    const uint64_t k = sh.l.list[at];
     emit(a, t, (int)~(uint32_t)(k >> 32), log_prob(of_ord((uint32_t)k), mx, q.inv_t, total));
   }
 }

@@ -188,6 +188,40 @@ def test_uniforms_at_and_past_the_ends():
         check(x, u, exact_sums=True, **f)
 
 
+def _few_tokens(T, V, values, seed=1):
+    """Rows of -inf but for a logit of 0 at token 5 and `values` at random later ones."""
+    at = torch.randperm(V - 6, generator=torch.Generator().manual_seed(seed))[:len(values)] + 6
+    x = torch.full((T, V), -float("inf"))
+    x[:, 5] = 0.0
+    x[:, at] = torch.tensor(values)
+    return x.cuda()
+
+
+@pytest.mark.parametrize("n", [40, 99, 1500])
+def test_the_last_token_of_a_weight_that_rounding_loses(n):
+    """A uniform of 1 takes the last kept token of positive weight, though e^-46 adds
+    nothing to a running sum that holds 1, and not one of weight 0 behind it."""
+    V = 5000
+    u = np.array([1.0, 1.5, float("inf")], np.float32)
+    zeros = [-46.0] * (n - n // 3) + [-800.0] * (n // 3)
+    for f in (dict(top_k=n + 1), dict(top_k=n // 2), dict(top_k=3000), dict(min_p=1e-30), dict(),
+              dict(top_k=n + 1, min_p=1e-30, temperature=0.9)):
+        for values in ([-46.0] * n, zeros):
+            print(f"[sample] {n} {f} {values[-1]}", flush=True)
+            check(_few_tokens(len(u), V, values, n), u, exact_sums=True, **f)
+
+
+@pytest.mark.parametrize("V,sigma", [(20000, 2.0), (151936, 0.5)])
+def test_a_uniform_of_one_over_rounded_sums(V, sigma):
+    """However a path adds the kept weights, none of its sums passes their total."""
+    T = 24
+    x = rows(V + 1, T, V, "f32", sigma=sigma, head=6.0)
+    for f in (dict(), dict(top_k=20), dict(top_k=64), dict(top_k=100), dict(top_k=900), dict(top_k=3000),
+              dict(top_p=0.9), dict(min_p=0.05), dict(min_p=0.01, top_p=0.7), dict(top_k=900, temperature=3.0)):
+        print(f"[sample] {V} {f}", flush=True)
+        check(x, np.ones(T, np.float32), exact_sums=True, **f)
+
+
 def test_parameters_that_are_no_numbers():
     nan = float("nan")
     x = rows(10, 4, 5000, "bf16")
