@@ -80,3 +80,20 @@ def test_lds_loads_wait_for_their_registers(which, tmp_path):
                     assert not (dst & reads) or states >= 5, f"{name}: {back} / {line}"
                 states += _wait_states(back)
     assert loads > 100, loads
+
+
+@pytest.mark.parametrize("kernel", ["compact_paged_kernel"])
+def test_a_batch_of_moves_is_loaded_together(kernel, tmp_path):
+    """A compaction's eight loads are all issued before one of them is waited for, and
+    their values stay in registers."""
+    code = _instructions(P.LIB_PATH, tmp_path)
+    (ins,) = (c for n, c in code.items() if kernel in n)
+    assert not [i for i in ins if i.startswith("scratch_")]
+    run = most = 0
+    for line in ins:
+        if line.startswith("global_load_dwordx4"):
+            run += 1
+        elif re.match(r"s_waitcnt.*vmcnt|global_store", line):
+            run = 0
+        most = max(most, run)
+    assert most == 8, most
