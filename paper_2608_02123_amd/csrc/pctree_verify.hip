@@ -170,7 +170,7 @@ __global__ __launch_bounds__(kVerifyThreads) void compact_kernel(
   int last = -1;
   for (int m = 0; m <= a; ++m) {
     const int v = nodes[m];
-    if (v <= last || v >= N || pre + v >= capacity) return;
+    if (v <= last || v >= N || v >= capacity - pre) return;  // (pre + v may pass 31 bits)
     last = v;
   }
   const long long col = (long long)blockIdx.x * blockDim.x + threadIdx.x;

@@ -165,3 +165,18 @@ def test_compact_kv(groups, width, R):
             want = (VO.compact_rows(cache[i, g], int(prefix[i]), acc_node[i], int(acc_len[i]))
                     if ok else cache[i, g])
             assert np.array_equal(got[i, g], want), (i, g)
+
+
+def test_prefixes_at_the_largest_integer():
+    """A prefix that passes 31 bits with a node added reaches past the capacity."""
+    P = _lib()
+    R, N, W, C, slot = 4, 16, 6, 40, 32
+    cache = torch.arange(R * C * slot, device="cuda").to(torch.uint8).view(R, 1, C, slot)
+    want = cache.clone()
+    node = np.tile(np.array([0, 2, 5, 9, 12, 15], np.int32), (R, 1))
+    prefix = np.array([2 ** 31 - 1, 2 ** 31 - 10, C - 1, 20], np.int32)
+    P.compact_kv(cache, _dev(prefix), _dev(node), _dev(np.full(R, W - 1, np.int32)), N)
+    torch.cuda.synchronize()
+    for m, n in enumerate(node[3]):
+        want[3, :, 20 + m] = want[3, :, 20 + int(n)].clone()
+    assert torch.equal(cache, want)
