@@ -82,7 +82,7 @@ def test_lds_loads_wait_for_their_registers(which, tmp_path):
     assert loads > 100, loads
 
 
-@pytest.mark.parametrize("kernel", ["compact_paged_kernel"])
+@pytest.mark.parametrize("kernel", ["compact_kernel", "compact_paged_kernel"])
 def test_a_batch_of_moves_is_loaded_together(kernel, tmp_path):
     """A compaction's eight loads are all issued before one of them is waited for, and
     their values stay in registers."""
