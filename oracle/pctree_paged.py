@@ -122,7 +122,7 @@ def compact(pool, table, prefix, accept_node, accept_len, budget):
         if any(int(prefix[r]) + x >= cap for x in nodes):
             continue
         moves = [(place(b, r, int(prefix[r]) + x, P, pages), place(b, r, int(prefix[r]) + m, P, pages))
-                 for m, x in enumerate(nodes) if x != m]
+                 for m, x in enumerate(nodes)]
         if any(s is None or d is None for s, d in moves):
             continue
         for (sp, so), (dp, do) in moves:

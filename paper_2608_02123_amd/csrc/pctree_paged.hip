@@ -165,11 +165,11 @@ __global__ __launch_bounds__(kCompactThreads) void compact_paged_kernel(CompactP
   const bool moves = lane <= len && node != lane;
   const uint64_t moving = __ballot(moves);
   const int n = __builtin_popcountll(moving);
-  if (moves) {
+  if (lane <= len) {  // (a node that stays has to lie on a slot too)
     const int s = pre + node, d = pre + lane;
     const int ps = table[s >> a.page_shift], pd = table[d >> a.page_shift];
     ok = (unsigned)ps < (unsigned)a.pages && (unsigned)pd < (unsigned)a.pages;
-    if (threadIdx.x < 64) {
+    if (moves && threadIdx.x < 64) {
       const int at = __builtin_popcountll(moving & ((1ull << lane) - 1));
       from[at] = ps * a.page_stride + (long long)(s & off_mask) * a.slot_units * 16;
       to[at] = pd * a.page_stride + (long long)(d & off_mask) * a.slot_units * 16;

@@ -502,6 +502,26 @@ def test_compact(page):
     assert got is pool and np.array_equal(_np(pool), want)
 
 
+def test_compact_checks_the_nodes_that_stay():
+    """An accepted node that would stay where it is, on a page that does not exist: its
+    request is left untouched."""
+    page, N, W = 4, 12, 6
+    table = np.array([[0, 1, 2, 3], [4, -1, 5, 6], [9, 7, 8, 99]], np.int32)
+    prefix = np.array([3, 4, 0], np.int32)
+    node = np.array([[0, 1, 4, 6, 9, -1], [0, 1, 4, 6, 7, -1], [0, 1, 2, 3, 9, -1]], np.int32)
+    alen = np.array([4, 4, 4], np.int32)
+    table[2, 0] = 10  # (of 10 pages: none)
+    pool = torch.randn(2, 10, 3, page, 8, generator=_gen(4)).to(torch.bfloat16).cuda()
+    before = pool.clone()
+    want = PO.compact(_np(pool), table, prefix, node, alen, N)
+
+    def up(x):
+        return torch.from_numpy(x).cuda()
+    P.compact_paged(pool, up(table), up(prefix), up(node), up(alen), N)
+    assert np.array_equal(_np(pool), want)
+    assert torch.equal(pool[:, 4:], before[:, 4:]) and not torch.equal(pool, before)
+
+
 # ---------------------------------------------------------------------------
 # streams, graphs
 # ---------------------------------------------------------------------------
