@@ -41,7 +41,6 @@ struct SampleArgs {
   long long row_stride;
   int T, V;
   int ng, nb, gshift;
-  bool bins;       // open rows have histograms
 };
 
 // Groups and blocks of a row of V logits at any alignment, and the workspace of T rows.

@@ -27,8 +27,9 @@
 // over all compute units: hist_kernel sums the weights in bins of 1/64 in log
 // weight, mark_kernel finds the bin in which top_p is reached, sums each block's
 // weights above it and lists the bin's own logits, and finish_kernel cuts that list
-// and draws.  One workgroup could do it alone (whole_row; it does for calls of few
-// rows with a top_k, and where the list does not do), which takes several times as long.
+// and draws.  One workgroup could do it alone (whole_row; it does for a top_k that the
+// bounds or the list do not reach, and where the bin's list does not do), which takes
+// several times as long.
 #include "pctree.h"
 
 #include <hip/hip_runtime.h>
@@ -1300,7 +1301,7 @@ __global__ __launch_bounds__(kPickThreads) __attribute__((amdgpu_waves_per_eu(4)
     }
     const bool list = bnd || all_in || q.k == 0;  // (else a top_k beyond the bounds)
     // (rows that the launches after this one can take are left to them early)
-    const int most = DEFER && a.bins && q.k == 0 && !all_in ? kFewGroups : kMaxGroups;
+    const int most = DEFER && q.k == 0 && !all_in ? kFewGroups : kMaxGroups;
     const int n = list ? gather<DT>(a, row, bound, most, sh) : kList + 1;
     if (n <= 64) {
       if (pick_of_64(a, t, q, mx, n, !bnd && !all_in ? total : 0.0, sh)) return;
@@ -1334,7 +1335,7 @@ __global__ __launch_bounds__(kPickThreads) __attribute__((amdgpu_waves_per_eu(4)
       }
     }
     if constexpr (DEFER) {
-      const bool by_bins = a.bins && q.k == 0;
+      const bool by_bins = q.k == 0;
       if (by_bins)
         for (int i = threadIdx.x; i < kBins; i += kPickThreads)
           a.hist[(size_t)t * kBins + i] = 0;
@@ -1608,10 +1609,6 @@ __global__ __launch_bounds__(kPickThreads) __attribute__((amdgpu_waves_per_eu(4)
                        [&](float v, int i, double w) { return key_of(v, i) >= last && w >= q.min_p; });
 }
 
-// Fewer rows than this that come with a top_k have no histograms: a top_k of zero among
-// them, a row that may be left to them, is cut by one workgroup.  (One row of 150,000
-// logits, open: 60 us with, 420 without; their two launches cost 3 us where it is not.)
-constexpr int kBinRows = 4;
 // The blocks of a scanned wave, and of a wave of the histograms' kernels in calls of few
 // and of many blocks (rows of 150,000 logits, us with 2, 4: one scanned row 10.1, 11.9,
 // 512 of them 91.0, 91.5; 16 open rows 72, 75, 32 91, 87, 128 167, 155).
@@ -1626,7 +1623,6 @@ hipError_t launch(SampleArgs a, hipStream_t stream) {
   constexpr int ES = DT == PCTREE_F32 ? 4 : 2;
   const int rows = a.T;
   const bool filters = a.open && (a.has & (kHasTopP | kHasTopK | kHasMinP));
-  a.bins = !(a.has & kHasTopK) || rows >= kBinRows;
   for (int t0 = 0; t0 < rows; t0 += kRoundRows) {
     a.T = rows - t0 < kRoundRows ? rows - t0 : kRoundRows;
     const bool many = (long long)a.T * a.nb >= kMany;
@@ -1634,7 +1630,11 @@ hipError_t launch(SampleArgs a, hipStream_t stream) {
     scan_kernel<DT, kScanBlocks><<<(unsigned)(a.T * segs), kScanThreads, 0, stream>>>(a, segs);
     if (filters) {
       pick_kernel<DT, true><<<(unsigned)a.T, kPickThreads, 0, stream>>>(a);
-      if (a.bins) {
+      // Rows are left to histograms by a top_p or min_p only.  (In every call that has one,
+      // though its rows may all be settled, which these two launches then make 4 us longer,
+      // 18.0 to 22.0 for one row of 150,000 logits with a top_k of 50: an open one among
+      // them takes 64 us, and 437 by one workgroup.)
+      if (a.has & (kHasTopP | kHasMinP)) {
         const int per = W * (many ? kManyBlocks : kFewBlocks);
         const int parts = (a.nb + per - 1) / per;
         const unsigned grid = (unsigned)std::min(a.T * parts, kOpenGrid);

@@ -4,8 +4,9 @@ addresses that nothing reads.
 
 As a program: ``launches.py STAND_IN LIBRARY`` with a list of calls on standard
 input, each {"reset": [cus, failing attribute queries, failing occupancy
-queries]}, {"round": pctree_shape fields} or {"attention": pctree_attn_shape
-fields}; prints, per call, the status and the launches.
+queries]}, {"round": pctree_shape fields}, {"attention": pctree_attn_shape
+fields} or {"sample": [rows, vocab, names of the filters' arrays]}; prints, per
+call, the status and the launches.
 """
 from __future__ import annotations
 
@@ -56,6 +57,11 @@ def _main(stand_in, library):
             inp, tree = (vp * 6)(*[A] * 6), (vp * 7)(*[A] * 7)
             status = lib.pctree_build_tree(shape, inp, tree, None, vp(A),
                                            ctypes.c_size_t(lib.pctree_workspace_bytes(shape)), None)
+        elif "sample" in call:
+            rows, vocab, given = call["sample"]
+            arrays = [vp(A if n in given else 0) for n in ("temperature", "top_k", "top_p", "min_p")]
+            status = lib.pctree_sample(vp(A), 1, rows, vocab, ctypes.c_int64(vocab), vp(A), *arrays,
+                                       vp(A), vp(A), vp(A), ctypes.c_size_t(1 << 40), None)
         else:
             class AttnShape(ctypes.Structure):
                 _fields_ = [("n", ctypes.c_int32 * 6), ("scale", ctypes.c_float)]

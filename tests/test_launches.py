@@ -87,3 +87,20 @@ def test_attention_edge_cases_take_the_kernels_they_name(tmp_path):
     for case, r in zip(E.CASES, _attention(tmp_path, shapes)):
         assert _names(r)[0] == f"{case[8].format(D=case[4])}", case[0]
         assert (len(r["kernels"]) == 2) == case[0].startswith("split runs"), case[0]
+
+
+@pytest.mark.parametrize("rows", [1, 3, 4, 100])
+def test_sampling_kernels_by_the_filters_that_are_given(rows, tmp_path):
+    """Rows may be left to histograms where a top_p or min_p is given, however few they
+    are and whatever else is given; a row of few tokens never is."""
+    given = [[], ["temperature"], ["top_k"], ["top_p"], ["top_k", "top_p"],
+             ["temperature", "top_k", "top_p", "min_p"], ["top_k", "min_p"]]
+    calls = [{"sample": [rows, V, g]} for V in (151936, 2048) for g in given]
+    for call, r in zip(calls, X.record(calls, P.LIB_PATH, tmp_path)):
+        _, V, g = call["sample"]
+        want = ["scan_kernel", "pick_kernel"]
+        if V > 2048 and {"top_p", "min_p"} & set(g):
+            want += ["hist_kernel", "mark_kernel", "finish_kernel"]
+        elif V > 2048 and "top_k" in g:
+            want += ["finish_kernel"]
+        assert [n.split("<")[0] for n in _names(r)] == want, call
