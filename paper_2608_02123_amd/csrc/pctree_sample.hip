@@ -1576,7 +1576,6 @@ __global__ __launch_bounds__(kPickThreads) __attribute__((amdgpu_waves_per_eu(4)
   const Params q = params_of(a, t);
   const bool border = q.p < 1.0;
   if (o.state == 2 || (border && (o.bin >= kBins - 1 || o.n > kList || o.limit <= 0.0))) {
-    for (int g = threadIdx.x; g < a.ng; g += kPickThreads) sh.gmax[g] = a.gmax[(size_t)t * a.ng + g];
     whole_row<DT>(a, t, row, q, o.mx, sh);
     return;
   }
