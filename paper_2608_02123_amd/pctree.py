@@ -614,6 +614,15 @@ class _Workspace:
         return self.ptr
 
 
+def _size(name, x):
+    """``x`` as an int that the C interface can take (ctypes keeps the low 32 bits of
+    another one)."""
+    x = int(x)
+    if not -2 ** 31 <= x < 2 ** 31:
+        raise ValueError(f"{name} must lie in [-2^31, 2^31), got {x}")
+    return x
+
+
 def _device_tensor(name, t, dtype, shape, idx):
     """``t`` must be a contiguous tensor of that type and shape on device ``idx``."""
     if not isinstance(t, torch.Tensor) or t.dtype is not dtype:
@@ -638,6 +647,8 @@ class PagedBatch:
     """
 
     def __init__(self, row_start, row_count, prefix_len, page_table, rows, max_rows=None):
+        self.rows = _size("rows", rows)
+        self.max_rows = self.rows if max_rows is None else _size("max_rows", max_rows)
         if not isinstance(page_table, torch.Tensor) or page_table.dim() != 2:
             raise ValueError("page_table must be an [R][max_pages] tensor")
         R, W = page_table.shape
@@ -645,8 +656,7 @@ class PagedBatch:
         for name, t, shp in (("page_table", page_table, (R, W)), ("row_start", row_start, (R,)),
                              ("row_count", row_count, (R,)), ("prefix_len", prefix_len, (R,))):
             _device_tensor(name, t, torch.int32, shp, self.idx)
-        self.requests, self.max_pages, self.rows = R, W, int(rows)
-        self.max_rows = self.rows if max_rows is None else int(max_rows)
+        self.requests, self.max_pages = R, W
         self.device = page_table.device
         self._keep = (row_start, row_count, prefix_len, page_table)
         self.sizes = self.requests, self.max_pages, self.rows, self.max_rows
@@ -754,13 +764,13 @@ class PagedAttention:
 
     def __init__(self, batch, q_heads, kv_heads, head_dim, page_size, scale=None):
         self.sizes = batch.sizes
-        self.q_heads, self.kv_heads, self.head_dim = q_heads, kv_heads, head_dim
-        self.page_size = page_size
+        self.q_heads, self.kv_heads = _size("q_heads", q_heads), _size("kv_heads", kv_heads)
+        self.head_dim, self.page_size = _size("head_dim", head_dim), _size("page_size", page_size)
         self.scale = float(scale) if scale is not None else head_dim ** -0.5
-        c = _PagedCache(None, None, kv_heads * page_size * head_dim, 1, page_size, kv_heads,
-                        head_dim, BF16)
+        Hkv, P, D = self.kv_heads, self.page_size, self.head_dim
+        c = _PagedCache(None, None, Hkv * P * D, 1, P, Hkv, D, BF16)
         self.ws_bytes = int(lib().pctree_paged_attention_workspace_bytes(
-            ctypes.byref(c), batch._ref, q_heads))
+            ctypes.byref(c), batch._ref, self.q_heads))
         self.idx = batch.idx
         self._ws = _Workspace(self.ws_bytes, batch.device)
         self.workspace = self._ws.tensor
@@ -811,6 +821,7 @@ def compact_paged(pool, page_table, prefix_len, accept_node, accept_len, budget,
     ``pool [groups][pages][heads][page_size][...]`` (e.g. every layer's K and V):
     the dimensions past ``page_size`` form a slot of a head, a multiple of 16 bytes;
     groups and pages may lie apart."""
+    budget = _size("budget", budget)
     if not isinstance(pool, torch.Tensor) or not pool.is_cuda or pool.dim() < 5 or \
             not (pool.is_contiguous() or pool[0, 0].is_contiguous()):
         raise ValueError("pool must be a [groups][pages][heads][page_size][...] device tensor "
@@ -844,7 +855,7 @@ class Sampler:
     repeated calls (calls that may overlap need an object each)."""
 
     def __init__(self, rows, vocab, device="cuda"):
-        self.rows, self.vocab = rows, vocab
+        self.rows, self.vocab = _size("rows", rows), _size("vocab", vocab)
         nb = int(lib().pctree_sample_workspace_bytes(rows, vocab))
         if nb == 0:
             _check(lib().pctree_sample(None, F32, rows, vocab, vocab, *([None] * 8), 0, None),

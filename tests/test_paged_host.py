@@ -168,3 +168,20 @@ def test_compaction_refuses_groups_that_overlap(kw):
     st = P.lib().pctree_compact_paged(A, a["group_stride"], a["page_stride"], 4, 10, 8, 16, 256, A, 20, A, A, A, 2,
                                       64, 16, None)
     assert st == P.ERR_INVALID_ARGUMENT
+
+
+@pytest.mark.parametrize("x", [(1 << 32) + 2, 1 << 31, -(1 << 32) + 2])
+def test_binding_refuses_sizes_past_31_bits(x):
+    """A size that the C interface cannot hold is not cut to its low bits."""
+    i, table = torch.zeros(3, dtype=torch.int32), torch.zeros(3, 4, dtype=torch.int32)
+    pool = torch.zeros(1, 4, 2, 16, 64)
+
+    class Batch:
+        sizes, idx, _ref = (3, 4, 2, 2), 0, ctypes.byref(batch())
+    for call in (lambda: P.PagedBatch(i, i, i, table, x), lambda: P.PagedBatch(i, i, i, table, 2, x),
+                 lambda: P.PagedAttention(Batch, x, 2, 128, 16), lambda: P.PagedAttention(Batch, 2, x, 128, 16),
+                 lambda: P.PagedAttention(Batch, 2, 2, x, 16), lambda: P.PagedAttention(Batch, 2, 2, 128, x),
+                 lambda: P.compact_paged(pool, table, i, i[:, None], i, x), lambda: P.Sampler(x, 100, device="cpu"),
+                 lambda: P.Sampler(2, x, device="cpu")):
+        with pytest.raises(ValueError, match="2\\^31"):
+            call()
