@@ -21,8 +21,9 @@ pctree_status check_cache(const pctree_paged_cache* c) {
   if (!c || c->pages < 1 || c->page_size < 1 || c->kv_heads < 1 || c->head_dim < 1)
     return PCTREE_ERR_INVALID_ARGUMENT;
   if (c->dtype != PCTREE_BF16 && c->dtype != PCTREE_F16) return PCTREE_ERR_INVALID_ARGUMENT;
+  // (a page of so many elements could pass 63 bits)
   if (c->page_stride % 8 != 0 ||
-      c->page_stride < (int64_t)c->kv_heads * c->page_size * c->head_dim)
+      c->page_stride / ((int64_t)c->page_size * c->head_dim) < c->kv_heads)
     return PCTREE_ERR_INVALID_ARGUMENT;
   if ((c->head_dim != 64 && c->head_dim != 128) || c->page_size > PCTREE_MAX_PAGE_SIZE ||
       (c->page_size & (c->page_size - 1)) != 0 || c->kv_heads > 65535 ||

@@ -185,3 +185,10 @@ def test_binding_refuses_sizes_past_31_bits(x):
                  lambda: P.Sampler(2, x, device="cpu")):
         with pytest.raises(ValueError, match="2\\^31"):
             call()
+
+
+def test_pages_of_more_elements_than_64_bits_hold():
+    """2^64 elements a page: larger than any page stride."""
+    big = dict(kv_heads=1 << 24, page_size=1 << 20, head_dim=1 << 20, page_stride=1 << 20)
+    assert do_append(c=cache(**big)) == P.ERR_INVALID_ARGUMENT
+    assert do_attention(c=cache(**big)) == P.ERR_INVALID_ARGUMENT
