@@ -165,6 +165,25 @@ def test_tree_rows(D, Hq, Hkv, N, R, page):
     run_attention(b, Hq, Hkv, D, page, torch.bfloat16, tree=True)
 
 
+@pytest.mark.parametrize("Hq,Hkv,D", [(2, 2, 128), (8, 2, 64), (5, 1, 128)])
+@pytest.mark.parametrize("N,counts", [(1024, [1024, 5, 701]), (1000, [31, 1000, 999])])
+def test_tree_rows_of_wide_masks(Hq, Hkv, D, N, counts):
+    """Masks of up to 32 words a row, counts below the budget, prefixes of no whole word."""
+    rng = np.random.default_rng((N, Hq))
+    b = make_batch(rng, [N] * 3, [37, 130, 3], 32)
+    b["row_count"] = np.array(counts, np.int32)
+    run_attention(b, Hq, Hkv, D, 32, torch.bfloat16, tree=True)
+
+
+@pytest.mark.parametrize("Hq,Hkv,D,dt", [(4, 2, 128, torch.bfloat16), (6, 1, 64, torch.float16)])
+def test_trees_of_few_rows_beside_many(Hq, Hkv, D, dt):
+    """One masked call whose requests go to both kernels, whole and cut into runs."""
+    rng = np.random.default_rng(Hq)
+    rows = [1, 200, 3, 5, 0, 90, 2, 1]
+    b = make_batch(rng, rows, [50, 129, 0, 2100, 10, 1700, 300, 1], 16)
+    run_attention(b, Hq, Hkv, D, 16, dt, tree=True, poison=False)
+
+
 def test_trees_in_padded_rows():
     """Trees of fewer nodes than the budget, in the builder's [R][N] layout."""
     rng = np.random.default_rng(3)
@@ -182,6 +201,14 @@ def test_longer_chunks(D, rows, ctx):
     run_attention(b, 4, 2, D, 64, torch.bfloat16, poison=ctx < 1000)
 
 
+@pytest.mark.parametrize("rows,ctx", [([1], [70001]), ([1, 1], [33000, 20]), ([40], [20000])])
+def test_long_contexts(rows, ctx):
+    """Runs of thousands of slots."""
+    rng = np.random.default_rng(ctx[0])
+    b = make_batch(rng, rows, ctx, 64)
+    run_attention(b, 2, 1, 64, 64, torch.bfloat16, poison=False)
+
+
 def test_mixed_rows():
     rng = np.random.default_rng(8)
     rows = [1, 1, 1, 200, 1, 1, 90, 1, 4, 1]
@@ -197,6 +224,16 @@ def test_many_requests(R, Hq, Hkv, D):
     rows[3] = 40
     b = make_batch(rng, rows, rng.integers(0, 300, R), 16)
     run_attention(b, Hq, Hkv, D, 16, torch.bfloat16)
+
+
+@pytest.mark.parametrize("R", [64, 65, 129])
+def test_many_trees(R):
+    """Masked rows of more requests than a wave has lanes, in both kernels."""
+    rng = np.random.default_rng(R)
+    rows = rng.choice([0, 1, 4, 7], R)
+    rows[R - 2] = 60
+    b = make_batch(rng, rows, rng.integers(0, 200, R), 16)
+    run_attention(b, 4, 2, 64, 16, torch.bfloat16, tree=True)
 
 
 @pytest.mark.parametrize("Hq,Hkv,D", [(4, 1, 64), (6, 3, 64), (8, 4, 128)])
@@ -300,6 +337,30 @@ def test_what_masked_slots_hold(dt, bad):
                 assert np.array_equal(np.isfinite(o), np.isfinite(got[t])), t
                 ok = np.isfinite(o)
                 assert np.abs(got[t] - o)[ok].max(initial=0) < 0.05
+
+
+@pytest.mark.parametrize("n", [6, 50])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+def test_what_masked_slots_hold_to_the_tolerance(n, bad):
+    """As above, in requests of few rows and of many, to the tolerance of the file's head:
+    nothing of such a slot reaches the rows that do not admit it."""
+    rng = np.random.default_rng(n)
+    D, page, prefix = 128, 16, 70
+    b = make_batch(rng, [n, n, n], [prefix, 0, 300], page)
+    for dt in DTYPES:
+        for tree in (False, True):
+            q, k, v, mask, _ = run_attention(b, 4, 2, D, page, dt, tree=tree, poison=False)
+            for j in (1, n // 2, n - 1):
+                at = PO.place(b, 0, prefix + j, page, b["pages"])
+                v[at[0], 1, at[1], 5 * j:] = bad
+            at = PO.place(b, 1, n // 2, page, b["pages"])
+            v[at[0], 0, at[1]] = bad
+            k[at[0], 1, at[1], 7] = bad
+            at = PO.place(b, 2, 300 + n - 1, page, b["pages"])
+            k[at[0], :, at[1]] = float("nan")
+            v[at[0], :, at[1]] = bad
+            out = P.paged_attention(q, k, v, dev_batch(b), mask=mask)
+            check_attention(b, q, k, v, out, D ** -0.5, mask, n)
 
 
 def test_clamped_batches():
@@ -412,6 +473,21 @@ def test_append(dt, D, rot, Hq, Hkv, page, interleaved, norm):
                     assert (gk[p, :, o] == 9.0).all() and (gv[p, :, o] == -9.0).all()
 
 
+def test_append_rows_of_many_requests():
+    """Every row finds its request among more than a wave has lanes."""
+    rng = np.random.default_rng(6)
+    R, page, D = 150, 16, 64
+    b = make_batch(rng, rng.choice([0, 1, 3], R), rng.integers(0, 60, R), page, gap=1)
+    k, v = (torch.randn(b["rows"], 2, D, generator=_gen(i)).to(torch.bfloat16).cuda() for i in (1, 2))
+    kc, vc = (torch.full((b["pages"], 2, page, D), 9.0, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    P.append_paged(dev_batch(b), kc, vc, k, v)
+    kw, vw = torch.full_like(kc, 9.0), torch.full_like(vc, 9.0)
+    for r, t, i, prefix, n in PO.live_rows(b, page):
+        p, o = PO.place(b, r, prefix + i, page, b["pages"])
+        kw[p, :, o], vw[p, :, o] = k[t], v[t]
+    assert torch.equal(kc, kw) and torch.equal(vc, vw)
+
+
 def test_append_many_rows_in_place():
     """Enough rows for one wave each, q written over itself, keys only."""
     rng = np.random.default_rng(2)
@@ -500,6 +576,25 @@ def test_compact(page):
         return torch.from_numpy(x).cuda()
     got = P.compact_paged(pool, up(table), up(prefix), up(node), up(alen), N)
     assert got is pool and np.array_equal(_np(pool), want)
+
+
+@pytest.mark.parametrize("n", [1, 2, 9, 17, 63])
+def test_compact_of_groups_inside_pages(n):
+    """Keys and values of a page side by side, paths of one batch of moves and of several."""
+    rng = np.random.default_rng(n)
+    R, N, page = 3, 80, 16
+    prefix = rng.integers(0, 50, R).astype(np.int32)
+    b = make_batch(rng, [N] * R, prefix, page)
+    node = np.stack([np.concatenate([[0], np.sort(rng.choice(np.arange(1, N), n, replace=False))])
+                     for _ in range(R)]).astype(np.int32)
+    alen = np.array([n, n, n - 1], np.int32)
+    pool = torch.randn(b["pages"], 2, 2, page, 8, generator=_gen(n)).to(torch.bfloat16).cuda().transpose(0, 1)
+    want = PO.compact(_np(pool), b["page_table"], prefix, node, alen, N)
+
+    def up(x):
+        return torch.from_numpy(x).cuda()
+    P.compact_paged(pool, up(b["page_table"]), up(prefix), up(node), up(alen), N)
+    assert np.array_equal(_np(pool), want)
 
 
 def test_compact_checks_the_nodes_that_stay():
