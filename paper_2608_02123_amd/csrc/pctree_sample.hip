@@ -1576,7 +1576,12 @@ __global__ __launch_bounds__(kPickThreads) __attribute__((amdgpu_waves_per_eu(4)
   const Params q = params_of(a, t);
   const bool border = q.p < 1.0;
   if (o.state == 2 || (border && (o.bin >= kBins - 1 || o.n > kList || o.limit <= 0.0))) {
-    whole_row<DT>(a, t, row, q, o.mx, sh);
+    // (a function of its own takes its arguments from scratch: copies, so that nothing of
+    // the kernel's lies there, whose rows mostly are done)
+    const SampleArgs args = a;
+    const Row alone = row;
+    const Params par = q;
+    whole_row<DT>(args, t, alone, par, o.mx, sh);
     return;
   }
   uint64_t last = 0;

@@ -97,3 +97,13 @@ def test_a_batch_of_moves_is_loaded_together(kernel, tmp_path):
             run = 0
         most = max(most, run)
     assert most == 8, most
+
+
+def test_a_settled_row_costs_no_scratch(tmp_path):
+    """finish_kernel looks at its row before anything of it goes through scratch."""
+    code = _instructions(P.LIB_PATH, tmp_path)
+    kernels = [c for n, c in code.items() if "finish_kernel" in n]
+    assert len(kernels) == 3
+    for ins in kernels:
+        first = next(i for i, line in enumerate(ins) if line.startswith("s_cbranch"))
+        assert not [line for line in ins[:first] if line.startswith("scratch_")]
