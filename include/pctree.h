@@ -345,7 +345,9 @@ typedef struct pctree_paged_batch {
   int32_t requests;          /* R                                            */
   int32_t max_pages;         /* width of the page table                      */
   int32_t rows;              /* T: rows of q, k, v and out, below 2^24       */
-  int32_t max_rows;          /* the most rows that a request has, <= rows    */
+  int32_t max_rows;          /* the most rows that a request has, <= rows (work is
+                                planned for it: more than the true most costs
+                                workgroups that find nothing)                */
 } pctree_paged_batch;
 
 /* New rows of one layer.  Head h of row t starts at element t * row_stride +
@@ -426,8 +428,9 @@ pctree_status pctree_paged_attention(const pctree_paged_cache* cache,
  * A logit of -inf (a masked token) or NaN is never taken; a row of nothing else
  * gives token -1, logprob -inf; +inf logits share the row among themselves.
  * Weights below e^-700 count as 0; a NaN uniform as 0, a NaN top_p or min_p as
- * off.  Weights and their sums are float64: the same row gives the same token
- * wherever it lies and whatever else is in the call.
+ * off.  Weights and their sums are float64, added in an order that depends on
+ * the row and its alignment alone: it gives the same token whatever else is in
+ * the call.
  *
  * The sampled tokens of a tree's nodes are the target_next of
  * pctree_accept_greedy: following the children that match them is then sampling

@@ -69,7 +69,7 @@ constexpr double kBinStep = 0.98449643700540841;  // e^(-1/64)
 constexpr double kLowest = -700.0;    // weights below e^-700 are 0
 constexpr double kLog2e = 1.4426950408889634074;
 
-// 2^r, |r| <= 1/2, by its Taylor series (the thirteenth term is below 2^-53).
+// 2^r, |r| <= 1/2, by its Taylor series (the first term left out, the thirteenth, is below 2^-52).
 __device__ __forceinline__ double exp2_small(double r) {
   constexpr double L = 0.69314718055994530942;
   constexpr double c1 = L, c2 = c1 * L / 2, c3 = c2 * L / 3, c4 = c3 * L / 4, c5 = c4 * L / 5,
@@ -349,7 +349,8 @@ __device__ __forceinline__ double wave_sums(double (&v)[N]) {
   }
 }
 
-// Bytes bound it: 512 bf16 rows of 151936, 156 MB, in 43 us (3.6 TB/s); 3 us for one row.
+// Bytes bound it where rows filter: 512 bf16 rows of 151936, 156 MB, in 43 us (3.6 TB/s); 3
+// us for one row.  Where no row does, the float64 exponentials of all weights do: 98 us.
 template <int DT, int BPW>
 __global__ __launch_bounds__(kScanThreads) void scan_kernel(SampleArgs a, int segs) {
   const int t = blockIdx.x / segs, seg = blockIdx.x % segs;
@@ -973,7 +974,8 @@ __device__ uint64_t nth_equal(const SampleArgs& a, const Row& row, uint32_t cut,
 }
 
 // The whole row by one workgroup: cuts it by histograms and draws.  What is kept at
-// the end is every logit whose key is at least `last`.
+// the end is every logit whose key is at least `last`.  (A top_k of 2000 over 150,000
+// logits takes it: 241 us a call of one row, 508 of 512.)
 template <int DT>
 __device__ __noinline__ void whole_row(const SampleArgs& a, int t, const Row& row, const Params& q,
                                        float mx, PickShared& sh) {
@@ -1635,9 +1637,10 @@ hipError_t launch(SampleArgs a, hipStream_t stream) {
     if (filters) {
       pick_kernel<DT, true><<<(unsigned)a.T, kPickThreads, 0, stream>>>(a);
       // Rows are left to histograms by a top_p or min_p only.  (In every call that has one,
-      // though its rows may all be settled, which these two launches then make 4 us longer,
-      // 18.0 to 22.0 for one row of 150,000 logits with a top_k of 50: an open one among
-      // them takes 64 us, and 437 by one workgroup.)
+      // though its rows may all be settled, which then costs two empty launches: one row of
+      // 150,000 logits with a top_k of 50 and a top_p takes 17.9 us in a graph, 16.1 without,
+      // and 22.9 for 16.8 where the host issues them.  An open row takes 64, and 437 by one
+      // workgroup.)
       if (a.has & (kHasTopP | kHasMinP)) {
         const int per = W * (many ? kManyBlocks : kFewBlocks);
         const int parts = (a.nb + per - 1) / per;

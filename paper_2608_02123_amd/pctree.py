@@ -643,7 +643,8 @@ class PagedBatch:
     page ``page_table[r][slot // page_size]`` (an entry that is no page's index
     stands for no page).  All are int32 device tensors whose contents may change
     from call to call; ``rows`` is the row count of q, k, v and out, ``max_rows``
-    the most rows any request has (``rows`` if not given).
+    the most rows any request has.  Give it: without it one request may have them
+    all, and the attention is planned for that (64 single tokens 241 us for 204).
     """
 
     def __init__(self, row_start, row_count, prefix_len, page_table, rows, max_rows=None):
