@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import math
+import operator
 import os
 
 import torch
@@ -617,7 +618,7 @@ class _Workspace:
 def _size(name, x):
     """``x`` as an int that the C interface can take (ctypes keeps the low 32 bits of
     another one)."""
-    x = int(x)
+    x = operator.index(x)
     if not -2 ** 31 <= x < 2 ** 31:
         raise ValueError(f"{name} must lie in [-2^31, 2^31), got {x}")
     return x
@@ -648,8 +649,8 @@ class PagedBatch:
     """
 
     def __init__(self, row_start, row_count, prefix_len, page_table, rows, max_rows=None):
-        self.rows = _size("rows", rows)
-        self.max_rows = self.rows if max_rows is None else _size("max_rows", max_rows)
+        self.rows = _size("rows", int(rows))
+        self.max_rows = self.rows if max_rows is None else _size("max_rows", int(max_rows))
         if not isinstance(page_table, torch.Tensor) or page_table.dim() != 2:
             raise ValueError("page_table must be an [R][max_pages] tensor")
         R, W = page_table.shape

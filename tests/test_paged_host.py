@@ -187,6 +187,15 @@ def test_binding_refuses_sizes_past_31_bits(x):
             call()
 
 
+def test_binding_refuses_sizes_that_are_no_integers():
+    class Batch:
+        sizes, idx, _ref = (3, 4, 2, 2), 0, ctypes.byref(batch())
+    for call in (lambda: P.PagedAttention(Batch, 2.5, 2, 128, 16), lambda: P.Sampler(2.5, 100, device="cpu"),
+                 lambda: P.compact_paged(torch.zeros(1, 4, 2, 16, 64), None, None, None, None, 8.5)):
+        with pytest.raises(TypeError):
+            call()
+
+
 def test_pages_of_more_elements_than_64_bits_hold():
     """2^64 elements a page: larger than any page stride."""
     big = dict(kv_heads=1 << 24, page_size=1 << 20, head_dim=1 << 20, page_stride=1 << 20)
