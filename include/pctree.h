@@ -465,6 +465,156 @@ pctree_status pctree_compact_paged(void* pool, int64_t group_stride, int64_t pag
                                    const int32_t* accept_len, int32_t requests, int32_t budget,
                                    int32_t max_depth, void* stream);
 
+/* ---------------------------------------------------------------------
+ * Pages in 8 bits.  A slot's keys and values are e4m3 numbers (bits s eeee mmm,
+ * bias 7, 0x7f and 0xff NaN, no infinities) times the scale of their block: of
+ * each page and kv head, `block` consecutive slots share a byte s, scale
+ * 2^(s - 127).  Written scales lie in [16, 246]; other bytes are read as the
+ * nearer end.  For a set of values, s is the smallest with which the largest
+ * finite magnitude is at most 448 times the scale (246 for larger ones), and x is
+ * held as x / scale, rounded to nearest even; infinities, NaN, and magnitudes
+ * above 464 * 2^119, as NaN.
+ *
+ * The calls are those over 16-bit pages, with what follows; sizes, clamping,
+ * masks and errors are the same.
+ * --------------------------------------------------------------------- */
+
+typedef struct pctree_paged_cache8 {
+  pctree_paged_cache pages; /* k and v hold bytes: page_stride is in bytes, a multiple
+                               of 16; dtype is that of the rows (q, k, v, q_out, out) */
+  uint8_t* k_scale;         /* [pages][Hkv][page_size / block]                        */
+  uint8_t* v_scale;
+  int64_t scale_stride;     /* bytes between two pages' scales, >= Hkv * page_size / block */
+  int32_t block;            /* 8, 16, 32 or 64, at most page_size                     */
+} pctree_paged_cache8;
+
+/* A block that takes new rows gets the scale of their set, or keeps its own where
+ * slots below prefix_len lie in it and it is the larger; under a grown scale those
+ * slots are held again, rounded once more.  Its other slots keep their bytes, which
+ * stand for nothing until a row is put there.  A block that takes new rows belongs
+ * to one request. */
+pctree_status pctree_append_paged8(const pctree_paged_cache8* cache,
+                                   const pctree_paged_batch* batch, const pctree_append* rows,
+                                   void* stream);
+
+size_t pctree_paged_attention8_workspace_bytes(const pctree_paged_cache8* cache,
+                                               const pctree_paged_batch* batch, int32_t q_heads);
+
+/* The held values enter the products as they are; with float16 rows they are rounded
+ * to float16, and beyond its range infinite, as 16-bit pages would have them. */
+pctree_status pctree_paged_attention8(const pctree_paged_cache8* cache,
+                                      const pctree_paged_batch* batch, const void* q,
+                                      int32_t q_heads, float scale, const uint32_t* mask,
+                                      int32_t budget, void* out, void* workspace,
+                                      size_t workspace_bytes, void* stream);
+
+/* pool: per group `pages` pages of [heads][page_size][head_dim] bytes; scale: of
+ * [heads][page_size / block] bytes, group g's page p at byte g * scale_group_stride +
+ * p * scale_page_stride.  A block that takes accepted rows gets the largest of their
+ * scales and, where slots below prefix_len lie in it, of its own; rows and those slots
+ * are held again where their scale was smaller.  A request whose accepted nodes all
+ * stay in place is left untouched. */
+pctree_status pctree_compact_paged8(void* pool, int64_t group_stride, int64_t page_stride,
+                                    uint8_t* scale, int64_t scale_group_stride,
+                                    int64_t scale_page_stride, int32_t groups, int32_t pages,
+                                    int32_t heads, int32_t page_size, int32_t head_dim,
+                                    int32_t block, const int32_t* page_table, int32_t max_pages,
+                                    const int32_t* prefix_len, const int32_t* accept_node,
+                                    const int32_t* accept_len, int32_t requests, int32_t budget,
+                                    int32_t max_depth, void* stream);
+
+/* ---------------------------------------------------------------------
+ * Residual addition and root-mean-square norm, before a projection: v = x +
+ * residual, residual <- v, y = v / sqrt(mean(v^2) + eps) * weight, for every row.
+ * Without `scale`, out is y in dtype; with it, out holds e4m3 bytes y / c, c =
+ * max |y| / 448 over each `group` elements of the row (the last group may be
+ * shorter), in scale (infinite and NaN elements do not count and are held as NaN;
+ * a group of zeros has scale 0).  float32 throughout, each output rounded once; v
+ * is not rounded before it is normed.
+ * --------------------------------------------------------------------- */
+#define PCTREE_MAX_NORM_WIDTH 32768
+
+typedef struct pctree_norm {
+  const void* x;        /* [rows][width] dtype                                       */
+  const void* weight;   /* [width] dtype, or NULL: ones                              */
+  void* residual;       /* [rows][width] dtype, updated, or NULL                     */
+  void* out;            /* [rows][width] dtype (may be x itself), or bytes           */
+  float* scale;         /* [rows][(width + group - 1) / group], or NULL: 16-bit out  */
+  int64_t x_stride;     /* row strides in elements, >= width, multiples of 8         */
+  int64_t residual_stride;
+  int64_t out_stride;
+  int32_t rows;         /* T, at most 2^21                                           */
+  int32_t width;        /* a multiple of 8, at most PCTREE_MAX_NORM_WIDTH            */
+  int32_t group;        /* 32, 64, 128 or 256; 0: the row (ignored without scale)    */
+  int32_t dtype;        /* PCTREE_BF16 or PCTREE_F16                                 */
+  float eps;            /* >= 0                                                      */
+} pctree_norm;
+
+/* Errors: INVALID_ARGUMENT (null or misaligned pointer: 16 bytes, 8 for out in bytes, 4
+ * for scale; a size or stride that the comments rule out), UNSUPPORTED (width or rows past
+ * the limits). */
+pctree_status pctree_rms_norm(const pctree_norm* args, void* stream);
+
+/* ---------------------------------------------------------------------
+ * Penalties, biases and a grammar's mask, on logits in place, before
+ * pctree_sample.  Row row_start[r] + i, i < row_count[r], of logits is request
+ * r's i-th row (a tree's node i); other rows are neither read nor written.  For
+ * each of its tokens, with x the logit:
+ *  - c counts the token among history[history_start[r] + prompt_count[r] ...] (the
+ *    request's history_count[r] tokens after its first prompt_count[r]) and, with
+ *    `token` and `mask`, among node i and its ancestors, token[r][j] for every bit
+ *    j < row_count[r] of mask row [r][i] (as from pctree_build_mask; the history then
+ *    ends before the tree's root);
+ *  - if c > 0 or the token is among the first prompt_count[r]: x / repetition[r] where
+ *    x > 0, else x * repetition[r];
+ *  - if c > 0: x - frequency[r] * c - presence[r];
+ *  - x + value of the last of the request's bias entries for the token;
+ *  - -inf where bit token % 32 of word token / 32 of the row's mask is not set.
+ * float32, one rounding at the end.  Logits that none of this concerns keep their
+ * bits.  Row t's mask is row allowed_row[t] of `allowed` (t itself where allowed_row is
+ * NULL); an index outside [0, masks) is no mask.
+ *
+ * Device arrays are clamped: starts and counts as in pctree_paged_batch (counts to
+ * `budget` with token), ranges of history and biases to their totals; tokens outside the
+ * vocabulary are ignored; a repetition that is not positive and finite counts as 1, an
+ * infinite or NaN frequency or presence as 0.
+ * --------------------------------------------------------------------- */
+typedef struct pctree_adjust {
+  void* logits;                 /* [rows][vocab] dtype, in place                       */
+  int64_t row_stride;           /* elements, >= vocab                                  */
+  const int32_t* row_start;     /* [R]                                                 */
+  const int32_t* row_count;     /* [R]                                                 */
+  const int32_t* history;       /* [history_total], or NULL                            */
+  const int32_t* history_start; /* [R], or NULL iff history is                         */
+  const int32_t* history_count; /* [R], or NULL iff history is                         */
+  const int32_t* prompt_count;  /* [R], or NULL: 0                                     */
+  const float* repetition;      /* [R], or NULL: 1                                     */
+  const float* frequency;       /* [R], or NULL: 0                                     */
+  const float* presence;        /* [R], or NULL: 0                                     */
+  const int32_t* bias_token;    /* [bias_total], or NULL                               */
+  const float* bias_value;      /* [bias_total], or NULL iff bias_token is             */
+  const int32_t* bias_start;    /* [R], or NULL iff bias_token is                      */
+  const int32_t* bias_count;    /* [R], or NULL iff bias_token is                      */
+  const int32_t* token;         /* [R][budget], or NULL                                */
+  const uint32_t* mask;         /* [R][budget][(budget+31)/32], or NULL iff token is   */
+  const uint32_t* allowed;      /* [masks][(vocab+31)/32], or NULL                     */
+  const int32_t* allowed_row;   /* [rows], or NULL                                     */
+  int32_t rows;                 /* T                                                   */
+  int32_t vocab;
+  int32_t requests;             /* R                                                   */
+  int32_t max_rows;             /* the most rows that a request has, <= rows           */
+  int32_t history_total;        /* below 2^29                                          */
+  int32_t bias_total;
+  int32_t budget;               /* N (0 where token is NULL)                           */
+  int32_t masks;                /* rows of allowed (at least `rows` without allowed_row) */
+  int32_t dtype;                /* PCTREE_F32, PCTREE_BF16 or PCTREE_F16               */
+} pctree_adjust;
+
+/* Errors: INVALID_ARGUMENT (null or misaligned pointer, a size that the comments rule
+ * out), UNSUPPORTED (vocab > PCTREE_MAX_VOCAB, requests > 65535, budget >
+ * PCTREE_MAX_MASK_BUDGET, history_total past its limit). */
+pctree_status pctree_adjust_logits(const pctree_adjust* args, void* stream);
+
 /* Static, human-readable name of a status code. */
 const char* pctree_status_string(pctree_status status);
 

@@ -13,7 +13,8 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libpctree.so")
 SOURCES = ["pctree_api.hip", "pctree_kernels.hip", "pctree_profile.hip", "pctree_verify.hip",
            "pctree_attention.hip", "pctree_paged.hip", "pctree_paged_attention.hip",
-           "pctree_paged_api.hip", "pctree_sample.hip"]
+           "pctree_paged_api.hip", "pctree_sample.hip", "pctree_held.hip", "pctree_norm.hip",
+           "pctree_adjust.hip", "pctree_step_api.hip"]
 ARCH = "gfx950"
 
 

@@ -1,0 +1,299 @@
+// A paged cache in 8 bits (pctree_held.h): new rows into their pages, and compaction
+// after acceptance.  A block of slots of one head has one scale, so a block, not a row,
+// is what a wave writes.
+#include "pctree.h"
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <algorithm>
+
+#include "pctree_held.h"
+#include "pctree_paged.h"
+#include "pctree_rows.h"
+#include "pctree_tile.h"
+
+namespace pctree {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kWaves = kThreads / 64;
+
+__device__ __forceinline__ float wave_max(float v) {
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
+  return v;
+}
+
+// The queries of row t: `part` of `split` waves, 512 / D heads at a time.
+template <int D, bool H>
+__device__ __forceinline__ void append_queries(const AppendArgs& a, int t, int part, int split) {
+  constexpr int LPH = D / 8, HPW = 64 / LPH;
+  const int lane = threadIdx.x & 63, e0 = (lane % LPH) * 8;
+  const int r = request_of_row(a.b, t);
+  if (r < 0) return;
+  const PagedReq rq = paged_req(a.b, r);
+  const bool turns = a.rope && e0 < a.rot;
+  Turn turn;
+  if (turns) load_turn(a, a.position ? a.position[t] : rq.prefix + (t - rq.start), e0, turn);
+  for (int i0 = part * HPW; i0 < a.Hq; i0 += split * HPW) {
+    const int h = i0 + lane / LPH;
+    u32x4 x = {0u, 0u, 0u, 0u};
+    if (h < a.Hq) x = *(const u32x4*)(a.q + t * a.q_stride + h * D + e0);
+    float y[8];
+    unpack8<H>(x, y);
+    if (a.q_norm) norm_head<D, H>(y, a.q_norm, a.eps, e0);
+    if (a.rope) turn_head<D>(a, y, turn, e0, turns);
+    if (h < a.Hq) *(u32x4*)(a.q_out + t * a.q_out_stride + h * D + e0) = pack8<H>(y);
+  }
+}
+
+// The n new rows t .. of a block of G slots, the first at offset o0 (slots below it hold
+// rows from before), of one head of the keys or the values: the rows stay in registers
+// between their largest magnitude and their rounding.
+template <int D, bool H, int G>
+__device__ __forceinline__ void append_block(const AppendArgs& a, bool keys, int h, int t, int n,
+                                             int o0, int slot0, uint8_t* block, uint8_t* scale) {
+  constexpr int LPH = D / 8, RPS = 64 / LPH, STEPS = G / RPS;  // lanes of a row, rows of a step
+  const int lane = threadIdx.x & 63, e0 = (lane % LPH) * 8, sub = lane / LPH;
+  const uint16_t* src = (keys ? a.k : a.v) + h * D + e0;
+  const long long stride = keys ? a.k_stride : a.v_stride;
+  u32x4 x[STEPS];
+#pragma unroll
+  for (int s = 0; s < STEPS; ++s)
+    x[s] = *(const u32x4*)(src + (t + min(max(s * RPS + sub - o0, 0), n - 1)) * stride);
+  const int was = o0 > 0 ? scale_in(*scale) : 0;
+  const bool turns = keys && a.rope && e0 < a.rot;
+  float y[STEPS][8];
+  float most = 0.0f;
+#pragma unroll
+  for (int s = 0; s < STEPS; ++s) {
+    if ((s + 1) * RPS <= o0 || s * RPS >= o0 + n) continue;  // (no new row: the same in every lane)
+    const int i = min(max(s * RPS + sub - o0, 0), n - 1);
+    unpack8<H>(x[s], y[s]);
+    if (keys) {
+      if (a.k_norm) norm_head<D, H>(y[s], a.k_norm, a.eps, e0);
+      if (a.rope) {
+        Turn turn;
+        if (turns) load_turn(a, a.position ? a.position[t + i] : slot0 + i, e0, turn);
+        turn_head<D>(a, y[s], turn, e0, turns);
+      }
+    }
+    // (lanes past the rows repeat one of them)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float m = fabsf(y[s][e]);
+      most = m < __builtin_inff() ? fmaxf(most, m) : most;
+    }
+  }
+  const int now = max(scale_of(wave_max(most)), was);
+  const float down = scale_down(now);
+#pragma unroll
+  for (int s = 0; s < STEPS; ++s) {
+    const int j = s * RPS + sub;
+    if (j < o0 || j >= o0 + n) continue;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) y[s][e] *= down;
+    *(uint2*)(block + j * D + e0) = hold8(y[s]);
+  }
+  if (now == was) return;
+  if (o0 > 0) {  // the rows from before under the grown scale
+    const float f = scale_up(127 - min(now - was, 126));
+    for (int j = sub; j < o0; j += RPS) {
+      uint2* p = (uint2*)(block + j * D + e0);
+      uint2 w = *p;
+      w.x = rescale4(w.x, f);
+      w.y = rescale4(w.y, f);
+      *p = w;
+    }
+  }
+  if (lane == 0) *scale = (uint8_t)now;
+}
+
+// Waves of queries first (qwaves of them, qsplit a row), then of keys and values: each
+// takes one head of one of them and, of `window` rows, the blocks whose first new row is
+// among these.
+template <int D, bool H, int G>
+__global__ __launch_bounds__(kThreads) void append8_kernel(AppendArgs a, HeldScales sc, int qblocks,
+                                                          int qsplit, int window) {
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  if ((int)blockIdx.x < qblocks) {
+    const int w = blockIdx.x * kWaves + wave;
+    if (w / qsplit < a.b.T) append_queries<D, H>(a, w / qsplit, w % qsplit, qsplit);
+    return;
+  }
+  const long long w = (long long)(blockIdx.x - qblocks) * kWaves + wave;
+  const int item = (int)(w % (2 * a.Hkv)), h = item % a.Hkv;
+  const bool keys = item < a.Hkv;
+  const long long t0 = w / (2 * a.Hkv) * window;
+  if (t0 >= a.b.T) return;
+  const int end = min((int)t0 + window, a.b.T);
+  const int blocks = 1 << (a.b.page_shift - sc.block_shift);  // of a page
+  for (int t = (int)t0; t < end;) {
+    const int r = request_of_row(a.b, t);
+    if (r < 0) {
+      ++t;
+      continue;
+    }
+    const PagedReq rq = paged_req(a.b, r);
+    const int i = t - rq.start, slot = rq.prefix + i, o0 = slot % G;
+    const int n = min(G - o0, rq.cnt - i);  // rows to the block's end
+    if (i == 0 || o0 == 0) {
+      const int page =
+          slot < a.b.C ? a.b.page_table[(size_t)r * a.b.max_pages + (slot >> a.b.page_shift)] : -1;
+      if ((unsigned)page < (unsigned)a.b.pages) {
+        const int off = slot & ((1 << a.b.page_shift) - 1);
+        uint8_t* block = (uint8_t*)(keys ? a.k_pages : a.v_pages) +
+                         ((size_t)page * a.b.page_units + (size_t)h * a.b.head_units) * 16 +
+                         (size_t)(off - o0) * D;
+        uint8_t* scale = (keys ? sc.k : sc.v) + (size_t)page * sc.stride + (size_t)h * blocks +
+                         (off >> sc.block_shift);
+        append_block<D, H, G>(a, keys, h, t, n, o0, slot, block, scale);
+      }
+    }
+    t += n;
+  }
+}
+
+template <int D, bool H, int G>
+hipError_t append(const AppendArgs& a, const HeldScales& s, hipStream_t stream) {
+  const int T = a.b.T;
+  int qsplit = 1;
+  long long qblocks = 0;
+  if (a.q) {
+    const int units = (a.Hq + 512 / D - 1) / (512 / D);
+    qsplit = std::max(1, std::min(units, 8192 / T));
+    qblocks = ((long long)T * qsplit + kWaves - 1) / kWaves;
+  }
+  const int window = (long long)T * 2 * a.Hkv <= 16384 ? 1 : G;
+  const long long waves = (long long)((T + window - 1) / window) * 2 * a.Hkv;
+  const long long blocks = qblocks + (waves + kWaves - 1) / kWaves;
+  append8_kernel<D, H, G><<<(unsigned)blocks, kThreads, 0, stream>>>(a, s, (int)qblocks, qsplit,
+                                                                        window);
+  return hipGetLastError();
+}
+
+template <int D, bool H>
+hipError_t append_blocks(const AppendArgs& a, const HeldScales& s, hipStream_t stream) {
+  switch (1 << s.block_shift) {
+    case 8: return append<D, H, 8>(a, s, stream);
+    case 16: return append<D, H, 16>(a, s, stream);
+    case 32: return append<D, H, 32>(a, s, stream);
+    case 64: return append<D, H, 64>(a, s, stream);
+  }
+  return hipErrorInvalidValue;
+}
+
+// Compaction: a wave moves the accepted rows of one (request, group, head).  All rows of
+// the path are in registers before the first store.  The scale of a block that takes
+// some of them is the largest of theirs and, where slots of the prefix lie in it, of
+// its own; rows under a smaller one are rounded to it.
+template <int D>
+__global__ __launch_bounds__(kThreads) void compact8_kernel(CompactHeldArgs a) {
+  constexpr int LPR = D / 16, RPS = 64 / LPR;         // lanes of a row, rows of a step
+  constexpr int STEPS = (PCTREE_MAX_BLOCK + 1) / RPS;  // of the longest path
+  const CompactPagedArgs& c = a.c;
+  const int lane = threadIdx.x & 63, req = blockIdx.y;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  const long long item = (long long)blockIdx.x * kWaves + wave;
+  const int len = c.accept_len[req], pre = c.prefix_len[req];
+  const long long capacity = (long long)c.max_pages << c.page_shift;
+  if (item >= (long long)c.groups * c.heads || len < 0 || len >= c.W || pre < 0) return;
+  const int* table = c.page_table + (size_t)req * c.max_pages;
+  // the path, a node to a lane, checked
+  const int node = lane <= len ? c.accept_node[(size_t)req * c.W + lane] : 0;
+  const int before = __shfl_up(node, 1, 64);
+  bool ok = true;
+  if (lane <= len)
+    ok = node >= 0 && node < c.N && (lane == 0 || node > before) && (long long)pre + node < capacity;
+  if (!__all(ok)) return;
+  if (!__any(lane <= len && node != lane)) return;  // nothing moves
+  const int src = pre + node, dst = pre + lane;
+  int ps = 0, pd = 0;
+  if (lane <= len) {
+    ps = table[src >> c.page_shift];
+    pd = table[dst >> c.page_shift];
+    ok = (unsigned)ps < (unsigned)c.pages && (unsigned)pd < (unsigned)c.pages;
+  }
+  if (!__all(ok)) return;
+  const int g = (int)(item / c.heads), h = (int)(item % c.heads);
+  const int pmask = (1 << c.page_shift) - 1, blocks = 1 << (c.page_shift - a.block_shift);
+  uint8_t* pool = (uint8_t*)c.pool + g * c.group_stride + ((size_t)h << c.page_shift) * D;
+  uint8_t* scales = a.scale + g * a.scale_group_stride + (size_t)h * blocks;
+  const auto scale_at = [&](int page, int slot) {
+    return scales + page * a.scale_page_stride + ((slot & pmask) >> a.block_shift);
+  };
+  const int theirs = lane <= len ? scale_in(*scale_at(ps, src)) : 0;
+  // (a row's place in the pool, from the lane that holds its node)
+  const long long from = ps * c.page_stride + (long long)(src & pmask) * D;
+  const long long to = pd * c.page_stride + (long long)(dst & pmask) * D;
+  const int sub = lane / LPR, e0 = (lane % LPR) * 16;
+  u32x4 x[STEPS];
+#pragma unroll
+  for (int s = 0; s < STEPS; ++s)
+    if (s * RPS <= len)
+      x[s] = *(const u32x4*)(pool + __shfl(from, min(s * RPS + sub, len), 64) + e0);
+  // each destination block's scale: a maximum over the lanes of its rows
+  const int b = (dst >> a.block_shift) - (pre >> a.block_shift);
+  const int kept = pre & ((1 << a.block_shift) - 1);  // slots of the prefix in the first
+  const int was = kept ? scale_in(*scale_at(__shfl(pd, 0, 64), pre)) : 0;
+  int now = 0;
+  const int last = __shfl(b, len, 64);
+  for (int i = 0; i <= last; ++i) {
+    int m = lane <= len && b == i ? theirs : 0;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) m = max(m, __shfl_xor(m, o, 64));
+    if (i == 0) m = max(m, was);
+    if (b == i) now = m;
+  }
+  const int now0 = __shfl(now, 0, 64);
+  if (kept && now0 > was) {  // the slots of the prefix under the grown scale
+    const float f = scale_up(127 - min(now0 - was, 126));
+    const long long base = __shfl(to, 0, 64) - (long long)kept * D;
+    for (int j = sub; j < kept; j += RPS) {
+      u32x4* p = (u32x4*)(pool + base + j * D + e0);
+      u32x4 w = *p;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) w[e] = rescale4(w[e], f);
+      *p = w;
+    }
+  }
+#pragma unroll
+  for (int s = 0; s < STEPS; ++s) {
+    if (s * RPS > len) break;
+    const int m = s * RPS + sub, mm = min(m, len);
+    const long long at = __shfl(to, mm, 64);
+    const int grow = __shfl(now - theirs, mm, 64);
+    const bool stays = __shfl(node, mm, 64) == mm;
+    if (m > len || (stays && grow == 0)) continue;
+    const float f = scale_up(127 - min(grow, 126));
+    u32x4 w = x[s];
+    if (grow) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) w[e] = rescale4(w[e], f);
+    }
+    *(u32x4*)(pool + at + e0) = w;
+  }
+  // (the first lane of a block's rows writes its scale)
+  const int b_before = __shfl_up(b, 1, 64);
+  if (lane <= len && (lane == 0 || b != b_before)) *scale_at(pd, dst) = (uint8_t)now;
+}
+
+}  // namespace
+
+hipError_t launch_append_held(const AppendArgs& a, const HeldScales& s, int D, bool f16,
+                              hipStream_t stream) {
+  if (D == 128)
+    return f16 ? append_blocks<128, true>(a, s, stream) : append_blocks<128, false>(a, s, stream);
+  return f16 ? append_blocks<64, true>(a, s, stream) : append_blocks<64, false>(a, s, stream);
+}
+
+hipError_t launch_compact_held(const CompactHeldArgs& a, hipStream_t stream) {
+  const long long items = (long long)a.c.groups * a.c.heads;
+  const dim3 grid((unsigned)((items + kWaves - 1) / kWaves), a.c.R);
+  if (a.c.slot_units == 8) compact8_kernel<128><<<grid, kThreads, 0, stream>>>(a);
+  else compact8_kernel<64><<<grid, kThreads, 0, stream>>>(a);
+  return hipGetLastError();
+}
+
+}  // namespace pctree

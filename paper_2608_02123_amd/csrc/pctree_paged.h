@@ -79,15 +79,26 @@ hipError_t launch_append(const AppendArgs& a, int D, bool f16, hipStream_t strea
 struct PagedPlan {
   int qblocks, few_qblocks;        // row blocks of a (request, kv head) at most
   int nsplit, few_nsplit;          // most slot runs of a request (1: no merge pass)
-  int least;                       // slots of the shortest run (the other kernel's is fixed)
+  int least, few_least;            // slots of the shortest run
   long long blocks, few_blocks;    // workgroups (XCD-grouped, padded; 0: not launched)
   int few, few_stride;             // the most rows of such a request
   size_t parts, few_parts;         // rows of partial results
   size_t ws_bytes;
 };
 
+// The scales beside a cache's pages in 8 bits (pctree_held.h): [pages][Hkv][page_size >>
+// block_shift] bytes, a page's `stride` bytes after the one before.
+struct HeldScales {
+  uint8_t* k;
+  uint8_t* v;
+  long long stride;
+  int block_shift;
+};
+
+// (Pages in 8 bits: k and v are bytes, b.page_units and b.head_units 16 of them.)
 struct PagedAttnArgs {
   PagedRows b;
+  HeldScales s;
   const uint16_t* q;     // [T][Hq][D]
   const uint16_t* k;
   const uint16_t* v;
@@ -98,15 +109,17 @@ struct PagedAttnArgs {
   float* few_o;          // [few_nsplit][R][Hkv][few_stride][D]
   float* few_ml;         // [few_nsplit][R][Hkv][few_stride][2]
   int Hq, Hkv, g, N, NW;
-  int qblocks, nsplit, least, few_qblocks, few_nsplit, few, few_stride;
+  int qblocks, nsplit, least, few_qblocks, few_nsplit, few_least, few, few_stride;
   float scale_log2;
 };
 
-PagedPlan plan_paged_attention(int R, int T, int max_rows, int Hq, int Hkv, int D, int C, int cus);
+// (held: pages in 8 bits)
+PagedPlan plan_paged_attention(int R, int T, int max_rows, int Hq, int Hkv, int D, int C, bool held,
+                               int cus);
 
 // (fills in what the plan and the workspace say)
 hipError_t launch_paged_attention(PagedAttnArgs a, const PagedPlan& plan, int D, bool f16,
-                                  void* workspace, hipStream_t stream);
+                                  bool held, void* workspace, hipStream_t stream);
 
 struct CompactPagedArgs {
   char* pool;

@@ -16,6 +16,7 @@
 #include <algorithm>
 
 #include "pctree_paged.h"
+#include "pctree_rows.h"
 #include "pctree_tile.h"
 
 namespace pctree {
@@ -42,36 +43,9 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendArgs a, in
   if ((unsigned)page >= (unsigned)a.b.pages) page = -1;
   const int e0 = (lane % LPH) * 8;  // the lane's first element of its head
 
-  // cos and sin of the lane's pairs
-  float cs[8], sn[8];
-  const int half = a.rot / 2;
   const bool turns = a.rope && e0 < a.rot;
-  if (turns) {
-    int pos = a.position ? a.position[t] : slot;
-    pos = min(max(pos, 0), a.positions - 1);
-    const float* row = a.rope + (size_t)pos * a.rot;
-    if (a.interleaved) {
-      const f32x4 c = *(const f32x4*)(row + e0 / 2), s = *(const f32x4*)(row + half + e0 / 2);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        cs[i] = c[i / 2];
-        sn[i] = s[i / 2];
-      }
-    } else {
-      const int p0 = e0 < half ? e0 : e0 - half;
-#pragma unroll
-      for (int i = 0; i < 8; i += 4) {
-        const f32x4 c = *(const f32x4*)(row + p0 + i), s = *(const f32x4*)(row + half + p0 + i);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          cs[i + j] = c[j];
-          sn[i + j] = s[j];
-        }
-      }
-    }
-  }
-  // the lane that holds the other element of each pair (halves)
-  const int partner = lane - (lane % LPH) + (e0 < half ? e0 + half : e0 - half) / 8;
+  Turn turn;
+  if (turns) load_turn(a, a.position ? a.position[t] : slot, e0, turn);
 
   const int qn = a.q ? a.Hq : 0, items = qn + 2 * a.Hkv;
   for (int i0 = part * HPW; i0 < items; i0 += split * HPW) {
@@ -84,47 +58,10 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendArgs a, in
                                       : a.v + t * a.v_stride + h * D;
     if (kind < 3 && (kind == 0 || page >= 0)) x = *(const u32x4*)(src + e0);
     float y[8];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      y[2 * i] = lo16<H>(x[i]);
-      y[2 * i + 1] = hi16<H>(x[i]);
-    }
-    const uint16_t* wt = kind == 0 ? a.q_norm : (kind == 1 ? a.k_norm : nullptr);
-    float ss = 0.0f;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) ss = __builtin_fmaf(y[i], y[i], ss);
-#pragma unroll
-    for (int o = 1; o < LPH; o <<= 1) ss += __shfl_xor(ss, o, 64);
-    if (wt) {
-      const float inv = 1.0f / sqrtf(ss * (1.0f / D) + a.eps);
-      const u32x4 w = *(const u32x4*)(wt + e0);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        y[2 * i] = y[2 * i] * inv * lo16<H>(w[i]);
-        y[2 * i + 1] = y[2 * i + 1] * inv * hi16<H>(w[i]);
-      }
-    }
-    if (a.rope) {
-      float z[8];
-      if (a.interleaved) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) z[i] = i & 1 ? y[i - 1] : -y[i + 1];
-      } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const float o = __shfl(y[i], partner, 64);
-          z[i] = e0 < half ? -o : o;
-        }
-      }
-      if (turns && kind < 2) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) y[i] = y[i] * cs[i] + z[i] * sn[i];
-      }
-    }
-    if (kind != 2) {  // (values keep their bits)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) x[i] = pack16<H>(y[2 * i], y[2 * i + 1]);
-    }
+    unpack8<H>(x, y);
+    norm_head<D, H>(y, kind == 0 ? a.q_norm : (kind == 1 ? a.k_norm : nullptr), a.eps, e0);
+    if (a.rope) turn_head<D>(a, y, turn, e0, turns && kind < 2);
+    if (kind != 2) x = pack8<H>(y);  // (values keep their bits)
     if (kind == 0) {
       *(u32x4*)(a.q_out + t * a.q_out_stride + h * D + e0) = x;
     } else if (kind < 3 && page >= 0) {

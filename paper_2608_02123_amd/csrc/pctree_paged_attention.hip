@@ -37,6 +37,7 @@
 
 #include <algorithm>
 
+#include "pctree_held.h"
 #include "pctree_lds.h"
 #include "pctree_paged.h"
 #include "pctree_tile.h"
@@ -59,6 +60,8 @@ constexpr int kMaxSplits = 32;
 constexpr int kFewRows = 32;
 constexpr int kFewChunk = 32;        // slots of a wave's step there
 constexpr int kFewRun = 4 * kFewChunk;  // the shortest run there, a chunk to each wave
+constexpr int kFewChunk8 = 64;       // the same over pages in 8 bits
+constexpr int kFewRun8 = 4 * kFewChunk8;
 constexpr int kMergeThreads = 256;
 constexpr int kMergeBatch = 8;
 constexpr int kMatrix = 0x8, kReadLds = 0x100;  // instruction classes of the scheduler
@@ -243,6 +246,32 @@ __device__ __forceinline__ uint32_t fine_pair(uint32_t w) {
   return (odd16<H>(w) ? 0u : w & 0xffffu) | (odd16<H>(w >> 16) ? 0u : w & 0xffff0000u);
 }
 
+// Four held values (pctree_held.h) times their scale, in 16 bits: exact, but for float16's
+// range.
+template <bool H>
+__device__ __forceinline__ u32x2 held4(uint32_t w, float scale) {
+  u32x2 r;
+  if constexpr (H) {
+    r[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, scale, false));
+    r[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, scale, true));
+  } else {
+    r[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, false));
+    r[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, true));
+  }
+  return r;
+}
+template <bool H>
+__device__ __forceinline__ u32x4 held8(uint32_t w0, uint32_t w1, float scale) {
+  const u32x2 a = held4<H>(w0, scale), b = held4<H>(w1, scale);
+  return u32x4{a[0], a[1], b[0], b[1]};
+}
+// Where the scale of a slot at offset `off` of a page lies.
+__device__ __forceinline__ size_t scale_place(const PagedAttnArgs& a, uint32_t page, int kvh,
+                                              int off) {
+  return page * (size_t)a.s.stride + ((size_t)kvh << (a.b.page_shift - a.s.block_shift)) +
+         (uint32_t)(off >> a.s.block_shift);
+}
+
 // Where the run of a request of few rows leaves row rho.
 __device__ __forceinline__ size_t few_part(const PagedAttnArgs& a, int split, int r, int kvh,
                                            int rho) {
@@ -252,7 +281,7 @@ __device__ __forceinline__ size_t few_part(const PagedAttnArgs& a, int split, in
 // Infinite and NaN values that were set to zero: they make the outputs of the rows
 // that do admit them NaN.  Rows ri[c] of a lane, their elements 16 t + d .. + 3 in
 // o[c][t]; slots [first, kend).  Rare, so slot by slot from memory.
-template <int D, bool H, int CT, int DT>
+template <int D, bool H, bool Q8, int CT, int DT>
 __device__ __forceinline__ void mend_odd(const PagedAttnArgs& a, const PagedReq& q, int r, int kvh,
                                          const int (&ri)[CT], int i_first, const uint32_t* mask,
                                          int first, int kend, int d, f32x4 (&o)[CT][DT]) {
@@ -262,8 +291,11 @@ __device__ __forceinline__ void mend_odd(const PagedAttnArgs& a, const PagedReq&
   for (int s = first; s < kend; ++s) {
     const int p = table[s >> a.b.page_shift], j = s - q.prefix;
     if ((unsigned)p >= (unsigned)a.b.pages) continue;
-    const uint16_t* vrow = a.v + ((size_t)p * a.b.page_units + (size_t)kvh * a.b.head_units) * 8 +
-                           (size_t)(s & pmask) * D + d;
+    const size_t head = (size_t)p * a.b.page_units + (size_t)kvh * a.b.head_units;
+    const uint16_t* vrow = a.v + head * 8 + (size_t)(s & pmask) * D + d;
+    const uint8_t* held = (const uint8_t*)a.v + head * 16 + (size_t)(s & pmask) * D + d;
+    float scale = 0.0f;
+    if constexpr (Q8) scale = scale_up(scale_in(a.s.v[scale_place(a, p, kvh, s & pmask)]));
     bool sees[CT];
 #pragma unroll
     for (int c = 0; c < CT; ++c)
@@ -271,7 +303,9 @@ __device__ __forceinline__ void mend_odd(const PagedAttnArgs& a, const PagedReq&
                                  : j <= ri[c]);
 #pragma unroll
     for (int t = 0; t < DT; ++t) {
-      const u32x2 w = *(const u32x2*)(vrow + 16 * t);
+      u32x2 w;
+      if constexpr (Q8) w = held4<H>(*(const uint32_t*)(held + 16 * t), scale);
+      else w = *(const u32x2*)(vrow + 16 * t);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const bool odd = odd16<H>(w[e / 2] >> (16 * (e & 1)));
@@ -287,7 +321,7 @@ __device__ __forceinline__ void mend_odd(const PagedAttnArgs& a, const PagedReq&
 // bound it, and the vector unit's softmax between them.  (2048 rows over 6000 slots, 32
 // and 8 heads of 128, 235 GFLOP: 228 to 238 us, 1.0 PFLOP/s, where a library product of
 // 8192 runs at 1.2.  32-slot chunks 290, 48 rows a wave 445, for 267 at the time: registers.)
-template <int D, bool H>
+template <int D, bool H, bool Q8>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) void paged_attn_kernel(
     PagedAttnArgs a) {
   constexpr int KS = D / 32, DT = D / 16, UPR = D / 8, CT = kColTiles;
@@ -398,11 +432,66 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
     }
     return bad;
   };
+  // Pages in 8 bits: a chunk goes through registers, loaded a chunk ahead and put into
+  // LDS in 16 bits, scaled, after the products of the one before.
+  constexpr int HU = D / 16, UPT = kChunk * HU / kThreads;  // 16-byte units of a row, of a thread
+  u32x4 kx[UPT], vx[UPT];
+  int ks[UPT], vs[UPT];
+  auto fetch_held = [&](int c0, int pg) __attribute__((always_inline)) -> uint64_t {
+    const bool none = (unsigned)pg >= (unsigned)a.b.pages;
+    const uint64_t bad = __ballot(none) & low_bits(kChunk);
+    const uint32_t pgc = none ? 0u : (uint32_t)pg;
+    const int last = kend - 1 - c0;
+#pragma unroll
+    for (int i = 0; i < UPT; ++i) {
+      const int row = min((i * kThreads + (int)threadIdx.x) / HU, last);
+      const uint32_t p = __builtin_amdgcn_ds_bpermute(row * 4, pgc);
+      const int off = (c0 + row) & pmask;
+      const size_t at = (size_t)p * a.b.page_units + head_base + (uint32_t)off * HU + threadIdx.x % HU;
+      const size_t sp = scale_place(a, p, wk.kvh, off);
+      kx[i] = ((const u32x4*)a.k)[at];
+      vx[i] = ((const u32x4*)a.v)[at];
+      ks[i] = a.s.k[sp];
+      vs[i] = a.s.v[sp];
+    }
+    return bad;
+  };
+  // (part: some row sees the chunk only in part, so infinite and NaN values become zeros)
+  auto stage = [&](int buf, bool part) __attribute__((always_inline)) {
+    bool odd = false;
+#pragma unroll
+    for (int i = 0; i < UPT; ++i) {
+      const int row = (i * kThreads + threadIdx.x) / HU, u = 2 * (threadIdx.x % HU);
+      const float kf = scale_up(scale_in(ks[i])), vf = scale_up(scale_in(vs[i]));
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        *(u32x4*)(&sKV[buf][0][row * D + ((u + b) ^ k_unit<D>(row)) * 8]) =
+            held8<H>(kx[i][2 * b], kx[i][2 * b + 1], kf);
+        u32x4 w = held8<H>(vx[i][2 * b], vx[i][2 * b + 1], vf);
+        if (part) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const uint32_t f = fine_pair<H>(w[e]);
+            odd |= f != w[e];
+            w[e] = f;
+          }
+        }
+        *(u32x4*)(&sKV[buf][1][row * D + ((u + b) ^ v_unit<D>(row)) * 8]) = w;
+      }
+    }
+    if (odd) sOdd = 1;
+  };
   int pg = page_of(kbeg);
-  uint64_t bad_next = fetch(kbeg, pg, 0);
+  uint64_t bad_next;
+  if constexpr (Q8) bad_next = fetch_held(kbeg, pg);
+  else bad_next = fetch(kbeg, pg, 0);
   pg = page_of(min(kbeg + kChunk, kend - 1));
 
   if (threadIdx.x == 0) sOdd = 0;
+  if constexpr (Q8) {
+    lds_barrier();
+    stage(0, bad_next || kbeg + kChunk > all_see);
+  }
   if (a.mask) {
     const uint32_t* mg = a.mask + ((size_t)wk.r * a.N + i_first) * a.NW;
     for (int i = threadIdx.x; i < (i_last - i_first + 1) * a.NW; i += kThreads) sMask[i] = mg[i];
@@ -481,14 +570,23 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
   // tiles' maxima, and the second half's weights computed beside the first half's
   // product.
   const int whole = a.b.page_shift >= 3 ? all_see : kbeg;
+  auto stage_next = [&]() __attribute__((always_inline)) {
+    if constexpr (Q8) {
+      if (c0 + kChunk < kend) stage(buf ^ 1, bad_next || c0 + 2 * kChunk > all_see);
+    }
+  };
   for (; c0 + kChunk <= whole && !bad_next; c0 += kChunk, buf ^= 1) {
-    wait_loads();
+    if constexpr (!Q8) wait_loads();
     lds_barrier();  // the chunk is complete; the other buffer is no longer read
     if (c0 + kChunk < kend) {
-      bad_next = fetch_scalar(c0 + kChunk, pg, buf ^ 1);
+      if constexpr (Q8) bad_next = fetch_held(c0 + kChunk, pg);
+      else bad_next = fetch_scalar(c0 + kChunk, pg, buf ^ 1);
       pg = page_of(min(c0 + 2 * kChunk, kend - 1));
     }
-    if (!w_live) continue;
+    if (!w_live) {
+      stage_next();
+      continue;
+    }
     f32x4 sacc[CT][kHalves][2];
     scores(sKV[buf][0], sacc);
     float mx[CT];
@@ -534,21 +632,23 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
       }
 #pragma unroll
     for (int h = 0; h < kHalves; ++h) weigh(sKV[buf][1], h, bp[h]);
+    stage_next();
   }
   for (; c0 < kend; c0 += kChunk, buf ^= 1) {
-    wait_loads();
+    if constexpr (!Q8) wait_loads();
     lds_barrier();  // the chunk is complete; the other buffer is no longer read
     const uint64_t bad = bad_next;
     some_bad |= bad != 0;
     if (c0 + kChunk < kend) {
-      bad_next = fetch(c0 + kChunk, pg, buf ^ 1);
+      if constexpr (Q8) bad_next = fetch_held(c0 + kChunk, pg);
+      else bad_next = fetch(c0 + kChunk, pg, buf ^ 1);
       pg = page_of(min(c0 + 2 * kChunk, kend - 1));
     }
     uint16_t* sK = sKV[buf][0];
     uint16_t* sV = sKV[buf][1];
     // Chunks that some row of the block sees only in part (the same in every
     // wave): infinite and NaN values, and those of no page, become zeros.
-    if (bad || c0 + kChunk > all_see) {
+    if (!Q8 && (bad || c0 + kChunk > all_see)) {
       bool odd = false;
 #pragma unroll
       for (int i = 0; i < IPW; ++i) {
@@ -568,7 +668,10 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
       if (odd) sOdd = 1;
       lds_barrier();
     }
-    if (!w_live || c0 >= w_end) continue;  // (causal) no row of this wave sees the chunk
+    if (!w_live || c0 >= w_end) {  // (causal) no row of this wave sees the chunk
+      stage_next();
+      continue;
+    }
     // every row of the wave admits every slot
     const bool full = !bad && c0 + kChunk <= min(kend, q.prefix + (a.mask ? 0 : w_first + 1));
 
@@ -591,11 +694,13 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
     }
 #pragma unroll
     for (int h = 0; h < kHalves; ++h) weigh(sV, h, bp[h]);
+    stage_next();
   }
-  // (every wave is past the loop's last barrier)
+  // (every wave is past the loop's last barrier, and the last chunk's values were looked
+  // at before it)
   if (sOdd) {
     const int first = some_bad ? kbeg : kbeg + max(all_see - kbeg, 0) / kChunk * kChunk;
-    mend_odd<D, H, CT, DT>(a, q, wk.r, wk.kvh, ri, i_first, sMask, first, kend, 4 * grp, o);
+    mend_odd<D, H, Q8, CT, DT>(a, q, wk.r, wk.kvh, ri, i_first, sMask, first, kend, 4 * grp, o);
   }
 
 #pragma unroll
@@ -626,6 +731,69 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
   }
 }
 
+// The results of a workgroup's waves, each in its own tile's place, joined.
+template <int D, bool H, bool Q8, typename Tile>
+__device__ __forceinline__ void few_join(const PagedAttnArgs& a, const Work& wk, Tile (&tiles)[kWaves],
+                                         float2 (&sML)[kWaves][16], const int& sOdd,
+                                         const uint32_t* mask, const f32x4 (&o)[D / 16], float m,
+                                         float l, int kbeg, int kend, bool direct) {
+  constexpr int DT = D / 16, PART = DT * 64;  // f32x4 of a wave's output
+  static_assert(sizeof(Tile) >= PART * sizeof(f32x4), "an output fits a tile");
+  const PagedReq& q = wk.q;
+  const int rows = q.cnt * a.g, rho0 = wk.qb * 16;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x & 63;
+  const int col = lane & 15, grp = lane >> 4;
+  const int rho = min(rho0 + col, rows - 1), i_first = rho0 / a.g;
+  const int ri = rho / a.g, hq = wk.kvh * a.g + rho % a.g;
+  if (grp == 0) sML[wave][col] = make_float2(m, l);
+  f32x4* sO = (f32x4*)tiles[wave];
+#pragma unroll
+  for (int t = 0; t < DT; ++t) sO[t * 64 + lane] = o[t];
+  lds_barrier();
+  const bool odd = sOdd != 0;
+  for (int e = threadIdx.x; e < PART; e += kThreads) {  // (e % 64 == lane)
+    if (rho0 + col >= rows) break;
+    const int t = e / 64;
+    float M = kNegInf;
+    float2 ml[kWaves];
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      ml[w] = sML[w][col];
+      M = fmaxf(M, ml[w].x);
+    }
+    float L = 0.0f;
+    f32x4 O = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      // (equal maxima, -inf among them: factor 1)
+      const float wt = ml[w].x == M ? 1.0f : exp2_hw((ml[w].x - M) * a.scale_log2);
+      L += wt * ml[w].y;
+      O += ((const f32x4*)tiles[w])[e] * wt;
+    }
+    const int d = t * 16 + 4 * grp;
+    if (odd) {
+      const int rows1[1] = {ri};
+      f32x4 one[1][1] = {{O}};
+      mend_odd<D, H, Q8, 1, 1>(a, q, wk.r, wk.kvh, rows1, i_first, mask, kbeg, kend, d, one);
+      O = one[0][0];
+    }
+    if (direct) {
+      const float inv = L == 0.0f ? 0.0f : 1.0f / L;
+      u32x2 wv;
+      wv[0] = pack16<H>(O[0] * inv, O[1] * inv);
+      wv[1] = pack16<H>(O[2] * inv, O[3] * inv);
+      *(u32x2*)(a.out + ((size_t)(q.start + ri) * a.Hq + hq) * D + d) = wv;
+    } else {
+      const size_t prow = few_part(a, wk.split, wk.r, wk.kvh, rho);
+      *(f32x4*)(a.few_o + prow * D + d) = O;
+      if (d == 0) {
+        a.few_ml[2 * prow] = M;
+        a.few_ml[2 * prow + 1] = L;
+      }
+    }
+  }
+}
+
 // Requests of few rows: 16 of one (request, kv head) to a workgroup.  Bytes bound it: 64
 // single tokens over 500 to 8000 slots, 711 MB, 142 us with the merge's 5, 5.0 TB/s; one
 // token over 1000 slots is two launches' latency, 7.7 and 3.7 us.
@@ -634,12 +802,10 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3))) v
     PagedAttnArgs a) {
   constexpr int KS = D / 32, DT = D / 16, UPR = D / 8;
   constexpr int INS = kFewChunk * UPR / 64;  // load instructions of a chunk's V
-  constexpr int PART = DT * 64;              // f32x4 of a wave's output
   __shared__ __attribute__((aligned(16))) uint16_t sV[kWaves][kFewChunk * D];
   __shared__ float2 sML[kWaves][16];
   __shared__ int sOdd;
   extern __shared__ uint32_t sMask[];
-  static_assert(sizeof(uint16_t) * kFewChunk * D >= PART * sizeof(f32x4), "an output fits a tile");
 
   const Work wk = work_of(a, a.few_qblocks, a.few_nsplit, 16, true);
   if (!wk.ok) return;
@@ -649,7 +815,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3))) v
   const int col = lane & 15, grp = lane >> 4;
   const int i_first = rho0 / a.g, i_last = (min(rho0 + 16, rows) - 1) / a.g;
   const int end = min(q.prefix + q.cnt, a.b.C);
-  const int run = run_slots(end, a.few_nsplit, kFewRun);
+  const int run = run_slots(end, a.few_nsplit, a.few_least);
   const bool direct = run >= end;
   const int kbeg = wk.split * run, kend = min(kbeg + run, row_end(a, q, i_last));
   if (kbeg >= kend) return;
@@ -755,56 +921,159 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3))) v
     __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
     __atomic_signal_fence(__ATOMIC_SEQ_CST);
   }
-  // the waves' results, each in its own tile's place
-  if (grp == 0) sML[wave][col] = make_float2(m, l[0]);
-  f32x4* sO = (f32x4*)sV[wave];
-#pragma unroll
-  for (int t = 0; t < DT; ++t) sO[t * 64 + lane] = o[t];
-  lds_barrier();
-  const bool odd = sOdd != 0;
-  for (int e = threadIdx.x; e < PART; e += kThreads) {  // (e % 64 == lane)
-    if (rho0 + col >= rows) break;
-    const int t = e / 64;
-    float M = kNegInf;
-    float2 ml[kWaves];
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-      ml[w] = sML[w][col];
-      M = fmaxf(M, ml[w].x);
-    }
-    float L = 0.0f;
-    f32x4 O = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-      // (equal maxima, -inf among them: factor 1)
-      const float wt = ml[w].x == M ? 1.0f : exp2_hw((ml[w].x - M) * a.scale_log2);
-      L += wt * ml[w].y;
-      O += ((const f32x4*)sV[w])[e] * wt;
-    }
-    const int d = t * 16 + 4 * grp;
-    if (odd) {
-      const int rows1[1] = {ri};
-      f32x4 one[1][1] = {{O}};
-      mend_odd<D, H, 1, 1>(a, q, wk.r, wk.kvh, rows1, i_first, sMask, kbeg, kend, d, one);
-      O = one[0][0];
-    }
-    if (direct) {
-      const float inv = L == 0.0f ? 0.0f : 1.0f / L;
-      u32x2 wv;
-      wv[0] = pack16<H>(O[0] * inv, O[1] * inv);
-      wv[1] = pack16<H>(O[2] * inv, O[3] * inv);
-      *(u32x2*)(a.out + ((size_t)(q.start + ri) * a.Hq + hq) * D + d) = wv;
-    } else {
-      const size_t prow = few_part(a, wk.split, wk.r, wk.kvh, rho);
-      *(f32x4*)(a.few_o + prow * D + d) = O;
-      if (d == 0) {
-        a.few_ml[2 * prow] = M;
-        a.few_ml[2 * prow + 1] = L;
-      }
-    }
-  }
+  few_join<D, H, false>(a, wk, sV, sML, sOdd, sMask, o, m, l[0], kbeg, kend, direct);
 }
 
+// The same over pages in 8 bits: a wave's step is 64 slots, as many bytes.  A lane takes
+// 16 of a key's bytes at a time, two steps of the first product, and the queries lie in
+// that order; values cross LDS in 8 bits, and a transposing read gives a lane 8 slots of
+// one element, whose scale is one (a block holds 8 slots at least).
+template <int D, bool H>
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3))) void paged_few8_kernel(
+    PagedAttnArgs a) {
+  constexpr int DT = D / 16, HU = D / 16, KU = HU / 4;  // 16-byte units of a row, of a lane's keys
+  constexpr int INS = kFewChunk8 * HU / 64;             // load instructions of a chunk's V
+  constexpr int BANKS = 16 / HU;                        // rows of 256 bytes
+  __shared__ __attribute__((aligned(16))) uint8_t sV[kWaves][kFewChunk8 * D];
+  __shared__ float2 sML[kWaves][16];
+  __shared__ int sOdd;
+  extern __shared__ uint32_t sMask[];
+
+  const Work wk = work_of(a, a.few_qblocks, a.few_nsplit, 16, true);
+  if (!wk.ok) return;
+  const PagedReq q = wk.q;
+  const int rows = q.cnt * a.g, rho0 = wk.qb * 16;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x & 63;
+  const int col = lane & 15, grp = lane >> 4;
+  const int i_first = rho0 / a.g, i_last = (min(rho0 + 16, rows) - 1) / a.g;
+  const int end = min(q.prefix + q.cnt, a.b.C);
+  const int run = run_slots(end, a.few_nsplit, a.few_least);
+  const bool direct = run >= end;
+  const int kbeg = wk.split * run, kend = min(kbeg + run, row_end(a, q, i_last));
+  if (kbeg >= kend) return;
+  const int all_see = min(kend, q.prefix + (a.mask ? 0 : i_first + 1));
+  const int* table = a.b.page_table + (size_t)wk.r * a.b.max_pages;
+  const int pmask = (1 << a.b.page_shift) - 1;
+  auto page_of = [&](int c0) __attribute__((always_inline)) {
+    return table[min(c0 + lane, kend - 1) >> a.b.page_shift];
+  };
+  const int c_first = kbeg + wave * kFewChunk8;
+  int pg = page_of(min(c_first, kend - 1));
+
+  const int rho = min(rho0 + col, rows - 1);
+  const int ri = rho / a.g, hq = wk.kvh * a.g + rho % a.g;
+  u32x4 bq[2 * KU];
+  {
+    const uint16_t* qrow = a.q + ((size_t)(q.start + ri) * a.Hq + hq) * D + grp * 16;
+#pragma unroll
+    for (int u = 0; u < KU; ++u) {
+      bq[2 * u] = *(const u32x4*)(qrow + u * 64);
+      bq[2 * u + 1] = *(const u32x4*)(qrow + u * 64 + 8);
+    }
+  }
+  if (threadIdx.x == 0) sOdd = 0;
+  if (a.mask) {
+    const uint32_t* mg = a.mask + ((size_t)wk.r * a.N + i_first) * a.NW;
+    for (int i = threadIdx.x; i < (i_last - i_first + 1) * a.NW; i += kThreads) sMask[i] = mg[i];
+  }
+  lds_barrier();
+  const uint32_t* mw = sMask + (ri - i_first) * a.NW;
+
+  f32x4 o[DT], l = {0.f, 0.f, 0.f, 0.f};
+  float m = kNegInf;
+#pragma unroll
+  for (int t = 0; t < DT; ++t) o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const int krow0 = 8 * (col >> 2) + (col & 3);
+  const int vkey = 8 * grp + (col >> 1);  // the slot whose values this lane addresses
+  constexpr uint32_t one = H ? 0x3c003c00u : 0x3f803f80u;
+  const u32x4 ones = {one, one, one, one};
+  for (int c0 = c_first; c0 < kend; c0 += kWaves * kFewChunk8) {
+    const bool none = (unsigned)pg >= (unsigned)a.b.pages;
+    const uint64_t bad = __ballot(none);
+    const uint32_t pgc = none ? 0u : (uint32_t)pg;
+    const int last = kend - 1 - c0;  // (slots past the run repeat its last one)
+    auto at = [&](int row) __attribute__((always_inline)) {  // 16-byte units before the row
+      row = min(row, last);
+      const uint32_t p = __builtin_amdgcn_ds_bpermute(row * 4, pgc);
+      return (size_t)p * a.b.page_units + (size_t)wk.kvh * a.b.head_units +
+             (uint32_t)((c0 + row) & pmask) * HU;
+    };
+    // Values, their rows' units permuted so that 16 rows' reads of one unit meet all banks.
+#pragma unroll
+    for (int i = 0; i < INS; ++i) {
+      const int u = i * 64 + lane, row = u / HU, pos = u % HU;
+      load_lds16((const uint4*)a.v + at(row) + (pos ^ (row / BANKS % HU)), &sV[wave][i * 1024]);
+    }
+    u32x4 kx[2][2][KU];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const u32x4* kr = (const u32x4*)a.k + at(32 * h + krow0 + 4 * t) + grp;
+#pragma unroll
+        for (int u = 0; u < KU; ++u) kx[h][t][u] = kr[4 * u];
+      }
+    // the scales of the chunk's groups of eight slots: keys in lanes 0 to 7, values in 8 to 15
+    const int srow = min(8 * (lane & 7), last);
+    const size_t sp = scale_place(a, __builtin_amdgcn_ds_bpermute(srow * 4, pgc), wk.kvh,
+                                  (c0 + srow) & pmask);
+    const int sbyte = scale_in((lane & 8 ? a.s.v : a.s.k)[sp]);
+    pg = page_of(min(c0 + kWaves * kFewChunk8, kend - 1));
+    f32x4 sacc[2][2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const float kf = scale_up(__builtin_amdgcn_ds_bpermute((4 * h + (col >> 2)) * 4, sbyte));
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        sacc[h][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int u = 0; u < KU; ++u) {
+          const u32x4 w = kx[h][t][u];
+          sacc[h][t] = mfma16<H>(held8<H>(w[0], w[1], kf), bq[2 * u], sacc[h][t]);
+          sacc[h][t] = mfma16<H>(held8<H>(w[2], w[3], kf), bq[2 * u + 1], sacc[h][t]);
+        }
+      }
+    }
+    const bool full = !bad && c0 + kFewChunk8 <= all_see;
+    const uint32_t adm = full ? 0u : admitted(a, q, mw, ri, c0, kend, bad, grp);
+    u32x4 bp[2];
+    const float alpha = softmax_chunk<H, 2>(sacc, adm, full, a.scale_log2, m, bp);
+    if (__any(alpha != 1.0f)) {
+      l *= alpha;
+#pragma unroll
+      for (int t = 0; t < DT; ++t) o[t] *= alpha;
+    }
+    l = mfma16<H>(ones, bp[0], l);
+    l = mfma16<H>(ones, bp[1], l);
+    wait_loads();
+    bool odd = false;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const float vf = scale_up(__builtin_amdgcn_ds_bpermute((8 + 4 * h + grp) * 4, sbyte));
+      const int key = 32 * h + vkey;
+#pragma unroll
+      for (int t = 0; t < DT; ++t) {
+        const u32x2 w = read_tr8(sV[wave] + key * D + (t ^ (key / BANKS % HU)) * 16 + (col & 1) * 8);
+        u32x4 v = held8<H>(w[0], w[1], vf);
+        if (!full) {  // infinite and NaN values become zeros
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const uint32_t f = fine_pair<H>(v[e]);
+            odd |= f != v[e];
+            v[e] = f;
+          }
+        }
+        o[t] = mfma16<H>(v, bp[h], o[t]);
+      }
+    }
+    if (odd) sOdd = 1;
+    // (the tile's reads are back before the next chunk's loads overwrite it)
+    __atomic_signal_fence(__ATOMIC_SEQ_CST);
+    __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
+    __atomic_signal_fence(__ATOMIC_SEQ_CST);
+  }
+  few_join<D, H, true>(a, wk, sV, sML, sOdd, sMask, o, m, l[0], kbeg, kend, direct);
+}
 // Merge of the runs: a wave takes 256 / D heads of one row, D / 4 threads each,
 // 4 consecutive elements apiece.  Requests of one run are already written.
 template <int D, bool H>
@@ -823,7 +1092,7 @@ __global__ __launch_bounds__(kMergeThreads) void paged_merge_kernel(PagedAttnArg
   if (i >= q.cnt || h >= a.Hq) return;
   const int end = min(q.prefix + q.cnt, a.b.C);
   const bool few = few_rows(a, q.cnt);
-  const int run = few ? run_slots(end, a.few_nsplit, kFewRun) : run_slots(end, a.nsplit, a.least);
+  const int run = few ? run_slots(end, a.few_nsplit, a.few_least) : run_slots(end, a.nsplit, a.least);
   if (run >= end) return;
   const int ns = (row_end(a, q, i) + run - 1) / run;
   const size_t qidx = (size_t)t * a.Hq + h;
@@ -877,12 +1146,17 @@ unsigned mask_bytes(const PagedAttnArgs& a, int rows) {
 }
 
 template <int D, bool H>
-hipError_t launch(const PagedAttnArgs& a, const PagedPlan& p, hipStream_t stream) {
-  if (p.blocks)
-    paged_attn_kernel<D, H>
-        <<<(unsigned)p.blocks, kThreads, mask_bytes(a, kRowsPerBlock), stream>>>(a);
-  if (p.few_blocks)
-    paged_few_kernel<D, H><<<(unsigned)p.few_blocks, kThreads, mask_bytes(a, 16), stream>>>(a);
+hipError_t launch(const PagedAttnArgs& a, const PagedPlan& p, bool held, hipStream_t stream) {
+  if (p.blocks) {
+    const unsigned blocks = (unsigned)p.blocks, lds = mask_bytes(a, kRowsPerBlock);
+    if (held) paged_attn_kernel<D, H, true><<<blocks, kThreads, lds, stream>>>(a);
+    else paged_attn_kernel<D, H, false><<<blocks, kThreads, lds, stream>>>(a);
+  }
+  if (p.few_blocks) {
+    const unsigned blocks = (unsigned)p.few_blocks, lds = mask_bytes(a, 16);
+    if (held) paged_few8_kernel<D, H><<<blocks, kThreads, lds, stream>>>(a);
+    else paged_few_kernel<D, H><<<blocks, kThreads, lds, stream>>>(a);
+  }
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || (p.nsplit == 1 && p.few_nsplit == 1)) return e;
   constexpr int HPW = 256 / D;
@@ -893,9 +1167,10 @@ hipError_t launch(const PagedAttnArgs& a, const PagedPlan& p, hipStream_t stream
 
 }  // namespace
 
-PagedPlan plan_paged_attention(int R, int T, int max_rows, int Hq, int Hkv, int D, int C,
+PagedPlan plan_paged_attention(int R, int T, int max_rows, int Hq, int Hkv, int D, int C, bool held,
                                int cus) {
   PagedPlan p;
+  p.few_least = held ? kFewRun8 : kFewRun;
   const int g = Hq / Hkv;
   const long long most = (long long)max_rows * g;  // rows of a request
   // Which kernels: requests of few rows have their own, unless none can have few (one
@@ -915,7 +1190,7 @@ PagedPlan plan_paged_attention(int R, int T, int max_rows, int Hq, int Hkv, int 
   // reads in two steps (us at 32, 16, 12, 8 runs at most: 8 single tokens of 500 to 4000
   // slots 31, 25, 25, 23; 40 of one kv head and up to 8000 slots 30, 22, 25, 27; 64 tokens
   // of eight heads have 3 runs each, 150, and 165 with 2).
-  p.few_nsplit = p.few ? std::min(runs(pairs * p.few_qblocks, 6 * cus, kFewRun), 12) : 1;
+  p.few_nsplit = p.few ? std::min(runs(pairs * p.few_qblocks, 6 * cus, p.few_least), 12) : 1;
   // workgroups for n row blocks of every (kv head, run) (work_of)
   const auto blocks = [&](long long n, int nsplit) {
     const long long pairs = (long long)Hkv * nsplit;
@@ -950,7 +1225,7 @@ PagedPlan plan_paged_attention(int R, int T, int max_rows, int Hq, int Hkv, int 
   return p;
 }
 
-hipError_t launch_paged_attention(PagedAttnArgs a, const PagedPlan& p, int D, bool f16,
+hipError_t launch_paged_attention(PagedAttnArgs a, const PagedPlan& p, int D, bool f16, bool held,
                                   void* workspace, hipStream_t stream) {
   a.qblocks = p.qblocks;
   a.nsplit = p.nsplit;
@@ -958,13 +1233,15 @@ hipError_t launch_paged_attention(PagedAttnArgs a, const PagedPlan& p, int D, bo
   a.few = p.few;
   a.few_qblocks = p.few_qblocks;
   a.few_nsplit = p.few_nsplit;
+  a.few_least = p.few_least;
   a.few_stride = p.few_stride;
   a.part_o = (float*)workspace;
   a.few_o = a.part_o + p.parts * D;
   a.part_ml = a.few_o + p.few_parts * D;
   a.few_ml = a.part_ml + p.parts * 2;
-  if (D == 128) return f16 ? launch<128, true>(a, p, stream) : launch<128, false>(a, p, stream);
-  return f16 ? launch<64, true>(a, p, stream) : launch<64, false>(a, p, stream);
+  if (D == 128)
+    return f16 ? launch<128, true>(a, p, held, stream) : launch<128, false>(a, p, held, stream);
+  return f16 ? launch<64, true>(a, p, held, stream) : launch<64, false>(a, p, held, stream);
 }
 
 }  // namespace pctree

@@ -104,6 +104,14 @@ __device__ __forceinline__ u32x2 read_tr(const uint16_t* src) {
       (__attribute__((address_space(3))) s16x4*)src));
 }
 
+// The same for bytes: in each 16 lanes, lanes 2 i and 2 i + 1 address row i (16
+// consecutive bytes, 8 each), and lane l receives column l of rows 0 .. 7.
+typedef int i32x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ u32x2 read_tr8(const uint8_t* src) {
+  return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32(
+      (__attribute__((address_space(3))) i32x2*)src));
+}
+
 // Low `n` bits set, n in [0, 64].
 __device__ __forceinline__ uint64_t low_bits(int n) {
   return n >= 64 ? ~0ull : ((1ull << n) - 1ull);

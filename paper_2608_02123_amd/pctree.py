@@ -37,6 +37,8 @@ __all__ = [
     "compact_paged",
     "Sampler",
     "sample",
+    "rms_norm",
+    "adjust_logits",
     "TreeBuilder",
     "timeline_available",
     "timeline_read",
@@ -109,6 +111,31 @@ class _Append(ctypes.Structure):
                [(n, ctypes.c_void_p) for n in ("q_norm", "k_norm", "rope", "position")] + \
                [("eps", ctypes.c_float)] + \
                [(n, ctypes.c_int32) for n in ("q_heads", "rot_dim", "positions", "interleaved")]
+
+
+class _PagedCache8(ctypes.Structure):
+    _fields_ = [("pages", _PagedCache), ("k_scale", ctypes.c_void_p),
+                ("v_scale", ctypes.c_void_p), ("scale_stride", ctypes.c_int64),
+                ("block", ctypes.c_int32)]
+
+
+class _Norm(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("x", "weight", "residual", "out", "scale")] + \
+               [(n, ctypes.c_int64) for n in ("x_stride", "residual_stride", "out_stride")] + \
+               [(n, ctypes.c_int32) for n in ("rows", "width", "group", "dtype")] + \
+               [("eps", ctypes.c_float)]
+
+
+class _Adjust(ctypes.Structure):
+    _fields_ = [("logits", ctypes.c_void_p), ("row_stride", ctypes.c_int64)] + \
+               [(n, ctypes.c_void_p) for n in
+                ("row_start", "row_count", "history", "history_start", "history_count",
+                 "prompt_count", "repetition", "frequency", "presence", "bias_token",
+                 "bias_value", "bias_start", "bias_count", "token", "mask", "allowed",
+                 "allowed_row")] + \
+               [(n, ctypes.c_int32) for n in
+                ("rows", "vocab", "requests", "max_rows", "history_total", "bias_total", "budget",
+                 "masks", "dtype")]
 
 
 class _Inputs(ctypes.Structure):
@@ -185,6 +212,20 @@ def lib() -> ctypes.CDLL:
         L.pctree_compact_paged.argtypes = [vp, i64, i64, i32, i32, i32, i32, i32, vp, i32, vp, vp,
                                            vp, i32, i32, i32, vp]
         L.pctree_compact_paged.restype = ctypes.c_int
+        cache8 = ctypes.POINTER(_PagedCache8)
+        L.pctree_append_paged8.argtypes = [cache8, batch, ctypes.POINTER(_Append), vp]
+        L.pctree_append_paged8.restype = ctypes.c_int
+        L.pctree_paged_attention8_workspace_bytes.argtypes = [cache8, batch, i32]
+        L.pctree_paged_attention8_workspace_bytes.restype = sz
+        L.pctree_paged_attention8.argtypes = [cache8, *L.pctree_paged_attention.argtypes[1:]]
+        L.pctree_paged_attention8.restype = ctypes.c_int
+        L.pctree_compact_paged8.argtypes = [vp, i64, i64, vp, i64, i64] + [i32] * 6 + \
+            [vp, i32, vp, vp, vp, i32, i32, i32, vp]
+        L.pctree_compact_paged8.restype = ctypes.c_int
+        L.pctree_rms_norm.argtypes = [ctypes.POINTER(_Norm), vp]
+        L.pctree_rms_norm.restype = ctypes.c_int
+        L.pctree_adjust_logits.argtypes = [ctypes.POINTER(_Adjust), vp]
+        L.pctree_adjust_logits.restype = ctypes.c_int
         L.pctree_status_string.argtypes = [ctypes.c_int]
         L.pctree_status_string.restype = ctypes.c_char_p
         L.pctree_abi_version.argtypes = []
@@ -666,12 +707,18 @@ class PagedBatch:
         self._ref = ctypes.byref(self._c)
 
 
-def _paged_cache(k, v, idx):
+_HELD, _SCALE = torch.float8_e4m3fn, torch.float8_e8m0fnu
+
+
+def _paged_cache(k, v, idx, rows=None):
     """The C view of one layer's pages [pages][Hkv][page_size][D]; the pages may lie
-    apart (stride 0 is free, the same for both)."""
+    apart (stride 0 is free, the same for both).  ``rows``: the new rows' type, where
+    the pages are held in 8 bits."""
+    types = _HALVES if rows is None else {_HELD: _HALVES.get(rows)}
     for name, t in (("k_cache", k), ("v_cache", v)):
-        if not isinstance(t, torch.Tensor) or t.dtype not in _HALVES:
-            raise TypeError(f"{name} must be a bfloat16 or float16 tensor")
+        if not isinstance(t, torch.Tensor) or t.dtype not in types:
+            raise TypeError(f"{name} must be a bfloat16 or float16 tensor" if rows is None else
+                            f"{name} must be a float8_e4m3fn tensor")
         if t.dim() != 4 or t.get_device() != idx or idx < 0:
             raise ValueError(f"{name} must be a [pages][Hkv][page_size][D] tensor on the batch's "
                              "device")
@@ -684,7 +731,32 @@ def _paged_cache(k, v, idx):
             (vs[1:] != inner and not v[0].is_contiguous()):
         raise ValueError("a page's [Hkv][page_size][D] must be contiguous")
     return _PagedCache(k.data_ptr(), v.data_ptr(), ks[0] if pages > 1 else Hkv * P * D, pages, P,
-                       Hkv, D, _HALVES[k.dtype])
+                       Hkv, D, types[k.dtype])
+
+
+def _held_cache(k, v, k_scale, v_scale, rows, idx):
+    """The C view of one layer's pages in 8 bits, with their scales [pages][Hkv][page_size /
+    block]; ``rows``: the type of the new rows."""
+    if rows not in _HALVES:
+        raise TypeError("the rows must be bfloat16 or float16 tensors")
+    for name, t in (("k_scale", k_scale), ("v_scale", v_scale)):
+        if not isinstance(t, torch.Tensor) or t.dtype is not _SCALE:
+            raise TypeError(f"{name} must be a float8_e8m0fnu tensor beside pages in 8 bits")
+    c = _paged_cache(k, v, idx, rows)
+    for name, t in (("k_scale", k_scale), ("v_scale", v_scale)):
+        if t.dim() != 3 or t.get_device() != idx or t.shape[:2] != k.shape[:2]:
+            raise ValueError(f"{name} must be a [pages][Hkv][page_size / block] tensor on the "
+                             "batch's device")
+    pages, Hkv, n = k_scale.shape
+    ks, vs = k_scale.stride(), v_scale.stride()
+    if k_scale.shape != v_scale.shape or (pages > 1 and ks[0] != vs[0]):
+        raise ValueError("k_scale and v_scale must have one shape and page stride")
+    if n < 1 or c.page_size % n:
+        raise ValueError(f"{n} scales do not divide a page of {c.page_size} slots")
+    if not k_scale[0].is_contiguous() or not v_scale[0].is_contiguous():
+        raise ValueError("a page's scales must be contiguous")
+    return _PagedCache8(c, k_scale.data_ptr(), v_scale.data_ptr(), ks[0] if pages > 1 else Hkv * n,
+                        c.page_size // n)
 
 
 def _row_tensor(name, t, T, D, dtype, idx):
@@ -715,16 +787,28 @@ def rope_table(positions, rot_dim, theta=10000.0, device="cuda"):
 
 
 def append_paged(batch, k_cache, v_cache, k, v, q=None, *, q_norm=None, k_norm=None, eps=1e-6,
-                 rope=None, interleaved=False, position=None, q_out=None, stream=None):
+                 rope=None, interleaved=False, position=None, q_out=None, k_scale=None,
+                 v_scale=None, stream=None):
     """New rows into their pages: ``k``, ``v [T][Hkv][D]`` and, if given, ``q [T][Hq][D]``
     (views of a fused projection will do) are normed per head (``q_norm``, ``k_norm
     [D]``: root mean square), rotated by ``rope`` (:func:`rope_table`) at ``position
     [T]`` (a row's slot if not given); keys and values go to the rows' slots.
     Returns the normed and rotated q in ``q_out`` (a new tensor if not given; rows
-    of no request are not written)."""
+    of no request are not written).
+
+    Pages of float8_e4m3fn are held in 8 bits, with scales ``k_scale, v_scale
+    [pages][Hkv][page_size / block]`` float8_e8m0fnu, a block being 8, 16, 32 or 64 slots
+    (include/pctree.h)."""
     idx, T = batch.idx, batch.rows
-    c = _paged_cache(k_cache, v_cache, idx)
-    dt, D = k_cache.dtype, c.head_dim
+    held = k_scale is not None or v_scale is not None
+    if held:
+        dt = getattr(k, "dtype", None)
+        whole = _held_cache(k_cache, v_cache, k_scale, v_scale, dt, idx)
+        c, call, name = whole.pages, lib().pctree_append_paged8, "pctree_append_paged8"
+    else:
+        c = whole = _paged_cache(k_cache, v_cache, idx)
+        dt, call, name = k_cache.dtype, lib().pctree_append_paged, "pctree_append_paged"
+    D = c.head_dim
     ks, kh = _row_tensor("k", k, T, D, dt, idx)
     vs, vh = _row_tensor("v", v, T, D, dt, idx)
     if kh != c.kv_heads or vh != kh:
@@ -755,14 +839,15 @@ def append_paged(batch, k_cache, v_cache, k, v, q=None, *, q_norm=None, k_norm=N
         a = _Append(_ptr(q), k.data_ptr(), v.data_ptr(), _ptr(q_out), qs, ks, vs, os_,
                     _ptr(q_norm), _ptr(k_norm), _ptr(rope), _ptr(position), eps, Hq, rot, npos,
                     1 if interleaved else 0)
-        status = lib().pctree_append_paged(ctypes.byref(c), batch._ref, ctypes.byref(a), st)
-    _check(status, "pctree_append_paged")
+        status = call(ctypes.byref(whole), batch._ref, ctypes.byref(a), st)
+    _check(status, name)
     return q_out
 
 
 class PagedAttention:
     """Attention of a batch's new rows over paged caches, with its workspace, for
-    repeated calls of one size (calls that may overlap need an object each)."""
+    repeated calls of one size (calls that may overlap need an object each).  Pages in 8
+    bits need less of it than those in 16: one object serves both."""
 
     def __init__(self, batch, q_heads, kv_heads, head_dim, page_size, scale=None):
         self.sizes = batch.sizes
@@ -777,19 +862,27 @@ class PagedAttention:
         self._ws = _Workspace(self.ws_bytes, batch.device)
         self.workspace = self._ws.tensor
 
-    def __call__(self, q, k_cache, v_cache, batch, mask=None, out=None, stream=None):
+    def __call__(self, q, k_cache, v_cache, batch, mask=None, out=None, *, k_scale=None,
+                 v_scale=None, stream=None):
         """``q [T][Hq][D]`` over ``k_cache, v_cache [pages][Hkv][page_size][D]``; causal, or
         with ``mask`` (:func:`build_mask`) the tree's.  Returns ``out [T][Hq][D]``
-        (rows of no request are not written)."""
+        (rows of no request are not written).  Pages in 8 bits come with their
+        scales, as in :func:`append_paged`."""
         idx = self.idx
         if batch.sizes != self.sizes or batch.idx != idx:
             raise ValueError("the batch is not of this object's sizes")
-        c = _paged_cache(k_cache, v_cache, idx)
+        if k_scale is not None or v_scale is not None:
+            dt = getattr(q, "dtype", None)
+            whole = _held_cache(k_cache, v_cache, k_scale, v_scale, dt, idx)
+            c, call, name = whole.pages, lib().pctree_paged_attention8, "pctree_paged_attention8"
+        else:
+            c = whole = _paged_cache(k_cache, v_cache, idx)
+            dt, call, name = k_cache.dtype, lib().pctree_paged_attention, "pctree_paged_attention"
         if c.kv_heads != self.kv_heads or c.head_dim != self.head_dim or \
                 c.page_size != self.page_size:
             raise ValueError("the pages are not of this object's sizes")
         shp = (batch.rows, self.q_heads, self.head_dim)
-        _device_tensor("q", q, k_cache.dtype, shp, idx)
+        _device_tensor("q", q, dt, shp, idx)
         budget = 0
         if mask is not None:
             if mask.dtype != torch.int32 and mask.dtype != torch.uint32:
@@ -798,31 +891,36 @@ class PagedAttention:
             _device_tensor("mask", mask, mask.dtype,
                            (batch.requests, budget, (budget + 31) // 32), idx)
         if out is not None:
-            _device_tensor("out", out, k_cache.dtype, shp, idx)
+            _device_tensor("out", out, dt, shp, idx)
         with _Here(idx, stream) as st:
             if out is None:
                 out = torch.empty(shp, dtype=q.dtype, device=q.device)
-            status = lib().pctree_paged_attention(
-                ctypes.byref(c), batch._ref, q.data_ptr(), self.q_heads, self.scale, _ptr(mask),
+            status = call(
+                ctypes.byref(whole), batch._ref, q.data_ptr(), self.q_heads, self.scale, _ptr(mask),
                 budget, out.data_ptr(), self._ws.on(st), self.ws_bytes, st)
-        _check(status, "pctree_paged_attention")
+        _check(status, name)
         return out
 
 
-def paged_attention(q, k_cache, v_cache, batch, mask=None, scale=None, out=None, stream=None):
+def paged_attention(q, k_cache, v_cache, batch, mask=None, scale=None, out=None, *, k_scale=None,
+                    v_scale=None, stream=None):
     """One call of :class:`PagedAttention`."""
     with _Here(batch.idx, stream):
         layer = PagedAttention(batch, q.shape[1], k_cache.shape[1], k_cache.shape[3],
                                k_cache.shape[2], scale)
-        return layer(q, k_cache, v_cache, batch, mask=mask, out=out)
+        return layer(q, k_cache, v_cache, batch, mask=mask, out=out, k_scale=k_scale,
+                     v_scale=v_scale)
 
 
-def compact_paged(pool, page_table, prefix_len, accept_node, accept_len, budget, stream=None):
+def compact_paged(pool, page_table, prefix_len, accept_node, accept_len, budget, stream=None, *,
+                  scale=None):
     """Move each request's accepted slots right after its prefix, in place.
 
     ``pool [groups][pages][heads][page_size][...]`` (e.g. every layer's K and V):
     the dimensions past ``page_size`` form a slot of a head, a multiple of 16 bytes;
-    groups and pages may lie apart."""
+    groups and pages may lie apart.  Pages in 8 bits (``pool [groups][pages][heads]
+    [page_size][D]`` float8_e4m3fn) come with ``scale [groups][pages][heads][page_size /
+    block]`` float8_e8m0fnu, which moves and grows with them."""
     budget = _size("budget", budget)
     if not isinstance(pool, torch.Tensor) or not pool.is_cuda or pool.dim() < 5 or \
             not (pool.is_contiguous() or pool[0, 0].is_contiguous()):
@@ -840,12 +938,39 @@ def compact_paged(pool, page_table, prefix_len, accept_node, accept_len, budget,
     stride = pool.stride()
     page_stride = stride[1] * es if pages > 1 else heads * P * slot
     group_stride = stride[0] * es if G > 1 else 0
+    if scale is not None:
+        if pool.dtype is not _HELD or pool.dim() != 5:
+            raise ValueError("scales go with a float8_e4m3fn pool [groups][pages][heads][page_size][D]")
+        return _compact_held(pool, group_stride, page_stride, scale, page_table, prefix_len,
+                             accept_node, accept_len, budget, stream)
     with _Here(idx, stream) as st:
         status = lib().pctree_compact_paged(
             pool.data_ptr(), group_stride, page_stride, *shape, slot, page_table.data_ptr(),
             page_table.shape[1], prefix_len.data_ptr(), accept_node.data_ptr(),
             accept_len.data_ptr(), R, budget, W - 1, st)
     _check(status, "pctree_compact_paged")
+    return pool
+
+
+def _compact_held(pool, group_stride, page_stride, scale, page_table, prefix_len, accept_node,
+                  accept_len, budget, stream):
+    G, pages, heads, P, D = pool.shape
+    idx = pool.get_device()
+    if not isinstance(scale, torch.Tensor) or scale.dtype is not _SCALE:
+        raise TypeError("scale must be a float8_e8m0fnu tensor")
+    if scale.dim() != 4 or scale.shape[:3] != (G, pages, heads) or scale.get_device() != idx or \
+            not scale.shape[3] or P % scale.shape[3] or not scale[0, 0].is_contiguous():
+        raise ValueError(f"scale must be a [{G}][{pages}][{heads}][{P} / block] tensor on the pool's "
+                         "device, a page's scales contiguous")
+    n, ss = scale.shape[3], scale.stride()
+    R, W = accept_node.shape
+    with _Here(idx, stream) as st:
+        status = lib().pctree_compact_paged8(
+            pool.data_ptr(), group_stride, page_stride, scale.data_ptr(), ss[0] if G > 1 else 0,
+            ss[1] if pages > 1 else heads * n, G, pages, heads, P, D, P // n,
+            page_table.data_ptr(), page_table.shape[1], prefix_len.data_ptr(),
+            accept_node.data_ptr(), accept_len.data_ptr(), R, budget, W - 1, st)
+    _check(status, "pctree_compact_paged8")
     return pool
 
 
@@ -917,6 +1042,142 @@ def sample(logits, uniform, *, temperature=None, top_k=None, top_p=None, min_p=N
     with _Here(logits.get_device(), stream):
         return Sampler(*logits.shape, device=logits.device)(
             logits, uniform, temperature=temperature, top_k=top_k, top_p=top_p, min_p=min_p)
+
+
+def _rows_2d(name, t, dtype, T, H, idx):
+    """Row stride of a [T][H] tensor whose rows may lie apart."""
+    if not isinstance(t, torch.Tensor) or t.dtype is not dtype:
+        raise TypeError(f"{name} must be a {dtype} tensor")
+    if t.shape != (T, H) or t.get_device() != idx or idx < 0:
+        raise ValueError(f"{name} must be a [{T}][{H}] tensor on the device of the other tensors, "
+                         f"got {tuple(t.shape)}")
+    st = t.stride()
+    if (H > 1 and st[1] != 1) or (T > 1 and st[0] < H):
+        raise ValueError(f"a row of {name} must be contiguous, rows must not overlap")
+    return st[0] if T > 1 else H
+
+
+def rms_norm(x, weight=None, residual=None, *, eps=1e-6, group=None, out=None, scale=None,
+             stream=None):
+    """``v = x + residual`` (``residual`` becomes ``v``), then ``v / sqrt(mean(v^2) + eps) *
+    weight`` of every row of ``x [T][H]`` (bfloat16 or float16; rows may lie apart).
+
+    Returns it in x's type (in ``out`` if given, which may be ``x``) or, with ``group``, as
+    ``(out, scale)``: float8_e4m3fn, and float32 scales ``[T][ceil(H / group)]`` that a group's
+    values are to be multiplied by (``group`` 32, 64, 128 or 256 elements, 0: a whole row)."""
+    if not isinstance(x, torch.Tensor) or x.dtype not in _HALVES:
+        raise TypeError("x must be a bfloat16 or float16 tensor")
+    if x.dim() != 2 or not x.is_cuda:
+        raise ValueError("x must be a [T][H] device tensor")
+    T, H = x.shape
+    idx, dt = x.get_device(), x.dtype
+    xs = _rows_2d("x", x, dt, T, H, idx)
+    if weight is not None:
+        _device_tensor("weight", weight, dt, (H,), idx)
+    rs = 0 if residual is None else _rows_2d("residual", residual, dt, T, H, idx)
+    held = group is not None
+    if held:
+        group = _size("group", group)
+        if group < 0:
+            raise ValueError(f"group must be 32, 64, 128, 256 or 0, got {group}")
+        n = -(-H // group) if group else 1
+    elif scale is not None:
+        raise ValueError("scale goes with group")
+    with _Here(idx, stream) as st:
+        if out is None:
+            out = torch.empty((T, H), dtype=_HELD if held else dt, device=x.device)
+        os_ = _rows_2d("out", out, _HELD if held else dt, T, H, idx)
+        if held:
+            if scale is None:
+                scale = torch.empty((T, n), dtype=torch.float32, device=x.device)
+            else:
+                _device_tensor("scale", scale, torch.float32, (T, n), idx)
+        a = _Norm(x.data_ptr(), _ptr(weight), _ptr(residual), out.data_ptr(), _ptr(scale), xs, rs,
+                  os_, T, H, group if held else 0, _HALVES[dt], eps)
+        status = lib().pctree_rms_norm(ctypes.byref(a), st)
+    _check(status, "pctree_rms_norm")
+    return (out, scale) if held else out
+
+
+def adjust_logits(logits, row_start, row_count, *, max_rows=None, history=None, history_start=None,
+                  history_count=None, prompt_count=None, repetition=None, frequency=None,
+                  presence=None, bias_token=None, bias_value=None, bias_start=None,
+                  bias_count=None, token=None, mask=None, allowed=None, allowed_row=None,
+                  stream=None):
+    """Penalties for repeated tokens, biases and a grammar's mask, on ``logits [T][V]`` (float32,
+    bfloat16 or float16; rows may lie apart) in place, before :class:`Sampler`.
+
+    Request ``r`` has rows ``row_start[r] + i``, ``i < row_count[r]`` (``max_rows``: the most any
+    has).  Its tokens so far are ``history_count[r]`` of ``history`` from ``history_start[r]``, the
+    first ``prompt_count[r]`` of them its prompt; with ``token [R][N]`` and ``mask``
+    (:func:`build_mask`) row ``i`` is a tree's node and counts its ancestors and itself too.
+    ``repetition`` (divides or multiplies the logits of tokens that were there, the prompt's
+    too), ``frequency`` (times the count since the prompt) and ``presence`` are ``[R]`` float32.
+    ``bias_value`` is added to the logits of ``bias_token``, ``bias_count[r]`` entries from
+    ``bias_start[r]`` (of a token's entries the last).  ``allowed [M][ceil(V / 32)]`` (int32
+    words): tokens whose bit is not set become -inf; row ``t`` takes mask ``allowed_row[t]`` (no
+    mask where that is none's index) or ``t``.  See include/pctree.h.  Returns ``logits``."""
+    if not isinstance(logits, torch.Tensor) or logits.dtype not in _LOGITS:
+        raise TypeError("logits must be a float32, bfloat16 or float16 tensor")
+    if logits.dim() != 2 or not logits.is_cuda:
+        raise ValueError("logits must be a [T][V] device tensor")
+    T, V = logits.shape
+    idx = logits.get_device()
+    stride = _rows_2d("logits", logits, logits.dtype, T, V, idx)
+    i32, f32 = torch.int32, torch.float32
+    if not isinstance(row_start, torch.Tensor) or row_start.dim() != 1:
+        raise ValueError("row_start must be an [R] tensor")
+    R = row_start.shape[0]
+    one = (R,)
+    _device_tensor("row_start", row_start, i32, one, idx)
+    _device_tensor("row_count", row_count, i32, one, idx)
+    most = T if max_rows is None else _size("max_rows", max_rows)
+
+    def listed(values, names):  # a list over all requests, and what goes with it
+        if values[0] is None:
+            return 0
+        n = values[0].numel() if isinstance(values[0], torch.Tensor) else 0
+        for name, t, dt in zip(names, values, (i32, f32)):
+            _device_tensor(name, t, dt, (n,), idx)
+        return _size(names[0], n)
+
+    total = listed((history,), ("history",))
+    biases = listed((bias_token, bias_value), ("bias_token", "bias_value"))
+    for name, t, dt in (("history_start", history_start, i32), ("history_count", history_count, i32),
+                        ("prompt_count", prompt_count, i32), ("repetition", repetition, f32),
+                        ("frequency", frequency, f32), ("presence", presence, f32),
+                        ("bias_start", bias_start, i32), ("bias_count", bias_count, i32)):
+        if t is not None:
+            _device_tensor(name, t, dt, one, idx)
+    budget = masks = 0
+    if token is not None:
+        budget = token.shape[1] if isinstance(token, torch.Tensor) and token.dim() == 2 else 0
+        _device_tensor("token", token, i32, (R, budget), idx)
+    if mask is not None:
+        if mask.dtype != torch.int32 and mask.dtype != torch.uint32:
+            raise TypeError("mask must be the [R][N][(N+31)/32] words of build_mask")
+        _device_tensor("mask", mask, mask.dtype, (R, budget, (budget + 31) // 32), idx)
+    if allowed is not None:
+        if not isinstance(allowed, torch.Tensor) or \
+                (allowed.dtype != torch.int32 and allowed.dtype != torch.uint32):
+            raise TypeError("allowed must be an int32 or uint32 tensor of words")
+        masks = allowed.shape[0] if allowed.dim() == 2 else 0
+        _device_tensor("allowed", allowed, allowed.dtype, (masks, (V + 31) // 32), idx)
+    if allowed_row is not None:
+        _device_tensor("allowed_row", allowed_row, i32, (T,), idx)
+    if history is not None and not total:  # (no request has any)
+        history = history_start = history_count = prompt_count = None
+    if bias_token is not None and not biases:
+        bias_token = bias_value = bias_start = bias_count = None
+    given = (row_start, row_count, history, history_start, history_count, prompt_count, repetition,
+             frequency, presence, bias_token, bias_value, bias_start, bias_count, token, mask,
+             allowed, allowed_row)
+    with _Here(idx, stream) as st:
+        a = _Adjust(logits.data_ptr(), stride, *map(_ptr, given), T, V, R, most, total, biases,
+                    budget, _size("masks", masks), _LOGITS[logits.dtype])
+        status = lib().pctree_adjust_logits(ctypes.byref(a), st)
+    _check(status, "pctree_adjust_logits")
+    return logits
 
 
 def device_inputs(inp: dict, device="cuda") -> dict:

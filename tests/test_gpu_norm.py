@@ -1,0 +1,129 @@
+"""GPU parity of the norm before a projection against the float64 oracle.
+
+Tolerances, with u the 16-bit type's half step: float32 arithmetic, whose sum of H squares goes
+through chains of at most 8 * 4 + 6 + 16 additions, so that its root is off by less than 30 * 2^-24,
+the root, the quotient, the sum and two products by 7 more: y within 2^-18 |y|, then one rounding.
+16 bits: |err| <= (u + 2^-17) |y| (float16's smallest half step 2^-25).  8 bits: a scale within
+2^-17 of its value, and half a step of e4m3: |err| <= (2^-4 + 2^-16) |y| and under its normal
+numbers 2^-10 of the scale.
+"""
+from __future__ import annotations
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import pctree_step as SO
+from paper_2608_02123_amd import pctree as P
+
+pytestmark = pytest.mark.gpu
+
+HALF = {torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11}
+DTYPES = [torch.bfloat16, torch.float16]
+
+
+def _np(t):
+    return t.detach().cpu().double().numpy()
+
+
+def check(x, w, r0, r1, eps, group, got):
+    """x, w and the residual before (r0) and after (r1); got: the call's answer."""
+    u, H = HALF[x.dtype], x.shape[1]
+    v, y = SO.rms_norm(_np(x), None if w is None else _np(w), None if r0 is None else _np(r0), eps)
+    if r0 is not None:
+        assert (np.abs(_np(r1) - v) <= (u + 2.0 ** -23) * np.abs(v) + 2.0 ** -25).all()
+    if group is None:
+        err = np.abs(_np(got) - y)
+        assert got.dtype == x.dtype and (err <= (u + 2.0 ** -17) * np.abs(y) + 2.0 ** -25).all()
+        return
+    out, scale = got
+    assert out.dtype == torch.float8_e4m3fn and scale.dtype == torch.float32
+    c = SO.group_scales(y, group or H)
+    s = _np(scale)
+    assert s.shape == c.shape and (np.abs(s - c) <= 2.0 ** -17 * c + 2.0 ** -149).all()
+    full = np.repeat(s, group or H, 1)[:, :H]
+    err = np.abs(_np(out) * full - y)
+    assert (err <= np.maximum((2.0 ** -4 + 2.0 ** -16) * np.abs(y), 2.0 ** -10 * full + 2.0 ** -16 * np.abs(y))).all()
+
+
+def run(T, H, group, dt, seed=0, residual=True, weight=True, eps=1e-6, amplitude=1.0, stride=0):
+    g = torch.Generator().manual_seed(seed)
+
+    def rows(a=1.0):
+        t = torch.zeros(T, H + stride, dtype=dt, device="cuda")[:, :H]
+        t.copy_(torch.randn(T, H, generator=g) * a)
+        return t
+    x, r = rows(amplitude), rows(amplitude) if residual else None
+    w = (1 + 0.2 * torch.randn(H, generator=g)).to(dt).cuda() if weight else None
+    r0 = r.clone() if residual else None
+    got = P.rms_norm(x, w, r, eps=eps, group=group)
+    check(x, w, r0, r, eps, group, got)
+
+
+@pytest.mark.parametrize("dt", DTYPES)
+@pytest.mark.parametrize("group", [None, 0, 32, 64, 128, 256])
+@pytest.mark.parametrize("T,H", [(1, 8), (3, 64), (2, 200), (5, 512), (1, 1000), (7, 2880), (4, 5120), (2, 8200),
+                                 (3, 16392), (1, 32768)])
+def test_rows(dt, group, T, H):
+    run(T, H, group, dt, seed=H)
+
+
+@pytest.mark.parametrize("kw", [dict(residual=False), dict(weight=False), dict(residual=False, weight=False),
+                                dict(stride=64), dict(eps=0.0), dict(eps=1.0), dict(amplitude=1e-3),
+                                dict(amplitude=1e3)])
+@pytest.mark.parametrize("group", [None, 0, 128])
+def test_options(kw, group):
+    run(33, 2560, group, torch.bfloat16, seed=3, **kw)
+
+
+def test_many_rows():
+    run(3000, 1024, 128, torch.bfloat16)
+
+
+def test_zeros_infinities_and_nan():
+    """A row of zeros has scales and values of zero; what is not finite stays where it is."""
+    x = torch.zeros(4, 256, dtype=torch.bfloat16, device="cuda")
+    x[1:] = torch.randn(3, 256, generator=torch.Generator().manual_seed(1)).bfloat16().cuda()
+    x[1, 3], x[2, 77] = float("nan"), float("inf")
+    for group in (None, 0, 32):
+        got = P.rms_norm(x, group=group)
+        y = got if group is None else got[0].float()
+        assert (y[0] == 0).all() and torch.isfinite(y[3]).all()
+        assert torch.isnan(y[1]).all() or torch.isnan(y[1, 3])  # (its square is in the row's mean)
+        assert torch.isnan(y[2, 77]) and (y[2, :77] == 0).all()
+        if group is not None:
+            assert (got[1][0] == 0).all() and torch.isfinite(got[1]).all()
+    got, scale = P.rms_norm(x * 0, torch.ones(256, dtype=torch.bfloat16, device="cuda"), eps=0.0, group=32)
+    assert torch.isnan(got.float()).all() and (scale == 0).all()  # 0 / 0
+
+
+def test_outputs_given_and_in_place():
+    g = torch.Generator().manual_seed(2)
+    x = torch.randn(6, 512, generator=g).half().cuda()
+    y = P.rms_norm(x)
+    wide = torch.full((6, 640), 9.0, dtype=torch.float16, device="cuda")
+    assert P.rms_norm(x, out=wide[:, :512]).data_ptr() == wide.data_ptr()
+    assert torch.equal(wide[:, :512], y) and (wide[:, 512:] == 9).all()
+    z = x.clone()
+    assert P.rms_norm(z, out=z) is z and torch.equal(z, y)
+    out = torch.empty(6, 512, dtype=torch.float8_e4m3fn, device="cuda")
+    scale = torch.empty(6, 4, device="cuda")
+    a, b = P.rms_norm(x, group=128, out=out, scale=scale)
+    assert a is out and b is scale
+    want, ws = P.rms_norm(x, group=128)
+    assert torch.equal(out.view(torch.uint8), want.view(torch.uint8)) and torch.equal(scale, ws)
+
+
+def test_refusals():
+    x = torch.zeros(4, 256, dtype=torch.bfloat16, device="cuda")
+    for kw, error in ((dict(weight=x[0].half()), TypeError), (dict(weight=x[0, :8]), ValueError),
+                      (dict(residual=x[:3]), ValueError), (dict(residual=x.t().contiguous().t()), ValueError),
+                      (dict(group=100), P.PCTreeError), (dict(group=-1), ValueError), (dict(scale=x), ValueError),
+                      (dict(group=0, out=x), TypeError), (dict(group=1.5), TypeError),
+                      (dict(eps=-1.0), P.PCTreeError)):
+        with pytest.raises(error):
+            P.rms_norm(x, **kw)
+    with pytest.raises(P.PCTreeError):
+        P.rms_norm(x[:, :100])
+    with pytest.raises(P.PCTreeError):
+        P.rms_norm(x[:, 4:12])
