@@ -612,7 +612,7 @@ typedef struct pctree_adjust {
 
 /* Errors: INVALID_ARGUMENT (null or misaligned pointer, a size that the comments rule
  * out), UNSUPPORTED (vocab > PCTREE_MAX_VOCAB, requests > 65535, budget >
- * PCTREE_MAX_MASK_BUDGET, history_total past its limit). */
+ * PCTREE_MAX_MASK_BUDGET, history_total past its limit, sizes past a launch). */
 pctree_status pctree_adjust_logits(const pctree_adjust* args, void* stream);
 
 /* Static, human-readable name of a status code. */

@@ -47,6 +47,8 @@ struct AdjustArgs {
   const int* allowed_row;   // [T] or null
   int M, AW;
 };
+// Whether a launch can have the call's workgroups.
+bool adjust_fits(const AdjustArgs& a);
 hipError_t launch_adjust(const AdjustArgs& a, int dtype, hipStream_t stream);
 
 }  // namespace pctree

@@ -9,8 +9,7 @@ namespace {
 
 bool aligned(const void* ptr, size_t a) { return ((uintptr_t)ptr & (a - 1)) == 0; }
 
-// A launch has at most 2^32 - 1 threads along x; a row of the norm has up to 1024.  (An
-// adjustment of the most requests and tokens is 65535 * 256 workgroups of 256.)
+// A launch has at most 2^32 - 1 threads along x; a row of the norm has up to 1024.
 constexpr int32_t kMaxNormRows = 1 << 21;
 constexpr int32_t kMaxHistory = (1 << 29) - 1;  // a count's bits (pctree_adjust.hip)
 
@@ -135,6 +134,7 @@ pctree_status pctree_adjust_logits(const pctree_adjust* j, void* stream) {
     a.allowed_row = j->allowed_row;
     a.M = j->masks;
     a.AW = (j->vocab + 31) / 32;
+    if (!adjust_fits(a)) return PCTREE_ERR_UNSUPPORTED;
     (void)hipGetLastError();
     const hipError_t e = launch_adjust(a, j->dtype, (hipStream_t)stream);
     return e == hipSuccess ? PCTREE_OK : PCTREE_ERR_HIP;

@@ -708,13 +708,14 @@ class PagedBatch:
 
 
 _HELD, _SCALE = torch.float8_e4m3fn, torch.float8_e8m0fnu
+_HELD_ONLY = (_HELD,)
 
 
 def _paged_cache(k, v, idx, rows=None):
     """The C view of one layer's pages [pages][Hkv][page_size][D]; the pages may lie
     apart (stride 0 is free, the same for both).  ``rows``: the new rows' type, where
     the pages are held in 8 bits."""
-    types = _HALVES if rows is None else {_HELD: _HALVES.get(rows)}
+    types = _HALVES if rows is None else _HELD_ONLY
     for name, t in (("k_cache", k), ("v_cache", v)):
         if not isinstance(t, torch.Tensor) or t.dtype not in types:
             raise TypeError(f"{name} must be a bfloat16 or float16 tensor" if rows is None else
@@ -731,7 +732,7 @@ def _paged_cache(k, v, idx, rows=None):
             (vs[1:] != inner and not v[0].is_contiguous()):
         raise ValueError("a page's [Hkv][page_size][D] must be contiguous")
     return _PagedCache(k.data_ptr(), v.data_ptr(), ks[0] if pages > 1 else Hkv * P * D, pages, P,
-                       Hkv, D, types[k.dtype])
+                       Hkv, D, _HALVES[rows or k.dtype])
 
 
 def _held_cache(k, v, k_scale, v_scale, rows, idx):
@@ -800,14 +801,13 @@ def append_paged(batch, k_cache, v_cache, k, v, q=None, *, q_norm=None, k_norm=N
     [pages][Hkv][page_size / block]`` float8_e8m0fnu, a block being 8, 16, 32 or 64 slots
     (include/pctree.h)."""
     idx, T = batch.idx, batch.rows
-    held = k_scale is not None or v_scale is not None
-    if held:
-        dt = getattr(k, "dtype", None)
-        whole = _held_cache(k_cache, v_cache, k_scale, v_scale, dt, idx)
-        c, call, name = whole.pages, lib().pctree_append_paged8, "pctree_append_paged8"
-    else:
+    if k_scale is None and v_scale is None:
         c = whole = _paged_cache(k_cache, v_cache, idx)
-        dt, call, name = k_cache.dtype, lib().pctree_append_paged, "pctree_append_paged"
+        dt, call = k_cache.dtype, lib().pctree_append_paged
+    else:
+        dt, call = k.dtype, lib().pctree_append_paged8
+        whole = _held_cache(k_cache, v_cache, k_scale, v_scale, dt, idx)
+        c = whole.pages
     D = c.head_dim
     ks, kh = _row_tensor("k", k, T, D, dt, idx)
     vs, vh = _row_tensor("v", v, T, D, dt, idx)
@@ -840,7 +840,7 @@ def append_paged(batch, k_cache, v_cache, k, v, q=None, *, q_norm=None, k_norm=N
                     _ptr(q_norm), _ptr(k_norm), _ptr(rope), _ptr(position), eps, Hq, rot, npos,
                     1 if interleaved else 0)
         status = call(ctypes.byref(whole), batch._ref, ctypes.byref(a), st)
-    _check(status, name)
+    _check(status, "pctree_append_paged")
     return q_out
 
 
@@ -871,13 +871,13 @@ class PagedAttention:
         idx = self.idx
         if batch.sizes != self.sizes or batch.idx != idx:
             raise ValueError("the batch is not of this object's sizes")
-        if k_scale is not None or v_scale is not None:
-            dt = getattr(q, "dtype", None)
-            whole = _held_cache(k_cache, v_cache, k_scale, v_scale, dt, idx)
-            c, call, name = whole.pages, lib().pctree_paged_attention8, "pctree_paged_attention8"
-        else:
+        if k_scale is None and v_scale is None:
             c = whole = _paged_cache(k_cache, v_cache, idx)
-            dt, call, name = k_cache.dtype, lib().pctree_paged_attention, "pctree_paged_attention"
+            dt, call = k_cache.dtype, lib().pctree_paged_attention
+        else:
+            dt, call = q.dtype, lib().pctree_paged_attention8
+            whole = _held_cache(k_cache, v_cache, k_scale, v_scale, dt, idx)
+            c = whole.pages
         if c.kv_heads != self.kv_heads or c.head_dim != self.head_dim or \
                 c.page_size != self.page_size:
             raise ValueError("the pages are not of this object's sizes")
@@ -898,7 +898,7 @@ class PagedAttention:
             status = call(
                 ctypes.byref(whole), batch._ref, q.data_ptr(), self.q_heads, self.scale, _ptr(mask),
                 budget, out.data_ptr(), self._ws.on(st), self.ws_bytes, st)
-        _check(status, name)
+        _check(status, "pctree_paged_attention")
         return out
 
 

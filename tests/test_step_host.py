@@ -50,7 +50,8 @@ def test_norms_that_are_refused(kw, code):
     (dict(allowed=None), 1), (dict(allowed=None, masks=0), 1), (dict(allowed_row=None, masks=5), 1),
     (dict(repetition=A + 2), 1), (dict(bias_token=A + 1), 1), (dict(allowed=A + 2), 1),
     (dict(vocab=(1 << 20) + 1, row_stride=1 << 21), 2), (dict(requests=70000), 2), (dict(budget=1025), 2),
-    (dict(history_total=1 << 29), 2)])
+    (dict(history_total=1 << 29), 2), (dict(vocab=1 << 20, row_stride=1 << 20, requests=65535, rows=65535), 2),
+    (dict(vocab=1 << 20, row_stride=1 << 20, rows=1 << 22, masks=1), 2)])
 def test_adjustments_that_are_refused(kw, code):
     assert adjust(**kw) == code
     assert P.lib().pctree_adjust_logits(None, None) == P.ERR_INVALID_ARGUMENT
