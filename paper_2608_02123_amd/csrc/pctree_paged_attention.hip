@@ -153,10 +153,14 @@ __device__ __forceinline__ Work work_of(const PagedAttnArgs& a, int qblocks, int
   PagedReq q = attn_req(a, min(lane, a.b.R - 1));
   if (lane >= a.b.R || few_rows(a, q.cnt) != few) q.cnt = 0;
   const int len = q.prefix + q.cnt, blocks = (q.cnt * a.g + rows - 1) / rows;
+  // (equal lengths by lane, and those past 2^25 as equal; without branches: 64 rounds of
+  // them were 5 us of every workgroup)
+  const int key = min(len, (1 << 25) - 1) << 6 | (63 - lane);
   int before = 0;
-  for (int i = 0; i < a.b.R; ++i) {
-    const int l = __builtin_amdgcn_readlane(len, i), n = __builtin_amdgcn_readlane(blocks, i);
-    before += l > len || (l == len && i < lane) ? n : 0;
+  for (int i0 = 0; i0 < a.b.R; i0 += 8) {
+#pragma unroll
+    for (int i = i0; i < i0 + 8; ++i)
+      before += __builtin_amdgcn_readlane(blocks, i) & -(int)(__builtin_amdgcn_readlane(key, i) > key);
   }
   const uint64_t mine = __ballot(rb >= before && rb - before < blocks);
   w.ok = mine != 0;
@@ -933,6 +937,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3))) v
     PagedAttnArgs a) {
   constexpr int DT = D / 16, HU = D / 16, KU = HU / 4;  // 16-byte units of a row, of a lane's keys
   constexpr int INS = kFewChunk8 * HU / 64;             // load instructions of a chunk's V
+  constexpr int RPI = 64 / HU;                          // slots of one of these
   constexpr int BANKS = 16 / HU;                        // rows of 256 bytes
   __shared__ __attribute__((aligned(16))) uint8_t sV[kWaves][kFewChunk8 * D];
   __shared__ float2 sML[kWaves][16];
@@ -983,38 +988,64 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3))) v
   float m = kNegInf;
 #pragma unroll
   for (int t = 0; t < DT; ++t) o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-  const int krow0 = 8 * (col >> 2) + (col & 3);
   const int vkey = 8 * grp + (col >> 1);  // the slot whose values this lane addresses
   constexpr uint32_t one = H ? 0x3c003c00u : 0x3f803f80u;
   const u32x4 ones = {one, one, one, one};
+  // The lane's place in a chunk: of its keys (slots 8 c + e and, 4 further, 8 c + 4 + e of a
+  // half; the same eight, so the same page and scale) and of the values it loads, the
+  // units of a row permuted so that 16 rows' reads of one unit meet all banks.
+  const int kgroup = col >> 2, krow = 8 * kgroup + (col & 3);
+  const uint32_t koff = (uint32_t)(krow * HU + grp) * 16;
+  uint32_t voff[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int row = i * RPI + lane / HU;
+    voff[i] = (uint32_t)(lane / HU * HU + (lane % HU ^ (row / BANKS % HU))) * 16;
+  }
+  const size_t head_bytes = (size_t)wk.kvh * a.b.head_units * 16;
+  const size_t page_bytes = (size_t)a.b.page_units * 16;
   for (int c0 = c_first; c0 < kend; c0 += kWaves * kFewChunk8) {
     const bool none = (unsigned)pg >= (unsigned)a.b.pages;
     const uint64_t bad = __ballot(none);
     const uint32_t pgc = none ? 0u : (uint32_t)pg;
-    const int last = kend - 1 - c0;  // (slots past the run repeat its last one)
-    auto at = [&](int row) __attribute__((always_inline)) {  // 16-byte units before the row
-      row = min(row, last);
-      const uint32_t p = __builtin_amdgcn_ds_bpermute(row * 4, pgc);
-      return (size_t)p * a.b.page_units + (size_t)wk.kvh * a.b.head_units +
-             (uint32_t)((c0 + row) & pmask) * HU;
-    };
-    // Values, their rows' units permuted so that 16 rows' reads of one unit meet all banks.
-#pragma unroll
-    for (int i = 0; i < INS; ++i) {
-      const int u = i * 64 + lane, row = u / HU, pos = u % HU;
-      load_lds16((const uint4*)a.v + at(row) + (pos ^ (row / BANKS % HU)), &sV[wave][i * 1024]);
-    }
+    // (slots past the run: others of its last page, which no row admits)
     u32x4 kx[2][2][KU];
+    if (a.b.page_shift >= 6) {  // the chunk lies in one page
+      const size_t at = (uint32_t)__builtin_amdgcn_readfirstlane((int)pgc) * page_bytes + head_bytes +
+                        (uint32_t)(c0 & pmask) * D;
+      const uint8_t *kb = (const uint8_t*)a.k + at, *vb = (const uint8_t*)a.v + at;
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
+      for (int i = 0; i < INS; ++i) load_lds16(vb + i * 1024, voff[i & 1], &sV[wave][i * 1024]);
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        const u32x4* kr = (const u32x4*)a.k + at(32 * h + krow0 + 4 * t) + grp;
+      for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int u = 0; u < KU; ++u) kx[h][t][u] = kr[4 * u];
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int u = 0; u < KU; ++u)
+            kx[h][t][u] = *(const u32x4*)(kb + (32 * h + 4 * t) * D + u * 64 + koff);
+    } else {
+#pragma unroll
+      for (int i = 0; i < INS; ++i) {
+        const int row = i * RPI + lane / HU;
+        const uint32_t p = __builtin_amdgcn_ds_bpermute(row * 4, pgc);
+        load_lds16((const uint8_t*)a.v + p * page_bytes + head_bytes +
+                       (uint32_t)((c0 + row) & pmask) * D + (voff[i & 1] % D),
+                   &sV[wave][i * 1024]);
       }
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int row = 32 * h + krow;
+        const uint32_t p = __builtin_amdgcn_ds_bpermute(row * 4, pgc);
+        const uint8_t* kb = (const uint8_t*)a.k + p * page_bytes + head_bytes +
+                            (uint32_t)((c0 + row) & pmask) * D + grp * 16;
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int u = 0; u < KU; ++u) kx[h][t][u] = *(const u32x4*)(kb + 4 * t * D + u * 64);
+      }
+    }
     // the scales of the chunk's groups of eight slots: keys in lanes 0 to 7, values in 8 to 15
-    const int srow = min(8 * (lane & 7), last);
+    const int srow = 8 * (lane & 7);
     const size_t sp = scale_place(a, __builtin_amdgcn_ds_bpermute(srow * 4, pgc), wk.kvh,
                                   (c0 + srow) & pmask);
     const int sbyte = scale_in((lane & 8 ? a.s.v : a.s.k)[sp]);
@@ -1022,7 +1053,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3))) v
     f32x4 sacc[2][2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const float kf = scale_up(__builtin_amdgcn_ds_bpermute((4 * h + (col >> 2)) * 4, sbyte));
+      const float kf = scale_up(__builtin_amdgcn_ds_bpermute((4 * h + kgroup) * 4, sbyte));
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
         sacc[h][t] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -1046,7 +1077,27 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3))) v
     l = mfma16<H>(ones, bp[0], l);
     l = mfma16<H>(ones, bp[1], l);
     wait_loads();
-    bool odd = false;
+    if (!full) {  // infinite and NaN values become zeros
+      bool odd = false;
+#pragma unroll 1
+      for (int i = 0; i < INS; ++i) {
+        u32x4 w = *(const u32x4*)(sV[wave] + i * 1024 + lane * 16);
+        const float f = scale_up(__builtin_amdgcn_ds_bpermute((8 + (i * RPI + lane / HU) / 8) * 4, sbyte));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const u32x2 v = held4<H>(w[e], f);
+          uint32_t keep = 0xffffffffu;
+          if (odd16<H>(v[0])) keep &= 0xffffff00u;
+          if (odd16<H>(v[0] >> 16)) keep &= 0xffff00ffu;
+          if (odd16<H>(v[1])) keep &= 0xff00ffffu;
+          if (odd16<H>(v[1] >> 16)) keep &= 0x00ffffffu;
+          odd |= keep != 0xffffffffu;
+          w[e] &= keep;
+        }
+        *(u32x4*)(sV[wave] + i * 1024 + lane * 16) = w;
+      }
+      if (odd) sOdd = 1;
+    }
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const float vf = scale_up(__builtin_amdgcn_ds_bpermute((8 + 4 * h + grp) * 4, sbyte));
@@ -1054,19 +1105,9 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3))) v
 #pragma unroll
       for (int t = 0; t < DT; ++t) {
         const u32x2 w = read_tr8(sV[wave] + key * D + (t ^ (key / BANKS % HU)) * 16 + (col & 1) * 8);
-        u32x4 v = held8<H>(w[0], w[1], vf);
-        if (!full) {  // infinite and NaN values become zeros
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const uint32_t f = fine_pair<H>(v[e]);
-            odd |= f != v[e];
-            v[e] = f;
-          }
-        }
-        o[t] = mfma16<H>(v, bp[h], o[t]);
+        o[t] = mfma16<H>(held8<H>(w[0], w[1], vf), bp[h], o[t]);
       }
     }
-    if (odd) sOdd = 1;
     // (the tile's reads are back before the next chunk's loads overwrite it)
     __atomic_signal_fence(__ATOMIC_SEQ_CST);
     __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)

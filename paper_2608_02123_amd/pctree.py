@@ -744,17 +744,19 @@ def _held_cache(k, v, k_scale, v_scale, rows, idx):
         if not isinstance(t, torch.Tensor) or t.dtype is not _SCALE:
             raise TypeError(f"{name} must be a float8_e8m0fnu tensor beside pages in 8 bits")
     c = _paged_cache(k, v, idx, rows)
-    for name, t in (("k_scale", k_scale), ("v_scale", v_scale)):
-        if t.dim() != 3 or t.get_device() != idx or t.shape[:2] != k.shape[:2]:
-            raise ValueError(f"{name} must be a [pages][Hkv][page_size / block] tensor on the "
-                             "batch's device")
-    pages, Hkv, n = k_scale.shape
+    if k_scale.dim() != 3 or k_scale.get_device() != idx or v_scale.get_device() != idx:
+        raise ValueError("k_scale and v_scale must be [pages][Hkv][page_size / block] tensors on the "
+                         "batch's device")
+    pages, Hkv, n = shape = k_scale.shape
     ks, vs = k_scale.stride(), v_scale.stride()
-    if k_scale.shape != v_scale.shape or (pages > 1 and ks[0] != vs[0]):
-        raise ValueError("k_scale and v_scale must have one shape and page stride")
+    if pages != c.pages or Hkv != c.kv_heads or shape != v_scale.shape or \
+            (pages > 1 and ks[0] != vs[0]):
+        raise ValueError("k_scale and v_scale must be of the pages' and heads' number, with one shape "
+                         "and page stride")
     if n < 1 or c.page_size % n:
         raise ValueError(f"{n} scales do not divide a page of {c.page_size} slots")
-    if not k_scale[0].is_contiguous() or not v_scale[0].is_contiguous():
+    if (ks[1:] != (n, 1) and not k_scale[0].is_contiguous()) or \
+            (vs[1:] != (n, 1) and not v_scale[0].is_contiguous()):
         raise ValueError("a page's scales must be contiguous")
     return _PagedCache8(c, k_scale.data_ptr(), v_scale.data_ptr(), ks[0] if pages > 1 else Hkv * n,
                         c.page_size // n)
@@ -958,11 +960,11 @@ def _compact_held(pool, group_stride, page_stride, scale, page_table, prefix_len
     idx = pool.get_device()
     if not isinstance(scale, torch.Tensor) or scale.dtype is not _SCALE:
         raise TypeError("scale must be a float8_e8m0fnu tensor")
-    if scale.dim() != 4 or scale.shape[:3] != (G, pages, heads) or scale.get_device() != idx or \
-            not scale.shape[3] or P % scale.shape[3] or not scale[0, 0].is_contiguous():
+    n, ss = scale.shape[-1] if scale.dim() == 4 else 0, scale.stride()
+    if n < 1 or P % n or scale.shape != (G, pages, heads, n) or scale.get_device() != idx or \
+            (ss[2:] != (n, 1) and not scale[0, 0].is_contiguous()):
         raise ValueError(f"scale must be a [{G}][{pages}][{heads}][{P} / block] tensor on the pool's "
                          "device, a page's scales contiguous")
-    n, ss = scale.shape[3], scale.stride()
     R, W = accept_node.shape
     with _Here(idx, stream) as st:
         status = lib().pctree_compact_paged8(
@@ -1057,6 +1059,10 @@ def _rows_2d(name, t, dtype, T, H, idx):
     return st[0] if T > 1 else H
 
 
+def _list_size(name, t):
+    return _size(name, t.numel()) if isinstance(t, torch.Tensor) else 0
+
+
 def rms_norm(x, weight=None, residual=None, *, eps=1e-6, group=None, out=None, scale=None,
              stream=None):
     """``v = x + residual`` (``residual`` becomes ``v``), then ``v / sqrt(mean(v^2) + eps) *
@@ -1085,11 +1091,12 @@ def rms_norm(x, weight=None, residual=None, *, eps=1e-6, group=None, out=None, s
         raise ValueError("scale goes with group")
     with _Here(idx, stream) as st:
         if out is None:
-            out = torch.empty((T, H), dtype=_HELD if held else dt, device=x.device)
-        os_ = _rows_2d("out", out, _HELD if held else dt, T, H, idx)
+            out, os_ = x.new_empty((T, H), dtype=_HELD if held else dt), H
+        else:
+            os_ = _rows_2d("out", out, _HELD if held else dt, T, H, idx)
         if held:
             if scale is None:
-                scale = torch.empty((T, n), dtype=torch.float32, device=x.device)
+                scale = x.new_empty((T, n), dtype=torch.float32)
             else:
                 _device_tensor("scale", scale, torch.float32, (T, n), idx)
         a = _Norm(x.data_ptr(), _ptr(weight), _ptr(residual), out.data_ptr(), _ptr(scale), xs, rs,
@@ -1133,22 +1140,28 @@ def adjust_logits(logits, row_start, row_count, *, max_rows=None, history=None, 
     _device_tensor("row_count", row_count, i32, one, idx)
     most = T if max_rows is None else _size("max_rows", max_rows)
 
-    def listed(values, names):  # a list over all requests, and what goes with it
-        if values[0] is None:
-            return 0
-        n = values[0].numel() if isinstance(values[0], torch.Tensor) else 0
-        for name, t, dt in zip(names, values, (i32, f32)):
-            _device_tensor(name, t, dt, (n,), idx)
-        return _size(names[0], n)
-
-    total = listed((history,), ("history",))
-    biases = listed((bias_token, bias_value), ("bias_token", "bias_value"))
-    for name, t, dt in (("history_start", history_start, i32), ("history_count", history_count, i32),
-                        ("prompt_count", prompt_count, i32), ("repetition", repetition, f32),
-                        ("frequency", frequency, f32), ("presence", presence, f32),
-                        ("bias_start", bias_start, i32), ("bias_count", bias_count, i32)):
+    # lists over all requests (empty where no request has any), and each request's part
+    total = biases = 0
+    if history is not None:
+        total = _list_size("history", history)
+        _device_tensor("history", history, i32, (total,), idx)
+        if not total:
+            history = history_start = history_count = prompt_count = None
+    if bias_token is not None:
+        biases = _list_size("bias_token", bias_token)
+        _device_tensor("bias_token", bias_token, i32, (biases,), idx)
+        if bias_value is not None:
+            _device_tensor("bias_value", bias_value, f32, (biases,), idx)
+        if not biases:
+            bias_token = bias_value = bias_start = bias_count = None
+    for name, t in (("history_start", history_start), ("history_count", history_count),
+                    ("prompt_count", prompt_count), ("bias_start", bias_start),
+                    ("bias_count", bias_count)):
         if t is not None:
-            _device_tensor(name, t, dt, one, idx)
+            _device_tensor(name, t, i32, one, idx)
+    for name, t in (("repetition", repetition), ("frequency", frequency), ("presence", presence)):
+        if t is not None:
+            _device_tensor(name, t, f32, one, idx)
     budget = masks = 0
     if token is not None:
         budget = token.shape[1] if isinstance(token, torch.Tensor) and token.dim() == 2 else 0
@@ -1161,20 +1174,18 @@ def adjust_logits(logits, row_start, row_count, *, max_rows=None, history=None, 
         if not isinstance(allowed, torch.Tensor) or \
                 (allowed.dtype != torch.int32 and allowed.dtype != torch.uint32):
             raise TypeError("allowed must be an int32 or uint32 tensor of words")
-        masks = allowed.shape[0] if allowed.dim() == 2 else 0
+        masks = _size("masks", allowed.shape[0] if allowed.dim() == 2 else 0)
         _device_tensor("allowed", allowed, allowed.dtype, (masks, (V + 31) // 32), idx)
     if allowed_row is not None:
         _device_tensor("allowed_row", allowed_row, i32, (T,), idx)
-    if history is not None and not total:  # (no request has any)
-        history = history_start = history_count = prompt_count = None
-    if bias_token is not None and not biases:
-        bias_token = bias_value = bias_start = bias_count = None
+    if allowed is not None and not masks:
+        allowed = allowed_row = None
     given = (row_start, row_count, history, history_start, history_count, prompt_count, repetition,
              frequency, presence, bias_token, bias_value, bias_start, bias_count, token, mask,
              allowed, allowed_row)
     with _Here(idx, stream) as st:
         a = _Adjust(logits.data_ptr(), stride, *map(_ptr, given), T, V, R, most, total, biases,
-                    budget, _size("masks", masks), _LOGITS[logits.dtype])
+                    budget, masks, _LOGITS[logits.dtype])
         status = lib().pctree_adjust_logits(ctypes.byref(a), st)
     _check(status, "pctree_adjust_logits")
     return logits
