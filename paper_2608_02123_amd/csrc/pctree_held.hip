@@ -25,6 +25,8 @@ __device__ __forceinline__ float wave_max(float v) {
   return v;
 }
 
+constexpr int kQueries = 4;  // loads that a wave of queries has in flight
+
 // The queries of row t: `part` of `split` waves, 512 / D heads at a time.
 template <int D, bool H>
 __device__ __forceinline__ void append_queries(const AppendArgs& a, int t, int part, int split) {
@@ -36,100 +38,139 @@ __device__ __forceinline__ void append_queries(const AppendArgs& a, int t, int p
   const bool turns = a.rope && e0 < a.rot;
   Turn turn;
   if (turns) load_turn(a, a.position ? a.position[t] : rq.prefix + (t - rq.start), e0, turn);
-  for (int i0 = part * HPW; i0 < a.Hq; i0 += split * HPW) {
-    const int h = i0 + lane / LPH;
-    u32x4 x = {0u, 0u, 0u, 0u};
-    if (h < a.Hq) x = *(const u32x4*)(a.q + t * a.q_stride + h * D + e0);
-    float y[8];
-    unpack8<H>(x, y);
-    if (a.q_norm) norm_head<D, H>(y, a.q_norm, a.eps, e0);
-    if (a.rope) turn_head<D>(a, y, turn, e0, turns);
-    if (h < a.Hq) *(u32x4*)(a.q_out + t * a.q_out_stride + h * D + e0) = pack8<H>(y);
+  for (int i0 = part * HPW; i0 < a.Hq; i0 += kQueries * split * HPW) {
+    u32x4 x[kQueries];
+#pragma unroll
+    for (int k = 0; k < kQueries; ++k) {  // (heads past the last: it again)
+      const int h = min(i0 + k * split * HPW + lane / LPH, a.Hq - 1);
+      x[k] = *(const u32x4*)(a.q + t * a.q_stride + h * D + e0);
+    }
+#pragma unroll
+    for (int k = 0; k < kQueries; ++k) {
+      const int h = i0 + k * split * HPW + lane / LPH;
+      if (i0 + k * split * HPW >= a.Hq) break;
+      float y[8];
+      unpack8<H>(x[k], y);
+      if (a.q_norm) norm_head<D, H>(y, a.q_norm, a.eps, e0);
+      if (a.rope) turn_head<D>(a, y, turn, e0, turns);
+      if (h < a.Hq) *(u32x4*)(a.q_out + t * a.q_out_stride + h * D + e0) = pack8<H>(y);
+    }
   }
 }
+
+// How the waves of a workgroup share blocks of G slots of one head: `waves` of them to a
+// block, `steps` loads of 512 / D rows each.  (A wave by itself took 31 us for the keys and
+// values of 8000 rows in blocks of 32, and the registers of eight steps left three waves a
+// SIMD.)
+template <int D, int G>
+struct Share {
+  static constexpr int rows = 512 / D;
+  static constexpr int waves = G / rows < kWaves ? G / rows : kWaves;
+  static constexpr int steps = G / rows / waves;
+  static constexpr int heads = kWaves / waves;
+};
 
 // The n new rows t .. of a block of G slots, the first at offset o0 (slots below it hold
-// rows from before), of one head of the keys or the values: the rows stay in registers
-// between their largest magnitude and their rounding.
+// rows from before), of one head of the keys or the values, by wave `part` of those that
+// share it: the rows stay in registers between their largest magnitude, which the waves
+// join in `most`, and their rounding.  Without `live` the wave only keeps the others'
+// company at the barrier.
 template <int D, bool H, int G>
-__device__ __forceinline__ void append_block(const AppendArgs& a, bool keys, int h, int t, int n,
-                                             int o0, int slot0, uint8_t* block, uint8_t* scale) {
-  constexpr int LPH = D / 8, RPS = 64 / LPH, STEPS = G / RPS;  // lanes of a row, rows of a step
-  const int lane = threadIdx.x & 63, e0 = (lane % LPH) * 8, sub = lane / LPH;
-  const uint16_t* src = (keys ? a.k : a.v) + h * D + e0;
-  const long long stride = keys ? a.k_stride : a.v_stride;
-  u32x4 x[STEPS];
-#pragma unroll
-  for (int s = 0; s < STEPS; ++s)
-    x[s] = *(const u32x4*)(src + (t + min(max(s * RPS + sub - o0, 0), n - 1)) * stride);
-  const int was = o0 > 0 ? scale_in(*scale) : 0;
+__device__ __forceinline__ void append_block(const AppendArgs& a, bool live, bool keys, int h, int t,
+                                             int n, int o0, int slot0, uint8_t* block,
+                                             uint8_t* scale, int part, float* most) {
+  using S = Share<D, G>;
+  constexpr int LPH = D / 8;
+  const int lane = threadIdx.x & 63, e0 = (lane % LPH) * 8;
+  const int j0 = part * S::steps * S::rows + lane / LPH;  // the lane's first slot of the block
+  const bool any = live && j0 - lane / LPH < o0 + n && j0 - lane / LPH + S::steps * S::rows > o0;
   const bool turns = keys && a.rope && e0 < a.rot;
-  float y[STEPS][8];
-  float most = 0.0f;
+  float y[S::steps][8];
+  int was = 0;
+  float large = 0.0f;
+  if (any) {  // (the same in every lane; lanes beside the rows repeat one of them)
+    const uint16_t* src = (keys ? a.k : a.v) + h * D + e0;
+    const long long stride = keys ? a.k_stride : a.v_stride;
+    u32x4 x[S::steps];
+    int pos[S::steps];
 #pragma unroll
-  for (int s = 0; s < STEPS; ++s) {
-    if ((s + 1) * RPS <= o0 || s * RPS >= o0 + n) continue;  // (no new row: the same in every lane)
-    const int i = min(max(s * RPS + sub - o0, 0), n - 1);
-    unpack8<H>(x[s], y[s]);
-    if (keys) {
-      if (a.k_norm) norm_head<D, H>(y[s], a.k_norm, a.eps, e0);
-      if (a.rope) {
-        Turn turn;
-        if (turns) load_turn(a, a.position ? a.position[t + i] : slot0 + i, e0, turn);
-        turn_head<D>(a, y[s], turn, e0, turns);
+    for (int s = 0; s < S::steps; ++s) {
+      const int i = min(max(j0 + s * S::rows - o0, 0), n - 1);
+      x[s] = *(const u32x4*)(src + (t + i) * stride);
+      pos[s] = turns && a.position ? a.position[t + i] : slot0 + i;
+    }
+#pragma unroll
+    for (int s = 0; s < S::steps; ++s) {
+      Turn turn;
+      if (turns) load_turn(a, pos[s], e0, turn);
+      unpack8<H>(x[s], y[s]);
+      if (keys && a.k_norm) norm_head<D, H>(y[s], a.k_norm, a.eps, e0);
+      if (keys && a.rope) turn_head<D>(a, y[s], turn, e0, turns);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float m = fabsf(y[s][e]);
+        large = m < __builtin_inff() ? fmaxf(large, m) : large;
       }
     }
-    // (lanes past the rows repeat one of them)
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const float m = fabsf(y[s][e]);
-      most = m < __builtin_inff() ? fmaxf(most, m) : most;
-    }
+    large = wave_max(large);
   }
-  const int now = max(scale_of(wave_max(most)), was);
-  const float down = scale_down(now);
+  if (live && o0 > 0) was = scale_in(*scale);
+  if constexpr (S::waves > 1) {
+    const int first = threadIdx.x / 64 - part;
+    if (lane == 0) most[first + part] = large;
+    __syncthreads();
 #pragma unroll
-  for (int s = 0; s < STEPS; ++s) {
-    const int j = s * RPS + sub;
-    if (j < o0 || j >= o0 + n) continue;
+    for (int w = 0; w < S::waves; ++w) large = fmaxf(large, most[first + w]);
+  }
+  if (!live) return;
+  const int now = max(scale_of(large), was);
+  if (any) {
+    const float down = scale_down(now);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) y[s][e] *= down;
-    *(uint2*)(block + j * D + e0) = hold8(y[s]);
+    for (int s = 0; s < S::steps; ++s) {
+      const int j = j0 + s * S::rows;
+      if (j < o0 || j >= o0 + n) continue;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) y[s][e] *= down;
+      *(uint2*)(block + j * D + e0) = hold8(y[s]);
+    }
   }
   if (now == was) return;
-  if (o0 > 0) {  // the rows from before under the grown scale
-    const float f = scale_up(127 - min(now - was, 126));
-    for (int j = sub; j < o0; j += RPS) {
-      uint2* p = (uint2*)(block + j * D + e0);
-      uint2 w = *p;
-      w.x = rescale4(w.x, f);
-      w.y = rescale4(w.y, f);
-      *p = w;
-    }
+  const float f = scale_up(127 - min(now - was, 126));
+  for (int j = part * S::rows + lane / LPH; j < o0; j += S::waves * S::rows) {
+    uint2* p = (uint2*)(block + j * D + e0);  // the rows from before under the grown scale
+    uint2 w = *p;
+    w.x = rescale4(w.x, f);
+    w.y = rescale4(w.y, f);
+    *p = w;
   }
-  if (lane == 0) *scale = (uint8_t)now;
+  if (part == 0 && lane == 0) *scale = (uint8_t)now;
 }
 
-// Waves of queries first (qwaves of them, qsplit a row), then of keys and values: each
-// takes one head of one of them and, of `window` rows, the blocks whose first new row is
-// among these.
+// Workgroups of keys and values first, whose chains are long (reversed, 8000 rows take 51
+// us for 48): each takes Share's heads of one or both and, of `window` rows, the blocks
+// whose first new row is among these.  Then qblocks of queries, qsplit waves a row.  Bytes
+// bound them (8000 rows of 32 and 8 heads of 128, 182 MB: 48 us, 3.8 TB/s).
 template <int D, bool H, int G>
 __global__ __launch_bounds__(kThreads) void append8_kernel(AppendArgs a, HeldScales sc, int qblocks,
                                                           int qsplit, int window) {
+  using S = Share<D, G>;
+  __shared__ float most[2][kWaves];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-  if ((int)blockIdx.x < qblocks) {
-    const int w = blockIdx.x * kWaves + wave;
+  const int kvblocks = gridDim.x - qblocks;
+  if ((int)blockIdx.x >= kvblocks) {
+    const int w = (blockIdx.x - kvblocks) * kWaves + wave;
     if (w / qsplit < a.b.T) append_queries<D, H>(a, w / qsplit, w % qsplit, qsplit);
     return;
   }
-  const long long w = (long long)(blockIdx.x - qblocks) * kWaves + wave;
-  const int item = (int)(w % (2 * a.Hkv)), h = item % a.Hkv;
-  const bool keys = item < a.Hkv;
-  const long long t0 = w / (2 * a.Hkv) * window;
-  if (t0 >= a.b.T) return;
-  const int end = min((int)t0 + window, a.b.T);
+  const int groups = (2 * a.Hkv + S::heads - 1) / S::heads;  // of heads
+  const int b = blockIdx.x;
+  const int item = b % groups * S::heads + wave / S::waves, h = item % a.Hkv;
+  const bool keys = item < a.Hkv, live = item < 2 * a.Hkv;
+  const int t0 = b / groups * window, end = min(t0 + window, a.b.T);
   const int blocks = 1 << (a.b.page_shift - sc.block_shift);  // of a page
-  for (int t = (int)t0; t < end;) {
+  int turn = 0;
+  for (int t = t0; t < end;) {  // (the same in every wave)
     const int r = request_of_row(a.b, t);
     if (r < 0) {
       ++t;
@@ -148,7 +189,8 @@ __global__ __launch_bounds__(kThreads) void append8_kernel(AppendArgs a, HeldSca
                          (size_t)(off - o0) * D;
         uint8_t* scale = (keys ? sc.k : sc.v) + (size_t)page * sc.stride + (size_t)h * blocks +
                          (off >> sc.block_shift);
-        append_block<D, H, G>(a, keys, h, t, n, o0, slot, block, scale);
+        append_block<D, H, G>(a, live, keys, h, t, n, o0, slot, block, scale, wave % S::waves,
+                              most[turn ^= 1]);
       }
     }
     t += n;
@@ -157,7 +199,8 @@ __global__ __launch_bounds__(kThreads) void append8_kernel(AppendArgs a, HeldSca
 
 template <int D, bool H, int G>
 hipError_t append(const AppendArgs& a, const HeldScales& s, hipStream_t stream) {
-  const int T = a.b.T;
+  using S = Share<D, G>;
+  const int T = a.b.T, groups = (2 * a.Hkv + S::heads - 1) / S::heads;
   int qsplit = 1;
   long long qblocks = 0;
   if (a.q) {
@@ -165,11 +208,10 @@ hipError_t append(const AppendArgs& a, const HeldScales& s, hipStream_t stream) 
     qsplit = std::max(1, std::min(units, 8192 / T));
     qblocks = ((long long)T * qsplit + kWaves - 1) / kWaves;
   }
-  const int window = (long long)T * 2 * a.Hkv <= 16384 ? 1 : G;
-  const long long waves = (long long)((T + window - 1) / window) * 2 * a.Hkv;
-  const long long blocks = qblocks + (waves + kWaves - 1) / kWaves;
+  const int window = (long long)T * groups <= 8192 ? 1 : G;
+  const long long blocks = qblocks + (long long)((T + window - 1) / window) * groups;
   append8_kernel<D, H, G><<<(unsigned)blocks, kThreads, 0, stream>>>(a, s, (int)qblocks, qsplit,
-                                                                        window);
+                                                                    window);
   return hipGetLastError();
 }
 

@@ -298,7 +298,8 @@ pctree_status pctree_append_paged8(const pctree_paged_cache8* cache,
     AppendArgs a;
     st = check_append(pages, rows, &a);
     if (st != PCTREE_OK) return st;
-    // a wave for every head of keys and of values at every row, at most
+    // (a workgroup for every head of keys and of values at every eighth row, at most, and for
+    // four rows' queries)
     if ((int64_t)batch->rows * pages->kv_heads > kMaxGrid) return PCTREE_ERR_UNSUPPORTED;
     a.b = rows_of(pages, batch, 16);
     (void)hipGetLastError();
