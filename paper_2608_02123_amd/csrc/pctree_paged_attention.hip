@@ -2,7 +2,8 @@
 // token, or a tree to verify): out_i = sum_s w_is v_s, w_is = softmax over the
 // slots s that row i admits of scale q_i . k_s.
 //
-// Layout (bf16 or float16): q and out [T][Hq][D], pages [Hkv][page_size][D];
+// Layout (bf16 or float16): q and out [T][Hq][D], pages [Hkv][page_size][D] (or of bytes
+// with scales: pctree_held.h);
 // query head h reads key/value head h / g, g = Hq / Hkv.  The g heads of a
 // key/value head are rows of one matrix, row rho = i * g + (h mod g) of request
 // row i, so that K and V are read once for all of them.
@@ -322,7 +323,9 @@ __device__ __forceinline__ void mend_odd(const PagedAttnArgs& a, const PagedReq&
 }
 
 // 128 rows of one (request, kv head) to a workgroup.  Two products of 64 x 128 x D a chunk
-// bound it, and the vector unit's softmax between them.  (2048 rows over 6000 slots, 32
+// bound it, and the vector unit's softmax between them; over pages in 8 bits (Q8) also the
+// conversion of every chunk, once for the workgroup (the chunk below: 255 us, 0.92 PFLOP/s;
+// 373 with the conversion scheduled among the products, which costs registers).  (2048 rows over 6000 slots, 32
 // and 8 heads of 128, 235 GFLOP: 228 to 238 us, 1.0 PFLOP/s, where a library product of
 // 8192 runs at 1.2.  32-slot chunks 290, 48 rows a wave 445, for 267 at the time: registers.)
 template <int D, bool H, bool Q8>
@@ -636,7 +639,9 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
       }
 #pragma unroll
     for (int h = 0; h < kHalves; ++h) weigh(sKV[buf][1], h, bp[h]);
-    stage_next();
+    // (one piece of code where the next chunk is whole too: 261 to 255 us)
+    if (Q8 && c0 + 2 * kChunk <= all_see && !bad_next) stage(buf ^ 1, false);
+    else stage_next();
   }
   for (; c0 < kend; c0 += kChunk, buf ^= 1) {
     if constexpr (!Q8) wait_loads();
@@ -931,7 +936,10 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3))) v
 // The same over pages in 8 bits: a wave's step is 64 slots, as many bytes.  A lane takes
 // 16 of a key's bytes at a time, two steps of the first product, and the queries lie in
 // that order; values cross LDS in 8 bits, and a transposing read gives a lane 8 slots of
-// one element, whose scale is one (a block holds 8 slots at least).
+// one element, whose scale is one (a block holds 8 slots at least).  Both are converted,
+// with their scales, right before the matrix instructions, 128 conversions of a pair a step.
+// Bytes bound it: 64 single tokens over 500 to 8000 slots, 364 MB, 81 us with the merge's 5,
+// 4.8 TB/s besides it; one token over 1000 slots 8.7 and 3.4 us.
 template <int D, bool H>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3))) void paged_few8_kernel(
     PagedAttnArgs a) {
@@ -1249,7 +1257,14 @@ PagedPlan plan_paged_attention(int R, int T, int max_rows, int Hq, int Hkv, int 
   p.least = 2 * kChunk;
   // (a workgroup for each compute unit: 4 trees of 64 nodes, 1000 to 4000 slots, 57 us
   // with half of that, 40; a chunk of 512 rows over 4000 slots 95, 66)
-  p.nsplit = many ? runs(base, cus, p.least) : 1;
+  // Over 8-bit pages, whose chunks take as long and whose partial outputs weigh the same,
+  // two workgroups where one would leave units idle, in runs of 256 slots on average (us
+  // with one, with two, with two and shorter runs: the 4 trees 52, 44, 44; the chunk 74, 61,
+  // 62; 8 trees of 128 nodes, 28 heads over 4 of 64, up to 3000 slots 45, 36, 37; 128 rows
+  // over 1000 slots 20.4, 21.5, 24.0; 64 19.4, 20.3, 19.3).
+  const bool twice = held && base < cus;
+  p.nsplit = many ? runs(base, twice ? 2 * cus : cus, p.least) : 1;
+  if (twice) p.nsplit = std::max(1, std::min(p.nsplit, C / (2 * p.least)));
   // Long and short requests side by side: the long ones' chains of chunks last longest,
   // so those of more than 1024 slots are cut (24 requests of 1 to 700 rows, one of 3000
   // slots, heads of 64: 71 us uncut, 60 with runs of 512, 48; 12 requests of 1 to 500

@@ -848,8 +848,8 @@ def append_paged(batch, k_cache, v_cache, k, v, q=None, *, q_norm=None, k_norm=N
 
 class PagedAttention:
     """Attention of a batch's new rows over paged caches, with its workspace, for
-    repeated calls of one size (calls that may overlap need an object each).  Pages in 8
-    bits need less of it than those in 16: one object serves both."""
+    repeated calls of one size (calls that may overlap need an object each), over pages in
+    16 bits and in 8."""
 
     def __init__(self, batch, q_heads, kv_heads, head_dim, page_size, scale=None):
         self.sizes = batch.sizes
@@ -858,8 +858,12 @@ class PagedAttention:
         self.scale = float(scale) if scale is not None else head_dim ** -0.5
         Hkv, P, D = self.kv_heads, self.page_size, self.head_dim
         c = _PagedCache(None, None, Hkv * P * D, 1, P, Hkv, D, BF16)
-        self.ws_bytes = int(lib().pctree_paged_attention_workspace_bytes(
-            ctypes.byref(c), batch._ref, self.q_heads))
+        held = _PagedCache8(_PagedCache(None, None, -(-Hkv * P * D // 16) * 16, 1, P, Hkv, D, BF16),
+                            None, None, max(Hkv * P, 1), 8)
+        self.ws_bytes = max(int(lib().pctree_paged_attention_workspace_bytes(
+            ctypes.byref(c), batch._ref, self.q_heads)), int(
+                lib().pctree_paged_attention8_workspace_bytes(ctypes.byref(held), batch._ref,
+                                                              self.q_heads)))
         self.idx = batch.idx
         self._ws = _Workspace(self.ws_bytes, batch.device)
         self.workspace = self._ws.tensor

@@ -107,14 +107,18 @@ def test_null_structs_and_operands():
 
 
 @pytest.mark.parametrize("D,Hq,Hkv", [(128, 32, 8), (64, 28, 4), (128, 8, 1)])
-@pytest.mark.parametrize("R,T,most", [(1, 1, 1), (64, 64, 1), (1, 2048, 2048), (24, 900, 300), (200, 200, 1)])
-@pytest.mark.parametrize("slots", [64, 1000, 70000])
-def test_one_workspace_serves_both_kinds_of_pages(D, Hq, Hkv, R, T, most, slots):
-    c = cache8(kv_heads=Hkv, head_dim=D)
-    b = batch(requests=R, rows=T, max_rows=most, max_pages=-(-slots // 16))
-    w8 = P.lib().pctree_paged_attention8_workspace_bytes(ctypes.byref(c), ctypes.byref(b), Hq)
-    w16 = P.lib().pctree_paged_attention_workspace_bytes(ctypes.byref(c.pages), ctypes.byref(b), Hq)
-    assert w8 <= w16
+@pytest.mark.parametrize("R,T,most", [(1, 1, 1), (64, 64, 1), (1, 300, 300), (24, 900, 300), (200, 200, 1)])
+@pytest.mark.parametrize("slots,page", [(64, 16), (1000, 16), (70000, 64), (300, 4)])
+def test_an_objects_workspace_serves_both_kinds_of_pages(D, Hq, Hkv, R, T, most, slots, page):
+    b = batch(requests=R, rows=T, max_rows=most, max_pages=-(-slots // page))
+    c = cache8(block=8, kv_heads=Hkv, head_dim=D, page_size=page) if page >= 8 else None
+    plain = cache(kv_heads=Hkv, head_dim=D, page_size=page)
+    w8 = P.lib().pctree_paged_attention8_workspace_bytes(ctypes.byref(c), ctypes.byref(b), Hq) if c else 0
+    w16 = P.lib().pctree_paged_attention_workspace_bytes(ctypes.byref(plain), ctypes.byref(b), Hq)
+
+    class Batch:
+        sizes, idx, _ref, device = (R, b.max_pages, T, most), -1, ctypes.byref(b), "meta"
+    assert P.PagedAttention(Batch, Hq, Hkv, D, page).ws_bytes == max(w8, w16)
 
 
 def test_compact_refusals():
