@@ -208,15 +208,98 @@ hipError_t append(const AppendArgs& a, const HeldScales& s, hipStream_t stream) 
     qsplit = std::max(1, std::min(units, 8192 / T));
     qblocks = ((long long)T * qsplit + kWaves - 1) / kWaves;
   }
-  const int window = (long long)T * groups <= 8192 ? 1 : G;
+  const int window = (long long)T * groups <= 4096 ? 1 : G;
   const long long blocks = qblocks + (long long)((T + window - 1) / window) * groups;
   append8_kernel<D, H, G><<<(unsigned)blocks, kThreads, 0, stream>>>(a, s, (int)qblocks, qsplit,
                                                                     window);
   return hipGetLastError();
 }
 
+// Requests of one row each (single tokens): the row's heads of queries, keys and values 512 /
+// D at a time, `split` waves a row; a head's scale is that of its one row and, where slots
+// from before lie in the block, of these.  (A call of 500 such rows 25 us with a
+// workgroup to every head, 16 so, which is the host's.)
+template <int D, bool H>
+__global__ __launch_bounds__(kThreads) void append8_single_kernel(AppendArgs a, HeldScales sc,
+                                                                 int split) {
+  constexpr int LPH = D / 8, HPW = 64 / LPH;  // lanes of a head, heads of a wave
+  const int lane = threadIdx.x & 63, e0 = (lane % LPH) * 8;
+  const int wave = __builtin_amdgcn_readfirstlane(blockIdx.x * kWaves + threadIdx.x / 64);
+  const int t = wave / split, part = wave % split;
+  if (t >= a.b.T) return;
+  const int r = request_of_row(a.b, t);
+  if (r < 0) return;
+  const PagedReq rq = paged_req(a.b, r);
+  const int slot = rq.prefix + (t - rq.start);
+  int page = slot < a.b.C ? a.b.page_table[(size_t)r * a.b.max_pages + (slot >> a.b.page_shift)] : -1;
+  if ((unsigned)page >= (unsigned)a.b.pages) page = -1;
+  const int off = slot & ((1 << a.b.page_shift) - 1), o0 = off & ((1 << sc.block_shift) - 1);
+  const int blocks = 1 << (a.b.page_shift - sc.block_shift);  // of a page
+  const bool turns = a.rope && e0 < a.rot;
+  Turn turn;
+  if (turns) load_turn(a, a.position ? a.position[t] : slot, e0, turn);
+  const int qn = a.q ? a.Hq : 0, items = qn + 2 * a.Hkv;
+  for (int i0 = part * HPW; i0 < items; i0 += split * HPW) {
+    const int it = i0 + lane / LPH;
+    const int kind = it < qn ? 0 : (it < qn + a.Hkv ? 1 : (it < items ? 2 : 3));
+    const int h = kind == 0 ? it : (kind == 1 ? it - qn : it - qn - a.Hkv);
+    const uint16_t* src = kind == 0   ? a.q + t * a.q_stride + h * D
+                          : kind == 1 ? a.k + t * a.k_stride + h * D
+                                      : a.v + t * a.v_stride + h * D;
+    const bool held = (kind == 1 || kind == 2) && page >= 0;
+    u32x4 x = {0u, 0u, 0u, 0u};
+    if (kind == 0 || held) x = *(const u32x4*)(src + e0);
+    uint8_t* scale = (kind == 1 ? sc.k : sc.v);
+    int was = 0;
+    if (held) {
+      scale += (size_t)page * sc.stride + (size_t)h * blocks + (off >> sc.block_shift);
+      if (o0 > 0) was = scale_in(*scale);
+    }
+    float y[8];
+    unpack8<H>(x, y);
+    norm_head<D, H>(y, kind == 0 ? a.q_norm : (kind == 1 ? a.k_norm : nullptr), a.eps, e0);
+    if (a.rope) turn_head<D>(a, y, turn, e0, turns && kind < 2);
+    float large = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float m = fabsf(y[e]);
+      large = m < __builtin_inff() ? fmaxf(large, m) : large;
+    }
+#pragma unroll
+    for (int o = 1; o < LPH; o <<= 1) large = fmaxf(large, __shfl_xor(large, o, 64));
+    if (kind == 0) *(u32x4*)(a.q_out + t * a.q_out_stride + h * D + e0) = pack8<H>(y);
+    if (!held) continue;
+    const int now = max(scale_of(large), was);
+    uint8_t* at = (uint8_t*)(kind == 1 ? a.k_pages : a.v_pages) +
+                  ((size_t)page * a.b.page_units + (size_t)h * a.b.head_units) * 16 +
+                  (size_t)(off - o0) * D + e0;
+    const float down = scale_down(now);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) y[e] *= down;
+    *(uint2*)(at + o0 * D) = hold8(y);
+    if (now == was) continue;
+    const float f = scale_up(127 - min(now - was, 126));
+    for (int j = 0; j < o0; ++j) {  // the rows from before under the grown scale
+      uint2* p = (uint2*)(at + j * D);
+      uint2 w = *p;
+      w.x = rescale4(w.x, f);
+      w.y = rescale4(w.y, f);
+      *p = w;
+    }
+    if (e0 == 0) *scale = (uint8_t)now;
+  }
+}
+
 template <int D, bool H>
 hipError_t append_blocks(const AppendArgs& a, const HeldScales& s, hipStream_t stream) {
+  if (a.b.max_rows == 1) {
+    const int units = ((a.q ? a.Hq : 0) + 2 * a.Hkv + 512 / D - 1) / (512 / D);
+    const int split = std::max(1, std::min(units, 8192 / a.b.T));
+    const long long waves = (long long)a.b.T * split;
+    append8_single_kernel<D, H>
+        <<<(unsigned)((waves + kWaves - 1) / kWaves), kThreads, 0, stream>>>(a, s, split);
+    return hipGetLastError();
+  }
   switch (1 << s.block_shift) {
     case 8: return append<D, H, 8>(a, s, stream);
     case 16: return append<D, H, 16>(a, s, stream);

@@ -402,6 +402,27 @@ def test_append_of_many_requests_one_row_each():
     run_append(b, 2, 2, 64, 16, 16, torch.float16)
 
 
+@pytest.mark.parametrize("dt", DTYPES)
+@pytest.mark.parametrize("D,Hq,Hkv", [(64, 3, 1), (128, 32, 8), (128, 5, 3)])
+@pytest.mark.parametrize("page,block", [(8, 8), (64, 16), (64, 64)])
+def test_append_of_single_tokens(dt, D, Hq, Hkv, page, block):
+    """Every place of a block, scales that stay and grow, requests without a row or a page."""
+    rng = np.random.default_rng((D, page, block))
+    prefix = np.concatenate([np.arange(block + 1), [200, 5, 77]])
+    b = make_batch(rng, [1] * len(prefix), prefix, page, gap=1)
+    b["row_count"][2], b["page_table"][5, 0] = 0, -1
+    amp = np.exp(rng.standard_normal(b["rows"]) * 4)
+    run_append(b, Hq, Hkv, D, page, block, dt, amplitude=np.clip(amp, 0, 3000), norm=bool(block % 64))
+
+
+def test_append_of_a_single_token_with_infinities():
+    b = make_batch(np.random.default_rng(3), [1, 1, 1], [5, 16, 0], 16)
+
+    def spoil(qkv):
+        qkv[0, 130], qkv[1, -3], qkv[2] = float("inf"), float("nan"), 0.0
+    run_append(b, 1, 2, 128, 16, 16, torch.bfloat16, norm=False, rope=False, spoil=spoil)
+
+
 def test_append_without_queries_and_slots_that_do_not_exist():
     """Rows past the table's end or on no page leave every byte as it was."""
     rng = np.random.default_rng(12)
