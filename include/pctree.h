@@ -512,8 +512,9 @@ pctree_status pctree_paged_attention8(const pctree_paged_cache8* cache,
  * [heads][page_size / block] bytes, group g's page p at byte g * scale_group_stride +
  * p * scale_page_stride.  A block that takes accepted rows gets the largest of their
  * scales and, where slots below prefix_len lie in it, of its own; rows and those slots
- * are held again where their scale was smaller.  A request whose accepted nodes all
- * stay in place is left untouched. */
+ * are held again where their scale was smaller.  Other slots of such a block stand for
+ * nothing.  A request whose accepted nodes all stay in place is left untouched.  A block
+ * that takes accepted rows belongs to one request. */
 pctree_status pctree_compact_paged8(void* pool, int64_t group_stride, int64_t page_stride,
                                     uint8_t* scale, int64_t scale_group_stride,
                                     int64_t scale_page_stride, int32_t groups, int32_t pages,
@@ -530,7 +531,8 @@ pctree_status pctree_compact_paged8(void* pool, int64_t group_stride, int64_t pa
  * max |y| / 448 over each `group` elements of the row (the last group may be
  * shorter), in scale (infinite and NaN elements do not count and are held as NaN;
  * a group of zeros has scale 0).  float32 throughout, each output rounded once; v
- * is not rounded before it is normed.
+ * is not rounded before it is normed.  (Where a row's sum of squares passes float32's
+ * range, its finite elements give 0.)
  * --------------------------------------------------------------------- */
 #define PCTREE_MAX_NORM_WIDTH 32768
 

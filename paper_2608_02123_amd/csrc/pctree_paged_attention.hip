@@ -322,9 +322,17 @@ __device__ __forceinline__ void mend_odd(const PagedAttnArgs& a, const PagedReq&
   }
 }
 
+// Where unit u of row `row` lies in a chunk that was converted (a further step on k_unit and
+// v_unit, the same for every row of a fragment's read): lanes write every second unit of a
+// row, and eight lanes' writes meet all banks only if half of them take the odd places.
+template <int D, bool Q8>
+__device__ __forceinline__ int staged(int u, int row) {
+  return !Q8 ? 0 : D == 128 ? (u >> 3) & 1 : row & 1;
+}
+
 // 128 rows of one (request, kv head) to a workgroup.  Two products of 64 x 128 x D a chunk
 // bound it, and the vector unit's softmax between them; over pages in 8 bits (Q8) also the
-// conversion of every chunk, once for the workgroup (the chunk below: 255 us, 0.92 PFLOP/s;
+// conversion of every chunk, once for the workgroup (the chunk below: 252 us, 0.93 PFLOP/s;
 // 373 with the conversion scheduled among the products, which costs registers).  (2048 rows over 6000 slots, 32
 // and 8 heads of 128, 235 GFLOP: 228 to 238 us, 1.0 PFLOP/s, where a library product of
 // 8192 runs at 1.2.  32-slot chunks 290, 48 rows a wave 445, for 267 at the time: registers.)
@@ -472,7 +480,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
       const float kf = scale_up(scale_in(ks[i])), vf = scale_up(scale_in(vs[i]));
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
-        *(u32x4*)(&sKV[buf][0][row * D + ((u + b) ^ k_unit<D>(row)) * 8]) =
+        *(u32x4*)(&sKV[buf][0][row * D + ((u + b) ^ k_unit<D>(row) ^ staged<D, Q8>(u, row)) * 8]) =
             held8<H>(kx[i][2 * b], kx[i][2 * b + 1], kf);
         u32x4 w = held8<H>(vx[i][2 * b], vx[i][2 * b + 1], vf);
         if (part) {
@@ -483,7 +491,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
             w[e] = f;
           }
         }
-        *(u32x4*)(&sKV[buf][1][row * D + ((u + b) ^ v_unit<D>(row)) * 8]) = w;
+        *(u32x4*)(&sKV[buf][1][row * D + ((u + b) ^ v_unit<D>(row) ^ staged<D, Q8>(u, row)) * 8]) = w;
       }
     }
     if (odd) sOdd = 1;
@@ -529,7 +537,9 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
     for (int k = 0; k < KS; ++k) {
 #pragma unroll
       for (int h = 0; h < kHalves; ++h) {
-        const uint16_t* kr = sK + (32 * h + krow0) * D + ((4 * k + grp) ^ k_unit<D>(krow0)) * 8;
+        const int u = 4 * k + grp;
+        const uint16_t* kr =
+            sK + (32 * h + krow0) * D + (u ^ k_unit<D>(krow0) ^ staged<D, Q8>(4 * k, krow0)) * 8;
         const u32x4 a0 = *(const u32x4*)kr;
         const u32x4 a1 = *(const u32x4*)(kr + 4 * D);
 #pragma unroll
@@ -553,8 +563,8 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
   auto weigh = [&](const uint16_t* sV, int h, const u32x4 (&bp)[CT]) __attribute__((always_inline)) {
 #pragma unroll
     for (int t = 0; t < DT; ++t) {
-      const uint16_t* vr = sV + (32 * h + vkey) * D +
-                           ((2 * t + ((col >> 1) & 1)) ^ v_unit<D>(vkey)) * 8 + (col & 1) * 4;
+      const int u = (2 * t + ((col >> 1) & 1)) ^ v_unit<D>(vkey) ^ staged<D, Q8>(2 * t, vkey);
+      const uint16_t* vr = sV + (32 * h + vkey) * D + u * 8 + (col & 1) * 4;
       const u32x2 lo = read_tr(vr), hi = read_tr(vr + 4 * D);
       const u32x4 av = {lo[0], lo[1], hi[0], hi[1]};
 #pragma unroll

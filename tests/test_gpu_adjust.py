@@ -178,6 +178,25 @@ def test_ranges_past_the_lists_are_clamped():
     check(logits, a)
 
 
+def test_nan_stays_and_what_no_row_holds_keeps_its_bits():
+    """A NaN logit of a token that only another branch of the tree holds keeps its payload; one
+    that is penalised stays NaN; a forbidden one becomes -inf."""
+    x = torch.zeros(3, 100, dtype=torch.int16, device="cuda")
+    x[:, 7], x[:, 9], x[:, 50] = 0x7f91, 0x7fa5, 0x7fc1
+    x = x.view(torch.bfloat16)
+    before = x.clone()
+    allowed = np.full((1, 4), -1, np.int32)
+    allowed[0, 1] = ~(1 << 18)  # token 50
+    a = {"row_start": np.zeros(1, np.int32), "row_count": np.array([3], np.int32),
+         "token": np.array([[1, 7, 9]], np.int32), "mask": np.array([[[1], [3], [5]]], np.int32),
+         "presence": np.ones(1, np.float32), "allowed": allowed, "allowed_row": np.zeros(3, np.int32)}
+    P.adjust_logits(x, up(a["row_start"]), up(a["row_count"]), **{k: up(v) for k, v in a.items() if k[:3] != "row"})
+    assert (x[:, 50] == -np.inf).all() and (x[:, 1] == -1).all()
+    bits, was = x.view(torch.int16), before.view(torch.int16)
+    assert bits[0, 7] == was[0, 7] and bits[2, 7] == was[2, 7] and bits[0, 9] == was[0, 9] and bits[1, 9] == was[1, 9]
+    assert torch.isnan(x[1, 7]) and torch.isnan(x[2, 9])
+
+
 def test_empty_lists():
     x = torch.randn(2, 300, generator=torch.Generator().manual_seed(0)).cuda()
     before, e = x.clone(), torch.zeros(0, dtype=torch.int32, device="cuda")
