@@ -617,10 +617,10 @@ class _Here:
     """The calls' device and stream: device ``idx`` (an int, which is compared in a
     tenth of a device object's time), and its current stream or the one that is passed
     (what a call allocates is then that stream's)."""
-    __slots__ = ("ctx",)
+    __slots__ = ("ctx", "idx")
 
     def __init__(self, idx, stream):
-        self.ctx = None
+        self.ctx, self.idx = None, idx
         if stream is not None:
             if stream.device.index != idx:
                 raise ValueError(f"the stream is one of {stream.device}, the tensors of cuda:{idx}")
@@ -631,7 +631,7 @@ class _Here:
     def __enter__(self):
         if self.ctx is not None:
             self.ctx.__enter__()
-        return _stream()
+        return _stream() if _raw_stream is None else _raw_stream(self.idx)
 
     def __exit__(self, *exc):
         if self.ctx is not None:
@@ -834,7 +834,7 @@ def append_paged(batch, k_cache, v_cache, k, v, q=None, *, q_norm=None, k_norm=N
         if q is not None:
             qs, Hq = _row_tensor("q", q, T, D, dt, idx)
             if q_out is None:
-                q_out = torch.empty((T, Hq, D), dtype=dt, device=q.device)
+                q_out = q.new_empty((T, Hq, D))
             os_, oh = _row_tensor("q_out", q_out, T, D, dt, idx)
             if oh != Hq:
                 raise ValueError("q_out must have q's shape")

@@ -208,6 +208,28 @@ def test_empty_lists():
     assert torch.equal(x, before)
 
 
+def test_logits_past_32_bits():
+    """Rows whose offsets pass 2^32 bytes, one of them with a mask."""
+    V, T = 151936, 15000  # 4.6 GB
+    x = torch.zeros(T, V, dtype=torch.bfloat16, device="cuda")
+    rows = torch.tensor([T - 2, 0], dtype=torch.int32, device="cuda")
+    count = torch.tensor([2, 1], dtype=torch.int32, device="cuda")
+    tokens = torch.tensor([5, V - 1, V - 1, 70000], dtype=torch.int32, device="cuda")
+    allowed = torch.full((1, (V + 31) // 32), -1, dtype=torch.int32, device="cuda")
+    allowed[0, 1] = 0  # tokens 32 to 63
+    which = torch.full((T,), -1, dtype=torch.int32, device="cuda")
+    which[T - 1] = 0
+    ones = torch.ones(2, device="cuda")
+    P.adjust_logits(x, rows, count, max_rows=2, history=tokens, history_start=up(np.array([0, 3], np.int32)),
+                    history_count=up(np.array([3, 1], np.int32)), frequency=ones, allowed=allowed, allowed_row=which)
+    assert x[T - 2, 5] == -1 and x[T - 1, V - 1] == -2 and x[0, 70000] == -1 and x[0, 5] == 0
+    assert (x[T - 1, 32:64] == -np.inf).all() and (x[T - 2, 32:64] == 0).all() and x[T - 1, 64] == 0
+    x[T - 2:, 5] = x[T - 2:, V - 1] = x[0, 70000] = 0
+    x[T - 1, 32:64] = 0
+    assert int(torch.count_nonzero(x.view(torch.int16).view(-1, V)[::100]).item()) == 0
+    assert not x[T - 3:].view(torch.int32).any()
+
+
 def test_refusals():
     x = torch.zeros(2, 100, device="cuda")
     i = torch.zeros(2, dtype=torch.int32, device="cuda")

@@ -498,6 +498,25 @@ def test_compact_paths():
         run_compact(rng, 0, 70, 64, 32, block, 2, 3, 128, 0, paths=paths, prefix=[3, 13, 0, 7, 5, 30, 16])
 
 
+def test_compact_past_32_bits():
+    """A pool whose second group lies 5 GiB behind the first, pages between."""
+    rng = np.random.default_rng(21)
+    b = make_batch(rng, [20], [11], 16)
+    raw = torch.zeros(6 << 30, dtype=torch.uint8, device="cuda")
+    pool, scale = random_pages(rng, 2, b["pages"], 2, 16, 64, block=8, low=110)
+    far = raw.as_strided(pool.shape, (5 << 30, 1 << 20, 1024, 64, 1))
+    far.copy_(torch.from_numpy(pool))
+    _, sd = _held(pool, scale)
+    node = np.array([[2, 7, 8, 19]], np.int32)
+
+    def up(x):
+        return torch.from_numpy(np.ascontiguousarray(x)).cuda()
+    P.compact_paged(far.view(E4M3), up(b["page_table"]), up(np.array([11], np.int32)), up(node),
+                    up(np.array([3], np.int32)), 20, scale=sd)
+    wp, ws = HO.compact(pool, scale, b["page_table"], [11], node, [3], 20)
+    assert same(far.cpu().numpy(), wp) and np.array_equal(_bytes(sd), ws)
+
+
 def test_compact_leaves_refused_requests_untouched():
     rng = np.random.default_rng(4)
 

@@ -80,6 +80,15 @@ def test_many_rows():
     run(3000, 1024, 128, torch.bfloat16)
 
 
+def test_rows_past_32_bits():
+    T, H = 140000, 16384  # 4.6 GB
+    x = torch.empty(T, H, dtype=torch.float16, device="cuda").normal_()
+    r = x.clone()
+    y, s = P.rms_norm(x, None, r, group=0)
+    for rows in (slice(0, 3), slice(T - 3, T)):
+        check(x[rows], None, x[rows], r[rows], 1e-6, 0, (y[rows], s[rows]))
+
+
 def test_zeros_infinities_and_nan():
     """A row of zeros has scales and values of zero; what is not finite stays where it is."""
     x = torch.zeros(4, 256, dtype=torch.bfloat16, device="cuda")
