@@ -144,6 +144,21 @@ def test_longer_chunks(D, dt, rows, ctx):
     run_attention(b, 6, 2, D, 64, 32, dt, poison=False)
 
 
+@pytest.mark.parametrize("Hq,Hkv,D", [(64, 1, 128), (40, 1, 64), (16, 1, 128), (33, 3, 64), (7, 7, 128)])
+def test_groups_of_heads(Hq, Hkv, D):
+    """Single tokens and short chunks whose heads alone are more rows than the small kernel's."""
+    rng = np.random.default_rng(Hq)
+    b = make_batch(rng, [1, 2, 1, 9], [700, 90, 0, 31], 32)
+    run_attention(b, Hq, Hkv, D, 32, 32, torch.bfloat16)
+
+
+def test_large_pages():
+    rng = np.random.default_rng(77)
+    b = make_batch(rng, [1, 100, 3], [1500, 1000, 5], 1024)
+    run_attention(b, 4, 2, 64, 1024, 64, torch.float16)
+    run_append(b, 4, 3, 64, 1024, 64, torch.float16)
+
+
 def test_many_requests():
     """More than 64, which are not ordered by length."""
     rng = np.random.default_rng(8)
@@ -357,6 +372,14 @@ def test_append(dt, D, page, block):
     rng = np.random.default_rng((page, block))
     b = make_batch(rng, [1, 5, 0, 70, 1, 33, 2], [0, 3, 9, block - 1, 2 * block, 63, block + 7], page, gap=1)
     run_append(b, 4, 2, D, page, block, dt)
+
+
+@pytest.mark.parametrize("Hkv", [1, 3, 5])
+@pytest.mark.parametrize("D,page,block", [(64, 8, 8), (64, 32, 16), (128, 16, 8), (128, 64, 64)])
+def test_append_of_odd_heads(Hkv, D, page, block):
+    """Heads that do not fill a workgroup."""
+    b = make_batch(np.random.default_rng((Hkv, block)), [9, 1, 40, 2], [3, 8, 30, 0], page)
+    run_append(b, 3, Hkv, D, page, block, torch.bfloat16)
 
 
 @pytest.mark.parametrize("kw", [dict(norm=False, rope=False), dict(rope=False), dict(norm=False, inter=True),
