@@ -147,11 +147,11 @@ __device__ __forceinline__ void append_block(const AppendArgs& a, bool live, boo
   if (part == 0 && lane == 0) *scale = (uint8_t)now;
 }
 
-// Workgroups of keys and values first, whose chains are long (reversed, 8000 rows take 51
-// us for 48): each takes Share's heads of one or both and, of `window` rows, the blocks
-// whose first new row is among these.  Then qblocks of queries, qsplit waves a row.  Bytes
-// bound them (8000 rows of 32 and 8 heads of 128, 182 MB: 48 us, 3.8 TB/s).
-template <int D, bool H, int G>
+// Workgroups of keys and values first, whose chains are long: each takes, of `window`
+// rows, the blocks whose first new row is among these, for Share's heads of the keys or the
+// values, or (Both) of the keys and then the values.  Then qblocks of queries, qsplit waves
+// a row.  Bytes bound them (7900 rows of 32 and 8 heads of 128, 182 MB: 45 us, 4.0 TB/s).
+template <int D, bool H, int G, bool Both>
 __global__ __launch_bounds__(kThreads) void append8_kernel(AppendArgs a, HeldScales sc, int qblocks,
                                                           int qsplit, int window) {
   using S = Share<D, G>;
@@ -163,10 +163,11 @@ __global__ __launch_bounds__(kThreads) void append8_kernel(AppendArgs a, HeldSca
     if (w / qsplit < a.b.T) append_queries<D, H>(a, w / qsplit, w % qsplit, qsplit);
     return;
   }
-  const int groups = (2 * a.Hkv + S::heads - 1) / S::heads;  // of heads
+  const int items = Both ? a.Hkv : 2 * a.Hkv;
+  const int groups = (items + S::heads - 1) / S::heads;  // of heads
   const int b = blockIdx.x;
   const int item = b % groups * S::heads + wave / S::waves, h = item % a.Hkv;
-  const bool keys = item < a.Hkv, live = item < 2 * a.Hkv;
+  const bool live = item < items;
   const int t0 = b / groups * window, end = min(t0 + window, a.b.T);
   const int blocks = 1 << (a.b.page_shift - sc.block_shift);  // of a page
   int turn = 0;
@@ -184,35 +185,51 @@ __global__ __launch_bounds__(kThreads) void append8_kernel(AppendArgs a, HeldSca
           slot < a.b.C ? a.b.page_table[(size_t)r * a.b.max_pages + (slot >> a.b.page_shift)] : -1;
       if ((unsigned)page < (unsigned)a.b.pages) {
         const int off = slot & ((1 << a.b.page_shift) - 1);
-        uint8_t* block = (uint8_t*)(keys ? a.k_pages : a.v_pages) +
-                         ((size_t)page * a.b.page_units + (size_t)h * a.b.head_units) * 16 +
-                         (size_t)(off - o0) * D;
-        uint8_t* scale = (keys ? sc.k : sc.v) + (size_t)page * sc.stride + (size_t)h * blocks +
-                         (off >> sc.block_shift);
-        append_block<D, H, G>(a, live, keys, h, t, n, o0, slot, block, scale, wave % S::waves,
-                              most[turn ^= 1]);
+#pragma unroll
+        for (int kind = 0; kind < (Both ? 2 : 1); ++kind) {
+          const bool keys = Both ? kind == 0 : item < a.Hkv;
+          uint8_t* block = (uint8_t*)(keys ? a.k_pages : a.v_pages) +
+                           ((size_t)page * a.b.page_units + (size_t)h * a.b.head_units) * 16 +
+                           (size_t)(off - o0) * D;
+          uint8_t* scale = (keys ? sc.k : sc.v) + (size_t)page * sc.stride + (size_t)h * blocks +
+                           (off >> sc.block_shift);
+          append_block<D, H, G>(a, live, keys, h, t, n, o0, slot, block, scale, wave % S::waves,
+                                most[turn ^= 1]);
+        }
       }
     }
     t += n;
   }
 }
 
-template <int D, bool H, int G>
-hipError_t append(const AppendArgs& a, const HeldScales& s, hipStream_t stream) {
+template <int D, bool H, int G, bool Both>
+hipError_t append_as(const AppendArgs& a, const HeldScales& s, hipStream_t stream) {
   using S = Share<D, G>;
-  const int T = a.b.T, groups = (2 * a.Hkv + S::heads - 1) / S::heads;
+  const int T = a.b.T, groups = ((Both ? a.Hkv : 2 * a.Hkv) + S::heads - 1) / S::heads;
   int qsplit = 1;
   long long qblocks = 0;
   if (a.q) {
     const int units = (a.Hq + 512 / D - 1) / (512 / D);
-    qsplit = std::max(1, std::min(units, 8192 / T));
+    qsplit = std::max(1, std::min(units, (Both ? 16384 : 8192) / T));
     qblocks = ((long long)T * qsplit + kWaves - 1) / kWaves;
   }
   const int window = (long long)T * groups <= 4096 ? 1 : G;
   const long long blocks = qblocks + (long long)((T + window - 1) / window) * groups;
-  append8_kernel<D, H, G><<<(unsigned)blocks, kThreads, 0, stream>>>(a, s, (int)qblocks, qsplit,
-                                                                    window);
+  append8_kernel<D, H, G, Both>
+      <<<(unsigned)blocks, kThreads, 0, stream>>>(a, s, (int)qblocks, qsplit, window);
   return hipGetLastError();
+}
+
+// Both where the workgroups of one kind are more than the card takes in about one round: the
+// request and page are found once for two blocks and queries begin earlier (32 and 8 heads of
+// 128: 16,000 rows in blocks of 16 115 us to 101, 6000 in blocks of 32 35 to 31; but 600 in
+// blocks of 8 7.4 to 13.8 and 4000 in blocks of 64 24 to 25).
+template <int D, bool H, int G>
+hipError_t append(const AppendArgs& a, const HeldScales& s, hipStream_t stream) {
+  using S = Share<D, G>;
+  const long long rows = (long long)a.b.T * ((2 * a.Hkv + S::heads - 1) / S::heads);
+  return rows > 2500LL * G ? append_as<D, H, G, true>(a, s, stream)
+                           : append_as<D, H, G, false>(a, s, stream);
 }
 
 // Requests of one row each (single tokens): the row's heads of queries, keys and values 512 /

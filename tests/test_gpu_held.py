@@ -419,6 +419,16 @@ def test_append_of_many_rows(Hkv, T):
     run_append(b, 2, Hkv, 64, 16, 8, torch.bfloat16)
 
 
+@pytest.mark.parametrize("D,Hkv,page,block,T", [(64, 47, 16, 8, 900), (128, 25, 8, 8, 900), (128, 25, 32, 16, 900),
+                                                (128, 50, 64, 32, 850), (64, 200, 64, 64, 450)])
+def test_append_of_rows_that_fill_the_card(D, Hkv, page, block, T):
+    """Keys and values by the same workgroups, also where their heads do not fill the last."""
+    rng = np.random.default_rng((D, Hkv, block))
+    cuts = np.sort(rng.choice(np.arange(1, T), 9, replace=False))
+    b = make_batch(rng, np.diff(np.concatenate([[0], cuts, [T]])), rng.integers(0, 90, 10), page, gap=1)
+    run_append(b, 3, Hkv, D, page, block, torch.bfloat16, low=110)
+
+
 def test_append_of_many_requests_one_row_each():
     rng = np.random.default_rng(11)
     b = make_batch(rng, [1] * 300, rng.integers(0, 40, 300), 16)
