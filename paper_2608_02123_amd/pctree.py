@@ -868,8 +868,8 @@ class PagedAttention:
         self._ws = _Workspace(self.ws_bytes, batch.device)
         self.workspace = self._ws.tensor
 
-    def __call__(self, q, k_cache, v_cache, batch, mask=None, out=None, *, k_scale=None,
-                 v_scale=None, stream=None):
+    def __call__(self, q, k_cache, v_cache, batch, mask=None, out=None, stream=None, *,
+                 k_scale=None, v_scale=None):
         """``q [T][Hq][D]`` over ``k_cache, v_cache [pages][Hkv][page_size][D]``; causal, or
         with ``mask`` (:func:`build_mask`) the tree's.  Returns ``out [T][Hq][D]``
         (rows of no request are not written).  Pages in 8 bits come with their
@@ -908,8 +908,8 @@ class PagedAttention:
         return out
 
 
-def paged_attention(q, k_cache, v_cache, batch, mask=None, scale=None, out=None, *, k_scale=None,
-                    v_scale=None, stream=None):
+def paged_attention(q, k_cache, v_cache, batch, mask=None, scale=None, out=None, stream=None, *,
+                    k_scale=None, v_scale=None):
     """One call of :class:`PagedAttention`."""
     with _Here(batch.idx, stream):
         layer = PagedAttention(batch, q.shape[1], k_cache.shape[1], k_cache.shape[3],

@@ -3,6 +3,7 @@ conversions and direct search, and the refusals of the C ABI and of the binding.
 from __future__ import annotations
 
 import ctypes
+import inspect
 import math
 
 import numpy as np
@@ -151,3 +152,14 @@ def test_binding_refuses_what_is_no_held_cache():
         P._held_cache(k, k, s, s, bf, 0)
     with pytest.raises(TypeError):  # pages in 8 bits without scales
         P._paged_cache(k, k, 0)
+
+
+@pytest.mark.parametrize("call,names", [
+    (P.PagedAttention.__call__, "self q k_cache v_cache batch mask out stream"),
+    (P.paged_attention, "q k_cache v_cache batch mask scale out stream"),
+    (P.compact_paged, "pool page_table prefix_len accept_node accept_len budget stream"),
+    (P.append_paged, "batch k_cache v_cache k v q")])
+def test_arguments_by_position(call, names):
+    """Those of 16-bit pages keep their places; scales come by name."""
+    p = inspect.signature(call).parameters.values()
+    assert [x.name for x in p if x.kind is x.POSITIONAL_OR_KEYWORD] == names.split()
