@@ -6,10 +6,12 @@
 // adjust_kernel: a workgroup takes a segment of the vocabulary and some rows of one
 // request.  It counts the request's history in a table of the segment in LDS, so a token's
 // count costs no memory beside the history itself, whatever the history's length; then
-// each wave goes over rows by itself and touches only the tokens that the table holds.  A
-// tree's node counts its ancestors' tokens: those in the segment are few, and listed for
-// each row.  One row after 2000 tokens 5.6 us: parameters, history, table and logits in a
-// chain; 512 rows 23 us, 64 single rows 21 of a call, their tokens' lines of memory.
+// each wave goes over rows by itself, or over its share of the tokens where rows are few,
+// and touches only the tokens that the table holds.  A tree's node counts its ancestors'
+// tokens: those in the segment are few, and listed for each row.  One row after 2000
+// tokens 5.4 us: parameters, history, table and logits in a chain; 512 rows 22 us, 64
+// single rows 20, their tokens' lines of memory.  (A table that holds most of a small
+// vocabulary: 512 rows of 1,827 tokens 70 us with waves by rows alone, 14 so.)
 // (Segments of 4096 tokens took 124 us for the 512 rows where these take 84, a mask's pass
 // in this kernel included at the time: fewer workgroups fit a compute unit; of 1024, 106.)
 #include "pctree.h"
@@ -18,6 +20,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "pctree_step.h"
 #include "pctree_tile.h"
@@ -183,7 +186,7 @@ __global__ __launch_bounds__(kThreads) void adjust_kernel(AdjustArgs a, int segm
   if (!a.presence || !(fabsf(p.presence) < __builtin_inff())) p.presence = 0.0f;
   const bool penalties = p.repetition != 1.0f || p.frequency != 0.0f || p.presence != 0.0f;
   const int cnt = rows_of(a, start, row_count).cnt;
-  const int per = max((cnt + groups - 1) / groups, kWaves);  // (of the rows there are)
+  const int per = (cnt + groups - 1) / groups;  // (of the rows there are)
   const int first = group * per, last = min(first + per, cnt);
   if (first >= last) return;
   const int v0 = seg * kSegment, width = min(kSegment, a.V - v0);
@@ -246,24 +249,30 @@ __global__ __launch_bounds__(kThreads) void adjust_kernel(AdjustArgs a, int segm
   const int listed = sListed, nodes = sNodes;
 
   // Rows of a wave a few at a time, whose loads all issue before the first is used; 64 of
-  // the table's tokens, one to a lane.
-  for (int i0 = first + wave; i0 < last; i0 += kRows * kWaves) {
-    int i[kRows], m[kRows];
+  // the table's tokens, one to a lane.  Where the workgroup has few rows its waves share
+  // them and take tokens in turn.
+  const int rows = last - first;
+  const bool share = rows <= kRows;
+  const int apart = share ? 1 : kWaves;  // rows of a wave
+  const int k_first = share ? wave * 64 : 0, k_step = share ? kWaves * 64 : 64;
+  const auto adjust = [&](auto number, int i0) {
+    constexpr int K = number.value;
+    int i[K], m[K];
 #pragma unroll
-    for (int j = 0; j < kRows; ++j) {
-      i[j] = min(i0 + j * kWaves, last - 1);
+    for (int j = 0; j < K; ++j) {
+      i[j] = min(i0 + j * apart, last - 1);
       m[j] = !a.allowed ? -1 : a.allowed_row ? a.allowed_row[start + i[j]] : start + i[j];
     }
-    for (int k0 = 0; k0 < listed; k0 += 64) {
+    for (int k0 = k_first; k0 < listed; k0 += k_step) {
       const bool has = k0 + lane < listed;
       const int at = list[min(k0 + lane, listed - 1)];
       const uint32_t e = table[at];
       const float b = e & kBias ? a.bias_value[bias[at] - 1u] : 0.0f;
-      T* place[kRows];
-      T x[kRows];
-      uint32_t ok[kRows], n[kRows];
+      T* place[K];
+      T x[K];
+      uint32_t ok[K], n[K];
 #pragma unroll
-      for (int j = 0; j < kRows; ++j) {
+      for (int j = 0; j < K; ++j) {
         place[j] = (T*)a.logits + (long long)(start + i[j]) * a.row_stride + v0 + at;
         x[j] = *place[j];
         n[j] = e & kCount;
@@ -273,33 +282,44 @@ __global__ __launch_bounds__(kThreads) void adjust_kernel(AdjustArgs a, int segm
       // and how often it is among the row's node and its ancestors
       for (int l0 = 0; l0 < nodes; l0 += 64) {
         const int l = min(l0 + lane, nodes - 1), node = node_is[l], token = node_at[l];
-        uint32_t word[kRows];
+        uint32_t word[K];
 #pragma unroll
-        for (int j = 0; j < kRows; ++j)
-          word[j] = a.mask[((size_t)r * a.N + i[j]) * a.NW + (node >> 5)];
+        for (int j = 0; j < K; ++j) word[j] = a.mask[((size_t)r * a.N + i[j]) * a.NW + (node >> 5)];
 #pragma unroll
-        for (int j = 0; j < kRows; ++j) {
+        for (int j = 0; j < K; ++j) {
+          if (i0 + j * apart >= last) break;
           uint64_t in = __ballot(l0 + lane < nodes && ((word[j] >> (node & 31)) & 1u));
           for (; in; in &= in - 1)
             n[j] += __builtin_amdgcn_readlane(token, (int)__builtin_ctzll(in)) == at;
         }
       }
 #pragma unroll
-      for (int j = 0; j < kRows; ++j) {
+      for (int j = 0; j < K; ++j) {
         const bool seen = (e & kSeen) || n[j];
         float y = penalised((float)x[j], seen, n[j], p);
         if (e & kBias) y += b;
-        if (has && (seen || (e & kBias)) && i0 + j * kWaves < last && ((ok[j] >> (at & 31)) & 1u))
+        if (has && (seen || (e & kBias)) && i0 + j * apart < last && ((ok[j] >> (at & 31)) & 1u))
           *place[j] = (T)y;
       }
     }
+  };
+  if (rows == 1) {
+    adjust(std::integral_constant<int, 1>{}, first);
+  } else {
+    for (int i0 = share ? first : first + wave; i0 < last; i0 += kRows * apart)
+      adjust(std::integral_constant<int, kRows>{}, i0);
   }
 }
 
+// Groups of a request's rows: of kRows at least, fewer where they leave compute units idle
+// (64 nodes over 3,831 tokens 9.4 us with four rows, 6.8 with one; over 32,000 with one
+// 8.4, with four 7.1).
 int row_groups(const AdjustArgs& a, int segments) {
   const long long pairs = (long long)a.R * segments;
-  const long long want = (1024 + pairs - 1) / pairs, most = (a.max_rows + kWaves - 1) / kWaves;
-  return (int)std::max(1ll, std::min(want, most));
+  const auto groups = [&](int blocks, int most) {
+    return std::min<long long>((blocks + pairs - 1) / pairs, most);
+  };
+  return (int)std::max({1ll, groups(1024, a.max_rows / kRows), groups(256, a.max_rows)});
 }
 
 template <typename T>

@@ -120,6 +120,17 @@ def test_trees_of_many_nodes():
     check(case(rng, 2, 300, 5000, torch.float32)[0], a)
 
 
+@pytest.mark.parametrize("R,rows,V", [(1, 1, 1800), (2, 3, 1800), (1, 70, 300), (40, 9, 2100), (70, 4, 2100), (90, 13, 4100)])
+def test_tables_that_hold_most_of_the_vocabulary(R, rows, V):
+    """Rows that a workgroup has one, a few or many of, and tokens that its waves share."""
+    rng = np.random.default_rng((R, rows))
+    logits, a = case(rng, R, rows, V, torch.bfloat16, tree=True, grammar=3, bias=200, history=(1000, 3500))
+    a["token"] = rng.integers(-1, V + 1, (R, rows)).astype(np.int32)
+    check(logits, a, max_rows=rows)
+    a["row_count"] = rng.integers(0, rows + 1, R).astype(np.int32)
+    check(case(rng, R, rows, V, torch.bfloat16)[0], a)
+
+
 def test_long_histories():
     rng = np.random.default_rng(2)
     check(*case(rng, 2, 1, 151936, torch.bfloat16, history=(40000, 60000), wild=False))
