@@ -530,9 +530,10 @@ pctree_status pctree_compact_paged8(void* pool, int64_t group_stride, int64_t pa
  * Without `scale`, out is y in dtype; with it, out holds e4m3 bytes y / c, c =
  * max |y| / 448 over each `group` elements of the row (the last group may be
  * shorter), in scale (infinite and NaN elements do not count and are held as NaN;
- * a group of zeros has scale 0).  float32 throughout, each output rounded once; v
- * is not rounded before it is normed.  (Where a row's sum of squares passes float32's
- * range, its finite elements give 0.)
+ * a group of zeros has scale 0; where c is one of float32's subnormal numbers, a
+ * quotient that its rounding leaves past 448 is held as 448).  float32 throughout,
+ * each output rounded once; v is not rounded before it is normed.  (Where a row's sum
+ * of squares passes float32's range, its finite elements give 0.)
  * --------------------------------------------------------------------- */
 #define PCTREE_MAX_NORM_WIDTH 32768
 

@@ -123,8 +123,13 @@ __global__ __launch_bounds__(1024) void norm_kernel(NormArgs a) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[i][e] = divided(v[i][e], d, r);
       } else {  // (whose reciprocal may not be there)
+        // A subnormal c is m / 448 rounded to a few bits, so that m / c reaches 671: held as
+        // 448.  (An infinity or NaN stays one.)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[i][e] /= d;
+        for (int e = 0; e < 8; ++e) {
+          const float q = v[i][e] / d;
+          v[i][e] = fabsf(q) < __builtin_inff() ? fminf(fmaxf(q, -kMostHeld), kMostHeld) : q;
+        }
       }
       *(uint2*)((uint8_t*)a.out + t * a.out_stride + u * 8) = hold8(v[i]);
       if (u * 8 % a.group == 0) a.scale[t * a.groups + u * 8 / a.group] = c;

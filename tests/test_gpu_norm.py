@@ -136,3 +136,62 @@ def test_refusals():
         P.rms_norm(x[:, :100])
     with pytest.raises(P.PCTreeError):
         P.rms_norm(x[:, 4:12])
+
+
+def check_quiet(x, w, group):
+    """8-bit outputs where groups' maxima are float32's subnormal numbers and somewhat more.
+
+    There every float32 result is off by half a subnormal step, h = 2^-150, beside its relative
+    error.  y = (v * inv) * w, |w| <= 1: off by 2 h more.  c = m / 448: by h more, so 448 c lies
+    within 448 h of m, and where a quotient y / c passes 448 what is held, 448 c, is off by that
+    much at most; where c is 0, m is below 449 h.  So the error is that of check() and 452 h."""
+    h = 2.0 ** -150
+    v, y = SO.rms_norm(_np(x), None if w is None else _np(w), None, 1e-6)
+    out, scale = P.rms_norm(x, w, group=group)
+    n = group or x.shape[1]
+    c, s = SO.group_scales(y, n), _np(scale)
+    assert (np.abs(s - c) <= 2.0 ** -17 * c + 2 * h).all()
+    got = _np(out.float())
+    assert np.isfinite(got).all(), f"{np.isnan(got).sum()} of {got.size} finite elements are NaN"
+    full = np.repeat(s, n, 1)
+    err = np.abs(got * full - y)
+    tol = np.maximum((2.0 ** -4 + 2.0 ** -16) * np.abs(y), 2.0 ** -10 * full + 2.0 ** -16 * np.abs(y)) + 452 * h
+    assert (err <= tol).all()
+    return c
+
+
+@pytest.mark.parametrize("group", [32, 128])
+@pytest.mark.parametrize("low,high", [(0, 14), (14, 30), (30, 60)])
+def test_groups_of_tiny_values_beside_an_outlier(group, low, high):
+    """Groups whose largest magnitude is 2^low to 2^high subnormal steps of float32: an outlier of
+    2^60 in 256 elements makes 1 / root 2^-56."""
+    g = torch.Generator().manual_seed(high)
+    T, H = 300, 256
+    n = H // group
+    x = torch.rand(T, n, group, generator=g) * 2 - 1
+    x[..., 0] = 1.0
+    x *= torch.exp2(low + (high - low) * torch.rand(T, n, 1, generator=g)) * 2.0 ** (56 - 149)
+    x = x.reshape(T, H)
+    x[:, 0] = 2.0 ** 60
+    c = check_quiet(x.bfloat16().cuda(), None, group)
+    assert (c[:, 1:] < 2.0 ** (high - 149) / 400).all()
+
+
+def test_groups_of_tiny_weights():
+    """Weights of bfloat16's least numbers, for rows of ordinary values."""
+    g = torch.Generator().manual_seed(4)
+    T, H = 200, 512
+    x = torch.randn(T, H, generator=g) * torch.exp2(-20 * torch.rand(T, 16, 1, generator=g)).expand(T, 16, 32).reshape(T, H)
+    w = torch.ldexp(torch.randint(1, 128, (H,), generator=g).float(), torch.tensor(-133))
+    w[:32] = 1.0
+    for group in (32, 64, 0):
+        check_quiet(x.bfloat16().cuda(), w.bfloat16().cuda() if group else (w.bfloat16() * 0 + w[40]).bfloat16().cuda(), group)
+
+
+def test_a_nan_makes_its_row_nan():
+    x = torch.randn(3, 256, generator=torch.Generator().manual_seed(5)).bfloat16().cuda()
+    x[1, 3] = float("nan")
+    for group in (None, 0, 32):
+        got = P.rms_norm(x, group=group)
+        y = got if group is None else got[0].float()
+        assert torch.isnan(y[1]).all() and torch.isfinite(y[[0, 2]]).all()
