@@ -607,7 +607,7 @@ typedef struct pctree_adjust {
   int32_t requests;             /* R                                                   */
   int32_t max_rows;             /* the most rows that a request has, <= rows           */
   int32_t history_total;        /* below 2^29                                          */
-  int32_t bias_total;
+  int32_t bias_total;           /* below 2^29                                          */
   int32_t budget;               /* N (0 where token is NULL)                           */
   int32_t masks;                /* rows of allowed (at least `rows` without allowed_row) */
   int32_t dtype;                /* PCTREE_F32, PCTREE_BF16 or PCTREE_F16               */
@@ -615,7 +615,8 @@ typedef struct pctree_adjust {
 
 /* Errors: INVALID_ARGUMENT (null or misaligned pointer, a size that the comments rule
  * out), UNSUPPORTED (vocab > PCTREE_MAX_VOCAB, requests > 65535, budget >
- * PCTREE_MAX_MASK_BUDGET, history_total past its limit, sizes past a launch). */
+ * PCTREE_MAX_MASK_BUDGET, history_total or bias_total past its limit, sizes past a
+ * launch). */
 pctree_status pctree_adjust_logits(const pctree_adjust* args, void* stream);
 
 /* Static, human-readable name of a status code. */

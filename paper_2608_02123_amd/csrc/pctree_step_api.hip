@@ -11,7 +11,8 @@ bool aligned(const void* ptr, size_t a) { return ((uintptr_t)ptr & (a - 1)) == 0
 
 // A launch has at most 2^32 - 1 threads along x; a row of the norm has up to 1024.
 constexpr int32_t kMaxNormRows = 1 << 21;
-constexpr int32_t kMaxHistory = (1 << 29) - 1;  // a count's bits (pctree_adjust.hip)
+// A count's bits (pctree_adjust.hip); a thread's index passes a list's end by its step.
+constexpr int32_t kMaxList = (1 << 29) - 1;
 
 bool strided(int64_t stride, int64_t width, int32_t rows) {
   return stride >= width && stride % 8 == 0 && stride <= INT64_MAX / 4 / rows;
@@ -62,7 +63,7 @@ pctree_status check_adjust(const pctree_adjust* j) {
   for (const void* p : words)
     if (!aligned(p, 4)) return PCTREE_ERR_INVALID_ARGUMENT;
   if (j->vocab > PCTREE_MAX_VOCAB || j->requests > 65535 || j->budget > PCTREE_MAX_MASK_BUDGET ||
-      j->history_total > kMaxHistory)
+      j->history_total > kMaxList || j->bias_total > kMaxList)
     return PCTREE_ERR_UNSUPPORTED;
   return PCTREE_OK;
 }

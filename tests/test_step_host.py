@@ -65,3 +65,10 @@ def test_binding_refuses_host_tensors_and_types():
                         (lambda: P.adjust_logits(x[0], i, i), ValueError)):
         with pytest.raises(error):
             call()
+
+
+@pytest.mark.parametrize("total", [1 << 29, (1 << 31) - 200, (1 << 31) - 1])
+def test_lists_of_biases_past_a_counters_range(total):
+    """A thread's counter passes a request's entries by up to a workgroup's step."""
+    assert adjust(bias_total=total) == P.ERR_UNSUPPORTED
+    assert adjust(history_total=total) == P.ERR_UNSUPPORTED
