@@ -471,9 +471,15 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
     }
     return bad;
   };
-  // (part: some row sees the chunk only in part, so infinite and NaN values become zeros)
-  auto stage = [&](int buf, bool part) __attribute__((always_inline)) {
+  // (part: some row sees the chunk only in part, so infinite and NaN values become zeros;
+  // bad: its slots without a page, whose values no row admits and nothing has to mend)
+  auto stage = [&](int buf, bool part, uint64_t bad) __attribute__((always_inline)) {
     bool odd = false;
+    if (bad) {
+#pragma unroll
+      for (int i = 0; i < UPT; ++i)
+        if ((bad >> ((i * kThreads + threadIdx.x) / HU)) & 1) vx[i] = u32x4{0u, 0u, 0u, 0u};
+    }
 #pragma unroll
     for (int i = 0; i < UPT; ++i) {
       const int row = (i * kThreads + threadIdx.x) / HU, u = 2 * (threadIdx.x % HU);
@@ -505,7 +511,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
   if (threadIdx.x == 0) sOdd = 0;
   if constexpr (Q8) {
     lds_barrier();
-    stage(0, bad_next || kbeg + kChunk > all_see);
+    stage(0, bad_next || kbeg + kChunk > all_see, bad_next);
   }
   if (a.mask) {
     const uint32_t* mg = a.mask + ((size_t)wk.r * a.N + i_first) * a.NW;
@@ -589,7 +595,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
   const int whole = a.b.page_shift >= 3 ? all_see : kbeg;
   auto stage_next = [&]() __attribute__((always_inline)) {
     if constexpr (Q8) {
-      if (c0 + kChunk < kend) stage(buf ^ 1, bad_next || c0 + 2 * kChunk > all_see);
+      if (c0 + kChunk < kend) stage(buf ^ 1, bad_next || c0 + 2 * kChunk > all_see, bad_next);
     }
   };
   for (; c0 + kChunk <= whole && !bad_next; c0 += kChunk, buf ^= 1) {
@@ -650,7 +656,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
 #pragma unroll
     for (int h = 0; h < kHalves; ++h) weigh(sKV[buf][1], h, bp[h]);
     // (one piece of code where the next chunk is whole too: 261 to 255 us)
-    if (Q8 && c0 + 2 * kChunk <= all_see && !bad_next) stage(buf ^ 1, false);
+    if (Q8 && c0 + 2 * kChunk <= all_see && !bad_next) stage(buf ^ 1, false, 0);
     else stage_next();
   }
   for (; c0 < kend; c0 += kChunk, buf ^= 1) {
@@ -1026,7 +1032,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3))) v
     const bool none = (unsigned)pg >= (unsigned)a.b.pages;
     const uint64_t bad = __ballot(none);
     const uint32_t pgc = none ? 0u : (uint32_t)pg;
-    // (slots past the run: others of its last page, which no row admits)
+    const int last = kend - 1 - c0;  // (slots past the run: others of its last page)
     u32x4 kx[2][2][KU];
     if (a.b.page_shift >= 6) {  // the chunk lies in one page
       const size_t at = (uint32_t)__builtin_amdgcn_readfirstlane((int)pgc) * page_bytes + head_bytes +
@@ -1100,7 +1106,9 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3))) v
 #pragma unroll 1
       for (int i = 0; i < INS; ++i) {
         u32x4 w = *(const u32x4*)(sV[wave] + i * 1024 + lane * 16);
-        const float f = scale_up(__builtin_amdgcn_ds_bpermute((8 + (i * RPI + lane / HU) / 8) * 4, sbyte));
+        const int row = i * RPI + lane / HU;
+        const bool gone = row > last || ((bad >> row) & 1);  // (no row admits it: nothing to mend)
+        const float f = scale_up(__builtin_amdgcn_ds_bpermute((8 + row / 8) * 4, sbyte));
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const u32x2 v = held4<H>(w[e], f);
@@ -1109,7 +1117,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3))) v
           if (odd16<H>(v[0] >> 16)) keep &= 0xffff00ffu;
           if (odd16<H>(v[1])) keep &= 0xff00ffffu;
           if (odd16<H>(v[1] >> 16)) keep &= 0x00ffffffu;
-          odd |= keep != 0xffffffffu;
+          odd |= !gone && keep != 0xffffffffu;
           w[e] &= keep;
         }
         *(u32x4*)(sV[wave] + i * 1024 + lane * 16) = w;

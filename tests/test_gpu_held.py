@@ -582,3 +582,55 @@ def test_compact_many_groups_and_strides():
     want, wants = raw.copy(), rs.copy()
     want[:, :2], wants[:, :2] = wp.swapaxes(0, 1), ws.swapaxes(0, 1)
     assert same(pool.cpu().numpy(), want) and np.array_equal(scale.cpu().numpy(), wants)
+
+
+def _time(call, n=20):
+    """The least of five times of a call among others, in us."""
+    begin, end, best = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True), float("inf")
+    for _ in range(6):
+        begin.record()
+        for _ in range(n):
+            call()
+        end.record()
+        torch.cuda.synchronize()
+        best = min(best, begin.elapsed_time(end) / n * 1e3)
+    return best
+
+
+@pytest.mark.parametrize("dt,D", [(torch.bfloat16, 128), (torch.float16, 64)])
+@pytest.mark.parametrize("page", [16, 64])
+@pytest.mark.parametrize("rows,hole", [(1, False), (1, True), (300, False), (300, True)])
+def test_slots_that_hold_nothing_cost_no_time(dt, D, page, rows, hole):
+    """NaN (memory that nothing was written to) behind the last row of a request, and in the pages that
+    no request has, leaves the output's bits and the call's time (walking a run for such values
+    slot by slot takes ten times as long and more)."""
+    ctx, Hq, Hkv = 4001, 8, 2
+    rng = np.random.default_rng(page)
+    b = make_batch(rng, [rows] * (8 if rows == 1 else 1), [ctx] * (8 if rows == 1 else 1), page)
+    table = b["page_table"]
+    table[table == 0] = np.setdiff1d(np.arange(b["pages"]), table)[-1]  # (which an entry of no page could be read as)
+    if hole:
+        table[:, 5] = -1
+    k, ks, v, vs = random_held(rng, b["pages"], Hkv, page, D, 8)
+    dead = np.ones((b["pages"], page), bool)
+    for r in range(len(table)):
+        for s in range(ctx + rows):
+            at = PO.place(b, r, s, page, b["pages"])
+            if at:
+                dead[at] = False
+    assert dead[0].all()
+    kn, vn = k.copy(), v.copy()
+    for a in (kn, vn):
+        a.transpose(0, 2, 1, 3)[dead] = 0x7f
+    q = torch.randn(b["rows"], Hq, D, generator=_gen(1)).to(dt).cuda()
+    batch = dev_batch(b)
+    layer = P.PagedAttention(batch, Hq, Hkv, D, page)
+    got, us = [], []
+    for kk, vv in ((k, v), (kn, vn)):
+        (kd, ksd), (vd, vsd) = _held(kk, ks), _held(vv, vs)
+        out = torch.zeros(b["rows"], Hq, D, dtype=dt, device="cuda")
+        us.append(_time(lambda: layer(q, kd, vd, batch, out=out, k_scale=ksd, v_scale=vsd)))
+        got.append(out)
+    print(f"[held attention] {us[0]:.1f} us, with NaN {us[1]:.1f}", flush=True)
+    assert torch.equal(got[0].view(torch.int16), got[1].view(torch.int16))
+    assert us[1] < 3 * us[0] + 20
