@@ -514,7 +514,8 @@ pctree_status pctree_paged_attention8(const pctree_paged_cache8* cache,
  * scales and, where slots below prefix_len lie in it, of its own; rows and those slots
  * are held again where their scale was smaller.  Other slots of such a block stand for
  * nothing.  A request whose accepted nodes all stay in place is left untouched.  A block
- * that takes accepted rows belongs to one request. */
+ * that takes accepted rows belongs to one request.  UNSUPPORTED also for groups * heads
+ * past 4 * (2^24 - 1). */
 pctree_status pctree_compact_paged8(void* pool, int64_t group_stride, int64_t page_stride,
                                     uint8_t* scale, int64_t scale_group_stride,
                                     int64_t scale_page_stride, int32_t groups, int32_t pages,

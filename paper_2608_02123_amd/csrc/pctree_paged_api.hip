@@ -469,6 +469,8 @@ pctree_status pctree_compact_paged8(void* pool, int64_t group_stride, int64_t pa
     if ((head_dim != 64 && head_dim != 128) ||
         (block != 8 && block != 16 && block != 32 && block != 64))
       return PCTREE_ERR_UNSUPPORTED;
+    // (a wave for every head of every group)
+    if (((int64_t)groups * heads + 3) / 4 > kMaxGrid) return PCTREE_ERR_UNSUPPORTED;
     if (block > page_size || !apart(groups, pages, (int64_t)heads * (page_size / block),
                                     scale_group_stride, scale_page_stride))
       return PCTREE_ERR_INVALID_ARGUMENT;

@@ -163,3 +163,11 @@ def test_arguments_by_position(call, names):
     """Those of 16-bit pages keep their places; scales come by name."""
     p = inspect.signature(call).parameters.values()
     assert [x.name for x in p if x.kind is x.POSITIONAL_OR_KEYWORD] == names.split()
+
+
+@pytest.mark.parametrize("groups,heads,D", [((1 << 25) - 1, 8, 128), ((1 << 26) + 64, 1, 64), (1 << 14, 1 << 13, 64)])
+def test_compactions_past_a_launch(groups, heads, D):
+    """A wave for every group and head: more than 2^32 - 1 threads cannot be launched."""
+    block = heads * 8 * D
+    assert P.lib().pctree_compact_paged8(A, block, block, A, heads, heads, groups, 1, heads, 8, D, 8, A, 20, A, A, A,
+                                         2, 64, 16, None) == P.ERR_UNSUPPORTED
