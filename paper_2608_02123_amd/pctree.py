@@ -842,7 +842,7 @@ def append_paged(batch, k_cache, v_cache, k, v, q=None, *, q_norm=None, k_norm=N
                     _ptr(q_norm), _ptr(k_norm), _ptr(rope), _ptr(position), eps, Hq, rot, npos,
                     1 if interleaved else 0)
         status = call(ctypes.byref(whole), batch._ref, ctypes.byref(a), st)
-    _check(status, "pctree_append_paged")
+    _check(status, call.__name__)
     return q_out
 
 
@@ -904,7 +904,7 @@ class PagedAttention:
             status = call(
                 ctypes.byref(whole), batch._ref, q.data_ptr(), self.q_heads, self.scale, _ptr(mask),
                 budget, out.data_ptr(), self._ws.on(st), self.ws_bytes, st)
-        _check(status, "pctree_paged_attention")
+        _check(status, call.__name__)
         return out
 
 

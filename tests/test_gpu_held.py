@@ -634,3 +634,18 @@ def test_slots_that_hold_nothing_cost_no_time(dt, D, page, rows, hole):
     print(f"[held attention] {us[0]:.1f} us, with NaN {us[1]:.1f}", flush=True)
     assert torch.equal(got[0].view(torch.int16), got[1].view(torch.int16))
     assert us[1] < 3 * us[0] + 20
+
+
+def test_errors_name_the_call():
+    """Blocks of four slots, which the pages' shapes allow and the library does not have."""
+    b = dev_batch(make_batch(np.random.default_rng(0), [1], [5], 16))
+    k = torch.zeros(4, 2, 16, 128, dtype=torch.uint8, device="cuda").view(E4M3)
+    s = torch.zeros(4, 2, 4, dtype=torch.uint8, device="cuda").view(E8M0)
+    row = torch.zeros(1, 2, 128, dtype=torch.bfloat16, device="cuda")
+    with pytest.raises(P.PCTreeError, match="^pctree_append_paged8:"):
+        P.append_paged(b, k, k, row, row, k_scale=s, v_scale=s)
+    with pytest.raises(P.PCTreeError, match="^pctree_paged_attention8:"):
+        P.PagedAttention(b, 2, 2, 128, 16)(row, k, k, b, k_scale=s, v_scale=s)
+    pages = torch.zeros(4, 2, 3, 128, dtype=torch.bfloat16, device="cuda")  # (three slots: no power of two)
+    with pytest.raises(P.PCTreeError, match="^pctree_append_paged:"):
+        P.append_paged(b, pages, pages, row, row)
