@@ -807,7 +807,7 @@ def append_paged(batch, k_cache, v_cache, k, v, q=None, *, q_norm=None, k_norm=N
         c = whole = _paged_cache(k_cache, v_cache, idx)
         dt, call = k_cache.dtype, lib().pctree_append_paged
     else:
-        dt, call = k.dtype, lib().pctree_append_paged8
+        dt, call = getattr(k, "dtype", None), lib().pctree_append_paged8
         whole = _held_cache(k_cache, v_cache, k_scale, v_scale, dt, idx)
         c = whole.pages
     D = c.head_dim
@@ -881,7 +881,7 @@ class PagedAttention:
             c = whole = _paged_cache(k_cache, v_cache, idx)
             dt, call = k_cache.dtype, lib().pctree_paged_attention
         else:
-            dt, call = q.dtype, lib().pctree_paged_attention8
+            dt, call = getattr(q, "dtype", None), lib().pctree_paged_attention8
             whole = _held_cache(k_cache, v_cache, k_scale, v_scale, dt, idx)
             c = whole.pages
         if c.kv_heads != self.kv_heads or c.head_dim != self.head_dim or \

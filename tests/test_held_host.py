@@ -171,3 +171,17 @@ def test_compactions_past_a_launch(groups, heads, D):
     block = heads * 8 * D
     assert P.lib().pctree_compact_paged8(A, block, block, A, heads, heads, groups, 1, heads, 8, D, 8, A, 20, A, A, A,
                                          2, 64, 16, None) == P.ERR_UNSUPPORTED
+
+
+def test_rows_that_are_no_tensors():
+    k = torch.zeros(4, 2, 16, 128, dtype=torch.uint8).view(torch.float8_e4m3fn)
+    s = torch.zeros(4, 2, 2, dtype=torch.uint8).view(torch.float8_e8m0fnu)
+
+    class Batch:
+        b = batch(requests=2, rows=3, max_rows=2, max_pages=4)
+        idx, rows, requests, sizes, _ref, device = -1, 3, 2, (2, 4, 3, 2), ctypes.byref(b), "meta"
+    for bad in (None, [1.0], 3):
+        with pytest.raises(TypeError):
+            P.append_paged(Batch, k, k, bad, bad, k_scale=s, v_scale=s)
+        with pytest.raises(TypeError):
+            P.PagedAttention(Batch, 2, 2, 128, 16)(bad, k, k, Batch, k_scale=s, v_scale=s)
