@@ -164,7 +164,7 @@ __device__ __forceinline__ float penalised(float x, bool seen, uint32_t count, c
 
 template <typename T>
 __global__ __launch_bounds__(kThreads) void adjust_kernel(AdjustArgs a, int segments, int groups) {
-  extern __shared__ uint32_t lds[];
+  extern __shared__ __attribute__((aligned(16))) uint32_t lds[];
   uint32_t* table = lds;                                               // [kSegment]
   uint32_t* bias = table + kSegment;                                   // [kSegment] where there are biases
   uint16_t* list = (uint16_t*)(bias + (a.bias_token ? kSegment : 0));  // [kSegment] tokens in the table

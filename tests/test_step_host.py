@@ -2,6 +2,8 @@
 from __future__ import annotations
 
 import ctypes
+import pathlib
+import re
 
 import pytest
 import torch
@@ -72,3 +74,20 @@ def test_lists_of_biases_past_a_counters_range(total):
     """A thread's counter passes a request's entries by up to a workgroup's step."""
     assert adjust(bias_total=total) == P.ERR_UNSUPPORTED
     assert adjust(history_total=total) == P.ERR_UNSUPPORTED
+
+
+def test_dynamic_lds_is_as_aligned_as_its_stores():
+    """The launch's LDS begins behind a kernel's own, at the array's alignment: what is written there in
+    16 bytes has to ask for as many."""
+    found = 0
+    for path in sorted((pathlib.Path(P.__file__).parent / "csrc").glob("*.hip")):
+        text = path.read_text()
+        for align, name in re.findall(r"extern __shared__ (__attribute__\(\(aligned\(16\)\)\) )?\w+ (\w+)\[\]", text):
+            names, more = set(), {name}
+            while more:  # what points into it
+                names |= more
+                more = {a for n in names for a in re.findall(rf"\* (\w+) = (?:\(\w+\*\))?\(?{n}\b", text)} - names
+            wide = any(re.search(rf"\(u?\w*x4\*\)\(?{n}\b", text) for n in names)
+            assert align or not wide, f"{path.name}: {name}"
+            found += wide
+    assert found
