@@ -1102,13 +1102,12 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3))) v
     l = mfma16<H>(ones, bp[1], l);
     wait_loads();
     if (!full) {  // infinite and NaN values become zeros
-      bool odd = false;
+      uint32_t odd = 0;  // a bit for each of the lane's 16 bytes
 #pragma unroll 1
       for (int i = 0; i < INS; ++i) {
         u32x4 w = *(const u32x4*)(sV[wave] + i * 1024 + lane * 16);
-        const int row = i * RPI + lane / HU;
-        const bool gone = row > last || ((bad >> row) & 1);  // (no row admits it: nothing to mend)
-        const float f = scale_up(__builtin_amdgcn_ds_bpermute((8 + row / 8) * 4, sbyte));
+        const float f = scale_up(__builtin_amdgcn_ds_bpermute((8 + (i * RPI + lane / HU) / 8) * 4, sbyte));
+        uint32_t all = 0xffffffffu;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const u32x2 v = held4<H>(w[e], f);
@@ -1117,12 +1116,16 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3))) v
           if (odd16<H>(v[0] >> 16)) keep &= 0xffff00ffu;
           if (odd16<H>(v[1])) keep &= 0xff00ffffu;
           if (odd16<H>(v[1] >> 16)) keep &= 0x00ffffffu;
-          odd |= !gone && keep != 0xffffffffu;
+          all &= keep;
           w[e] &= keep;
         }
+        odd |= (uint32_t)(all != 0xffffffffu) << i;
         *(u32x4*)(sV[wave] + i * 1024 + lane * 16) = w;
       }
-      if (odd) sOdd = 1;
+      for (; odd; odd &= odd - 1) {  // (a slot that no row admits leaves nothing to mend)
+        const int row = __builtin_ctz(odd) * RPI + lane / HU;
+        if (row <= last && !((bad >> row) & 1)) sOdd = 1;
+      }
     }
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
@@ -1256,7 +1259,9 @@ PagedPlan plan_paged_attention(int R, int T, int max_rows, int Hq, int Hkv, int 
   // Runs for six workgroups a compute unit, at most 12 of a request, which the merge
   // reads in two steps (us at 32, 16, 12, 8 runs at most: 8 single tokens of 500 to 4000
   // slots 31, 25, 25, 23; 40 of one kv head and up to 8000 slots 30, 22, 25, 27; 64 tokens
-  // of eight heads have 3 runs each, 150, and 165 with 2).
+  // of eight heads have 3 runs each, 150, and 165 with 2).  Long contexts of one or two
+  // requests would want more: one request of eight heads is 96 workgroups, which take 95 us
+  // for 131,072 slots in 8 bits, three requests 155 (in 16 bits 201 and 332).
   p.few_nsplit = p.few ? std::min(runs(pairs * p.few_qblocks, 6 * cus, p.few_least), 12) : 1;
   // workgroups for n row blocks of every (kv head, run) (work_of)
   const auto blocks = [&](long long n, int nsplit) {
@@ -1276,8 +1281,8 @@ PagedPlan plan_paged_attention(int R, int T, int max_rows, int Hq, int Hkv, int 
   // (a workgroup for each compute unit: 4 trees of 64 nodes, 1000 to 4000 slots, 57 us
   // with half of that, 40; a chunk of 512 rows over 4000 slots 95, 66)
   // Over 8-bit pages, whose chunks take as long and whose partial outputs weigh the same,
-  // two workgroups where one would leave units idle, in runs of 256 slots on average (us
-  // with one, with two, with two and shorter runs: the 4 trees 52, 44, 44; the chunk 74, 61,
+  // two workgroups where one would leave units idle, but no more runs than the page table's
+  // capacity has 256 slots (us with one, with two, with two and shorter runs: the 4 trees 52, 44, 44; the chunk 74, 61,
   // 62; 8 trees of 128 nodes, 28 heads over 4 of 64, up to 3000 slots 45, 36, 37; 128 rows
   // over 1000 slots 20.4, 21.5, 24.0; 64 19.4, 20.3, 19.3).
   const bool twice = held && base < cus;
