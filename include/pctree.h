@@ -488,7 +488,8 @@ typedef struct pctree_paged_cache8 {
   int32_t block;            /* 8, 16, 32 or 64, at most page_size                     */
 } pctree_paged_cache8;
 
-/* A block that takes new rows gets the scale of their set, or keeps its own where
+/* A block that takes new rows gets the scale of their set (of all of a tree's nodes,
+ * whichever are accepted later), or keeps its own where
  * slots below prefix_len lie in it and it is the larger; under a grown scale those
  * slots are held again, rounded once more.  Its other slots keep their bytes, which
  * stand for nothing until a row is put there.  A block that takes new rows belongs

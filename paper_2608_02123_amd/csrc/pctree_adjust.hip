@@ -1,17 +1,23 @@
 // Penalties for repeated tokens, biases and a grammar's mask on rows of logits, in place.
 //
-// forbid_kernel: -inf where a row's mask has no bit, eight logits to a lane; where all
-// eight are forbidden they are written without being read, where none is they are not
-// touched.  Bytes bound it.
+// forbid_kernel: -inf where a row's mask has no bit, eight logits to a lane; eight that are
+// all forbidden are written without being read.  A line of 128 bytes is written whole where
+// any of its logits is forbidden, its groups without one read and written back, and not
+// touched where none is.  Waves wait for most of their time (142 of 181 million wave clocks
+// in the call below): each does one piece, whose row, words, logits and stores follow one
+// another.
 // adjust_kernel: a workgroup takes a segment of the vocabulary and some rows of one
 // request.  It counts the request's history in a table of the segment in LDS, so a token's
 // count costs no memory beside the history itself, whatever the history's length; then
 // each wave goes over rows by itself, or over its share of the tokens where rows are few,
 // and touches only the tokens that the table holds.  A tree's node counts its ancestors'
 // tokens: those in the segment are few, and listed for each row.  One row after 2000
-// tokens 5.4 us: parameters, history, table and logits in a chain; 512 rows 22 us, 64
-// single rows 20, their tokens' lines of memory.  (A table that holds most of a small
-// vocabulary: 512 rows of 1,827 tokens 70 us with waves by rows alone, 14 so.)
+// tokens 5.4 us: parameters, history, table and logits in a chain; 512 rows of four trees
+// 22 us, their tokens' lines of memory.  64 single rows of 151,936 after 4000 tokens each 21
+// us, of which 13 are 4800 workgroups that clear and search a table each (as long after 4
+// tokens), 5 their reading the history, 75 times a request, and 3 the lines.  (A table that
+// holds most of a small vocabulary: 512 rows of 1,827 tokens 70 us with waves by rows
+// alone, 14 so.)
 // (Segments of 4096 tokens took 124 us for the 512 rows where these take 84, a mask's pass
 // in this kernel included at the time: fewer workgroups fit a compute unit; of 1024, 106.)
 #include "pctree.h"

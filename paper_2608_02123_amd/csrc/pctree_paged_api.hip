@@ -298,8 +298,9 @@ pctree_status pctree_append_paged8(const pctree_paged_cache8* cache,
     AppendArgs a;
     st = check_append(pages, rows, &a);
     if (st != PCTREE_OK) return st;
-    // (a workgroup for every head of keys and of values at every eighth row, at most, and for
-    // four rows' queries)
+    // (Workgroups of keys and values: at most 4096 where each takes one row, else one for
+    // Share's heads of every `block` rows, so at most rows * kv_heads / 4 + 2 * kv_heads; of
+    // queries one for four rows, or 4096.)
     if ((int64_t)batch->rows * pages->kv_heads > kMaxGrid) return PCTREE_ERR_UNSUPPORTED;
     a.b = rows_of(pages, batch, 16);
     (void)hipGetLastError();
